@@ -419,6 +419,85 @@ kla_status kla_mc_nll(int32_t S, int64_t n, const float* logp, float* nll, hipSt
 kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const float* dnll, float* dlogp,
                                hipStream_t stream);
 
+/*
+ * Linear attention with a decay for each head: the layer's information state with a
+ * given gate in place of the filter's, as retention-style mixers have it beside or in
+ * place of the filter.  Per batch b and head h, with gamma = exp(g[h]),
+ *
+ *   S_t[n,d] = gamma S_{t-1}[n,d] + k_t[n] v_t[d]          y_t[d] = sum_n q_t[n] S_t[n,d]
+ *
+ *   q, k [B, T, H, dk]   v, y [B, T, H, dv]   dtype (the descriptor's, as for the layer)
+ *   g    [H] fp32, the logarithms of the decays: g <= 0 (checked under KLA_CHECK=1), -inf
+ *        for no memory.  The decays are constants of the model and take no gradient.
+ *   s0, sT [B, H, dk, dv] fp32, the states before the first and after the last token: s0
+ *        NULL for zero, sT NULL when it is not wanted.
+ *   len  [B] int32 or NULL: sequence b has len[b] tokens (taken into 0 .. T).  Tokens past
+ *        them are not read, sT is the state after the last of them, and y and the
+ *        gradients of the rows past them are written as zeros.
+ *
+ * The arithmetic is fp32 for either dtype: bf16 products are exact, their fp32 factors
+ * carried to 16 bits or more, and the state keeps its 24 bits.  A value that is not finite
+ * reaches its own token and later ones only (in the backward, earlier ones).  The backward
+ * needs no saved context: it returns dq, dk [B, T, H, dk] and dv [B, T, H, dv] (dtype,
+ * required) and ds0 [B, H, dk, dv] (fp32 or NULL) from dy [B, T, H, dv] and dsT
+ * [B, H, dk, dv] fp32 (NULL: zero).  The step takes one token for S sequences and updates
+ * state [S, H, dk, dv] in place.  H max(dk, dv) <= 2^24 and T <= 2^30.
+ */
+size_t kla_linear_attn_workspace(const kla_desc* desc);
+size_t kla_linear_attn_backward_workspace(const kla_desc* desc);
+kla_status kla_linear_attn_forward(const kla_desc* desc, const void* q, const void* k, const void* v, const float* g,
+                                   const float* s0, const int32_t* len, void* y, float* sT,
+                                   void* ws, size_t ws_bytes, hipStream_t stream);
+kla_status kla_linear_attn_backward(const kla_desc* desc, const void* q, const void* k, const void* v, const float* g,
+                                    const float* s0, const int32_t* len, const void* dy, const float* dsT,
+                                    void* dq, void* dk, void* dv, float* ds0,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+kla_status kla_linear_attn_step(int32_t S, int32_t H, int32_t dk, int32_t dv, int32_t dtype,
+                                const void* q, const void* k, const void* v, const float* g,
+                                float* state, void* y, hipStream_t stream);
+
+/*
+ * Layer norm over rows of n elements (the norm in front of a layer and of the decoder):
+ *
+ *   out = (x - mean) rstd w + bias,   mean = sum x / n,   rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)
+ *
+ *   x, out, dout, dx [rows, n] dtype, n in 1 .. 16384; w [n] fp32; bias [n] fp32 or NULL;
+ *   mean, rstd [rows] fp32: written for the backward (each may be NULL in the forward).
+ * Sums are fp32, the squares about the mean.  dw [n] (required) and dbias [n] (or NULL),
+ * fp32, are overwritten with the sums over the rows, in a fixed order through the workspace.
+ */
+size_t kla_layer_norm_workspace(int32_t n);
+kla_status kla_layer_norm_forward(int64_t rows, int32_t n, int32_t dtype, const void* x, const float* w,
+                                  const float* bias, float eps, void* out, float* mean, float* rstd, hipStream_t stream);
+kla_status kla_layer_norm_backward(int64_t rows, int32_t n, int32_t dtype, const void* x, const float* w,
+                                   const float* mean, const float* rstd, const void* dout, void* dx, float* dw,
+                                   float* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Log probabilities of given tokens, the logp that kla_mc_nll takes (S draws of the logits
+ * of n tokens, the same targets for each; S = 1 for a plain model), with the entropy of
+ * each distribution and its most probable tokens:
+ *
+ *   logp[s, i] = x[s, i, target[i]] - log sum_v exp(x[s, i, v]),   entropy[s, i] = -sum_v p_v log p_v
+ *
+ *   logits x [S, n, V] dtype; target [n] int64: a negative one is no target (logp 0, no
+ *   gradient), one of V or more makes logp NaN.  logp [S, n] fp32; entropy [S, n] fp32 or
+ *   NULL; stat [S, n, 2] fp32 or NULL, for the backward (each row's largest logit and the
+ *   sum of exponentials about it); top (0 .. 32, at most V) tokens: top_logp [S, n, top]
+ *   fp32 and top_index [S, n, top] int64, the largest first and the lower index first among
+ *   equals (-1 and NaN where a row has fewer logits that are not NaN).
+ * Logits of -inf are tokens of probability zero; a row of nothing else has no distribution:
+ * logp -inf, entropy 0, gradient zero.  The backward gives dlogits [S, n, V] dtype from
+ * dlogp and dentropy [S, n] fp32 (either NULL: zero; dentropy needs the entropy).
+ */
+size_t kla_token_logp_workspace(int32_t S, int64_t n, int32_t V, int32_t top);
+kla_status kla_token_logp_forward(int32_t S, int64_t n, int32_t V, int32_t top, int32_t dtype, const void* logits,
+                                  const int64_t* target, float* logp, float* entropy, float* stat, float* top_logp,
+                                  int64_t* top_index, void* ws, size_t ws_bytes, hipStream_t stream);
+kla_status kla_token_logp_backward(int32_t S, int64_t n, int32_t V, int32_t dtype, const void* logits,
+                                   const int64_t* target, const float* stat, const float* entropy, const float* dlogp,
+                                   const float* dentropy, void* dlogits, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char* kla_status_string(kla_status status);
 

@@ -28,7 +28,7 @@ FLAGS = [
 ]
 SOURCES = ["kla_api.cpp", "recurrent.hip", "validate.hip", "ou.hip", "pc.hip", "block.hip", "chunk_fwd.hip",
            "chunk_seg.hip", "chunk_bwd_dv.hip", "chunk_bwd_dk.hip", "chunk64.hip", "chunk64_par.hip",
-           "noalloc.hip", "mc.hip"]
+           "noalloc.hip", "mc.hip", "linattn.hip", "layernorm.hip", "logp.hip"]
 
 
 def _hipcc() -> str:

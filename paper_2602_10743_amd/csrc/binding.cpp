@@ -9,7 +9,9 @@
 // KLA_CHECK=1 the library waits for the stream.
 #include <array>
 #include <string>
+#include <vector>
 
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/extension.h>
 
@@ -218,9 +220,271 @@ py::object decode_step(const Tensor& q, const Tensor& k, const Tensor& v, const 
     return py::make_tuple(y, obj(yvar));
 }
 
+// ---- the operators around the layer: each call runs on its tensors' device, whichever is current
+
+void check_gpu(const Tensor& t, const char* name) {
+    if (!t.is_cuda()) value_error(std::string(name) + " must live on a GPU; there is no CPU path");
+    if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+}
+
+void check_like(const Tensor& t, at::IntArrayRef shape, const Tensor& q, const char* name) {
+    if (t.sizes() != shape) value_error(std::string(name) + " has shape " + shape_str(t.sizes()) + ", expected " + shape_str(shape));
+    if (t.scalar_type() != q.scalar_type() || t.device() != q.device())
+        value_error(std::string(name) + " must share the inputs' dtype and device");
+    if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+}
+
+void check_int(const Opt& t, at::ScalarType type, at::IntArrayRef shape, const Tensor& q, const char* name) {
+    if (!t) return;
+    if (t->scalar_type() != type || t->sizes() != shape || t->device() != q.device() || !t->is_contiguous())
+        value_error(std::string(name) + " must be a contiguous " + (type == at::kInt ? "int32" : "int64") +
+                    " tensor of shape " + shape_str(shape) + " on " + q.device().str());
+}
+
+int32_t int32_of(int64_t n, const char* what) {
+    if (n > INT32_MAX) value_error(std::string(what) + " does not fit 32 bits");
+    return (int32_t)n;
+}
+
+kla_desc check_lin(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s, const Opt& len) {
+    check_gpu(q, "q");
+    const int dt = dtype_of(q);
+    if (q.dim() != 4 || v.dim() != 4) value_error("q must be [B, T, H, dk] and v [B, T, H, dv]");
+    const int64_t B = q.size(0), T = q.size(1), H = q.size(2), dk = q.size(3), dv = v.size(3);
+    check_like(k, {B, T, H, dk}, q, "k");
+    check_like(v, {B, T, H, dv}, q, "v");
+    check_f32(g, {H}, q, "g");
+    check_f32(s, {B, H, dk, dv}, q, "s0");
+    check_int(len, at::kInt, {B}, q, "lengths");
+    return kla_desc{int32_of(B, "B"), int32_of(T, "T"), int32_of(H, "H"), int32_of(dk, "dk"), int32_of(dv, "dv"), (kla_dtype)dt};
+}
+
+// (y, sT) or a status
+py::object linear_attn_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+                               const Opt& len, const Opt& y_in, bool want_state) {
+    const kla_desc d = check_lin(q, k, v, g, s0, len);
+    if (y_in) check_like(*y_in, {d.B, d.T, d.H, d.dv}, q, "y");
+    Tensor y;
+    Opt sT;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(q.device().index());
+        y = y_in ? *y_in : at::empty({d.B, d.T, d.H, d.dv}, q.options());
+        if (want_state) sT = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
+        const size_t nw = kla_linear_attn_workspace(&d);
+        Opt ws;
+        if (nw) ws = bytes(nw, q);
+        st = kla_linear_attn_forward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len),
+                                     ptr(y), fptr(sT), ptr(ws), nw, stream_of(q));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::make_tuple(y, obj(sT));
+}
+
+// (dq, dk, dv, ds0) or a status
+py::object linear_attn_backward(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+                                const Opt& len, const Tensor& dy, const Opt& dsT, bool want_init) {
+    const kla_desc d = check_lin(q, k, v, g, s0, len);
+    check_like(dy, {d.B, d.T, d.H, d.dv}, q, "dy");
+    check_f32(dsT, {d.B, d.H, d.dk, d.dv}, q, "dsT");
+    Tensor dq, dk, dv;
+    Opt ds0;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(q.device().index());
+        dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
+        if (want_init) ds0 = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
+        const size_t nw = kla_linear_attn_backward_workspace(&d);
+        Opt ws;
+        if (nw) ws = bytes(nw, q);
+        st = kla_linear_attn_backward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len),
+                                      ptr(dy), fptr(dsT), ptr(dq), ptr(dk), ptr(dv), fptr(ds0), ptr(ws), nw, stream_of(q));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::make_tuple(dq, dk, dv, obj(ds0));
+}
+
+// y or a status; state updated in place
+py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Tensor& state,
+                            const Opt& y_in) {
+    check_gpu(q, "q");
+    const int dt = dtype_of(q);
+    if (q.dim() != 3 || v.dim() != 3) value_error("q must be [S, H, dk] and v [S, H, dv]");
+    const int64_t S = q.size(0), H = q.size(1), dk = q.size(2), dv = v.size(2);
+    check_like(k, {S, H, dk}, q, "k");
+    check_like(v, {S, H, dv}, q, "v");
+    check_f32(g, {H}, q, "g");
+    check_f32(state, {S, H, dk, dv}, q, "state");
+    if (y_in) check_like(*y_in, {S, H, dv}, q, "y");
+    Tensor y;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(q.device().index());
+        y = y_in ? *y_in : at::empty({S, H, dv}, q.options());
+        st = kla_linear_attn_step(int32_of(S, "S"), int32_of(H, "H"), int32_of(dk, "dk"), int32_of(dv, "dv"), dt, ptr(q), ptr(k),
+                                  ptr(v), (const float*)ptr(g), (float*)ptr(state), ptr(y), stream_of(q));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::cast(y);
+}
+
+struct Rows {
+    int64_t rows;
+    int32_t n;
+    int dtype;
+    std::vector<int64_t> lead;
+};
+
+Rows check_rows(const Tensor& x, const char* name) {
+    check_gpu(x, name);
+    const int dt = dtype_of(x);
+    if (x.dim() < 1) value_error(std::string(name) + " must have a dimension to normalise over");
+    const int64_t n = x.size(-1);
+    std::vector<int64_t> lead(x.sizes().begin(), x.sizes().end() - 1);
+    int64_t rows = 1;
+    for (int64_t s : lead) rows *= s;
+    return {rows, int32_of(n, "the row length"), dt, lead};
+}
+
+// (out, mean, rstd) or a status
+py::object layer_norm_forward(const Tensor& x, const Tensor& w, const Opt& bias, double eps) {
+    const Rows r = check_rows(x, "x");
+    check_f32(w, {r.n}, x, "w");
+    check_f32(bias, {r.n}, x, "bias");
+    Tensor out, mean, rstd;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(x.device().index());
+        out = at::empty_like(x);
+        mean = at::empty(r.lead, x.options().dtype(at::kFloat));
+        rstd = at::empty_like(mean);
+        st = kla_layer_norm_forward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), fptr(bias), (float)eps, ptr(out),
+                                    (float*)ptr(mean), (float*)ptr(rstd), stream_of(x));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::make_tuple(out, mean, rstd);
+}
+
+// (dx, dw, dbias) or a status
+py::object layer_norm_backward(const Tensor& x, const Tensor& w, const Tensor& mean, const Tensor& rstd, const Tensor& dout,
+                               bool want_bias) {
+    const Rows r = check_rows(x, "x");
+    check_f32(w, {r.n}, x, "w");
+    check_f32(mean, r.lead, x, "mean");
+    check_f32(rstd, r.lead, x, "rstd");
+    check_like(dout, x.sizes(), x, "dout");
+    Tensor dx, dw;
+    Opt db;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(x.device().index());
+        dx = at::empty_like(x);
+        dw = at::empty_like(w);
+        if (want_bias) db = at::empty_like(w);
+        const size_t nw = kla_layer_norm_workspace(r.n);
+        const Tensor ws = bytes(nw, x);
+        st = kla_layer_norm_backward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), (const float*)ptr(mean),
+                                     (const float*)ptr(rstd), ptr(dout), ptr(dx), (float*)ptr(dw), fptr(db), ptr(ws), nw,
+                                     stream_of(x));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::make_tuple(dx, dw, obj(db));
+}
+
+struct Logits {
+    int32_t S, V;
+    int64_t n;
+    int dtype;
+    std::vector<int64_t> lead;
+};
+
+// logits [*lead, V], target [*tail] with lead ending in tail: the dimensions before it are draws
+Logits check_logits(const Tensor& x, const Tensor& target) {
+    const Rows r = check_rows(x, "logits");
+    const at::IntArrayRef lead(r.lead), t = target.sizes();
+    if (t.size() > lead.size() || lead.slice(lead.size() - t.size()) != t)
+        value_error("target has shape " + shape_str(t) + ", expected the last dimensions of " + shape_str(lead));
+    check_int(target, at::kLong, t, x, "target");
+    int64_t S = 1;
+    for (size_t i = 0; i < lead.size() - t.size(); ++i) S *= lead[i];
+    return {int32_of(S, "the number of draws"), r.n, target.numel(), r.dtype, r.lead};
+}
+
+// (logp, entropy, stat, top_logp, top_index) or a status
+py::object token_logp_forward(const Tensor& x, const Tensor& target, bool want_entropy, int64_t top, bool want_stat) {
+    const Logits l = check_logits(x, target);
+    if (top < 0 || top > INT32_MAX) value_error("top must not be negative");
+    Tensor logp;
+    Opt entropy, stat, top_logp, top_index;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(x.device().index());
+        const auto f32 = x.options().dtype(at::kFloat);
+        logp = at::empty(l.lead, f32);
+        auto with = [&](int64_t n) {
+            std::vector<int64_t> s = l.lead;
+            s.push_back(n);
+            return s;
+        };
+        if (want_entropy) entropy = at::empty(l.lead, f32);
+        if (want_stat) stat = at::empty(with(2), f32);
+        if (top > 0) {
+            top_logp = at::empty(with(top), f32);
+            top_index = at::empty(with(top), x.options().dtype(at::kLong));
+        }
+        const size_t nw = kla_token_logp_workspace(l.S, l.n, l.V, (int32_t)top);
+        Opt ws;
+        if (nw) ws = bytes(nw, x);
+        st = logp.numel() == 0 ? KLA_OK   // nothing to do, and no draws at all are allowed here
+                               : kla_token_logp_forward(l.S, l.n, l.V, (int32_t)top, l.dtype, ptr(x), (const int64_t*)ptr(target),
+                                                        (float*)ptr(logp), fptr(entropy), fptr(stat), fptr(top_logp),
+                                                        (int64_t*)ptr(top_index), ptr(ws), nw, stream_of(x));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::make_tuple(logp, obj(entropy), obj(stat), obj(top_logp), obj(top_index));
+}
+
+// dlogits or a status
+py::object token_logp_backward(const Tensor& x, const Tensor& target, const Tensor& stat, const Opt& entropy,
+                               const Opt& dlogp, const Opt& dentropy) {
+    const Logits l = check_logits(x, target);
+    std::vector<int64_t> two = l.lead;
+    two.push_back(2);
+    check_f32(stat, two, x, "stat");
+    check_f32(entropy, l.lead, x, "entropy");
+    check_f32(dlogp, l.lead, x, "dlogp");
+    check_f32(dentropy, l.lead, x, "dentropy");
+    Tensor dx;
+    kla_status st;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(x.device().index());
+        dx = at::empty_like(x);
+        st = x.numel() == 0 ? KLA_OK
+                            : kla_token_logp_backward(l.S, l.n, l.V, l.dtype, ptr(x), (const int64_t*)ptr(target),
+                                                      (const float*)ptr(stat), fptr(entropy), fptr(dlogp), fptr(dentropy),
+                                                      ptr(dx), stream_of(x));
+    }
+    if (st != KLA_OK) return py::int_((int)st);
+    return py::cast(dx);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_kla_torch, m) {
+    m.def("linear_attn_forward", &linear_attn_forward);
+    m.def("linear_attn_backward", &linear_attn_backward);
+    m.def("linear_attn_step", &linear_attn_step);
+    m.def("layer_norm_forward", &layer_norm_forward);
+    m.def("layer_norm_backward", &layer_norm_backward);
+    m.def("token_logp_forward", &token_logp_forward);
+    m.def("token_logp_backward", &token_logp_backward);
     m.def("forward", &forward);
     m.def("backward", &backward);
     m.def("decode_step", &decode_step);

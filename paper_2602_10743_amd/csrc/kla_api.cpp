@@ -705,6 +705,178 @@ kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const fl
     return kla::launch_mc_nll_bwd(S, (size_t)n, logp, dnll, dlogp, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
 }
 
+// ---------------------------------------------------------------- linear attention with a decay per head
+
+namespace {
+// Row offsets inside a 32-token chunk are 32-bit.
+kla_status lin_desc(const kla_desc* d) {
+    const kla_status st = check_desc(d);
+    if (st != KLA_OK) return st;
+    const int w = d->dk > d->dv ? d->dk : d->dv;
+    return (int64_t)d->H * w > (1 << 24) || d->T > (1 << 30) ? KLA_ERR_SHAPE : KLA_OK;
+}
+
+// KLA_CHECK=1: g <= 0 for every head (synchronous).
+kla_status lin_domain(const float* g, int H, hipStream_t stream) {
+    if (!check_mode()) return KLA_OK;
+    float host[64];
+    for (int h0 = 0; h0 < H; h0 += 64) {
+        const int n = H - h0 < 64 ? H - h0 : 64;
+        if (hipMemcpyAsync(host, g + h0, n * sizeof(float), hipMemcpyDeviceToHost, stream) != hipSuccess ||
+            hipStreamSynchronize(stream) != hipSuccess)
+            return KLA_ERR_HIP;
+        for (int i = 0; i < n; ++i)
+            if (!(host[i] <= 0.f)) return KLA_ERR_NUMERIC;
+    }
+    return KLA_OK;
+}
+}  // namespace
+
+size_t kla_linear_attn_workspace(const kla_desc* desc) {
+    return lin_desc(desc) == KLA_OK ? round_up(kla::linattn_workspace(shape_of(desc), false)) : 0;
+}
+
+size_t kla_linear_attn_backward_workspace(const kla_desc* desc) {
+    return lin_desc(desc) == KLA_OK ? round_up(kla::linattn_workspace(shape_of(desc), true)) : 0;
+}
+
+kla_status kla_linear_attn_forward(const kla_desc* desc, const void* q, const void* k, const void* v, const float* g,
+                                   const float* s0, const int32_t* len, void* y, float* sT, void* ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+    kla_status st = lin_desc(desc);
+    if (st != KLA_OK) return st;
+    if (!g || (desc->T > 0 && (!q || !k || !v || !y))) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)g, (const void*)s0, (const void*)len, y, (void*)sT, ws)) return KLA_ERR_ALIGN;
+    const size_t need = kla_linear_attn_workspace(desc);
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    st = lin_domain(g, desc->H, stream);
+    if (st != KLA_OK) return st;
+    const kla::LinPass p{q, k, v, y, desc->dk, desc->dv, false, s0, sT, false, false};
+    return kla::launch_linattn(shape_of(desc), p, g, len, ws, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
+kla_status kla_linear_attn_backward(const kla_desc* desc, const void* q, const void* k, const void* v, const float* g,
+                                    const float* s0, const int32_t* len, const void* dy, const float* dsT, void* dq,
+                                    void* dk, void* dv, float* ds0, void* ws, size_t ws_bytes, hipStream_t stream) {
+    kla_status st = lin_desc(desc);
+    if (st != KLA_OK) return st;
+    if (!g || (desc->T > 0 && (!q || !k || !v || !dy || !dq || !dk || !dv))) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)g, (const void*)s0, (const void*)len, dy, (const void*)dsT, dq, dk, dv,
+                     (void*)ds0, ws))
+        return KLA_ERR_ALIGN;
+    const size_t need = kla_linear_attn_backward_workspace(desc);
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    st = lin_domain(g, desc->H, stream);
+    if (st != KLA_OK) return st;
+    const kla::Shape s = shape_of(desc);
+    const kla::LinPass pass[3] = {{dy, v, k, dq, desc->dv, desc->dk, false, s0, nullptr, true, false},
+                                  {v, dy, q, dk, desc->dv, desc->dk, true, dsT, nullptr, true, false},
+                                  {k, q, dy, dv, desc->dk, desc->dv, true, dsT, ds0, false, false}};
+    for (const kla::LinPass& p : pass)
+        if (kla::launch_linattn(s, p, g, len, ws, stream) != hipSuccess) return KLA_ERR_HIP;
+    return KLA_OK;
+}
+
+kla_status kla_linear_attn_step(int32_t S, int32_t H, int32_t dk, int32_t dv, int32_t dtype, const void* q, const void* k,
+                                const void* v, const float* g, float* state, void* y, hipStream_t stream) {
+    const kla_desc d{S, 1, H, dk, dv, dtype};
+    kla_status st = check_desc(&d);
+    if (st != KLA_OK) return st;
+    if (!q || !k || !v || !g || !state || !y) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)g, (void*)state, y)) return KLA_ERR_ALIGN;
+    st = lin_domain(g, H, stream);
+    if (st != KLA_OK) return st;
+    return kla::launch_linattn_step(shape_of(&d), q, k, v, g, state, y, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
+// ---------------------------------------------------------------- layer norm
+
+namespace {
+kla_status norm_shape(int64_t rows, int32_t n, int32_t dtype) {
+    if (dtype != KLA_F32 && dtype != KLA_BF16) return KLA_ERR_DTYPE;
+    if (rows < 0 || n < 1 || n > 16384 || rows > INT64_MAX / n / 4) return KLA_ERR_SHAPE;
+    return KLA_OK;
+}
+}  // namespace
+
+size_t kla_layer_norm_workspace(int32_t n) { return n >= 1 && n <= 16384 ? kla::layernorm_parts_bytes(n) : 0; }
+
+kla_status kla_layer_norm_forward(int64_t rows, int32_t n, int32_t dtype, const void* x, const float* w, const float* bias,
+                                  float eps, void* out, float* mean, float* rstd, hipStream_t stream) {
+    const kla_status st = norm_shape(rows, n, dtype);
+    if (st != KLA_OK) return st;
+    if (!(eps >= 0.f)) return KLA_ERR_SHAPE;
+    if (!w || (rows > 0 && (!x || !out))) return KLA_ERR_NULL;
+    if (!all_aligned(x, (const void*)w, (const void*)bias, out, (void*)mean, (void*)rstd)) return KLA_ERR_ALIGN;
+    return kla::launch_layernorm_fwd((size_t)rows, n, dtype == KLA_BF16, x, w, bias, eps, out, mean, rstd, stream) ==
+                   hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
+}
+
+kla_status kla_layer_norm_backward(int64_t rows, int32_t n, int32_t dtype, const void* x, const float* w, const float* mean,
+                                   const float* rstd, const void* dout, void* dx, float* dw, float* dbias, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+    const kla_status st = norm_shape(rows, n, dtype);
+    if (st != KLA_OK) return st;
+    if (!w || !dw || (rows > 0 && (!x || !mean || !rstd || !dout || !dx))) return KLA_ERR_NULL;
+    if (!all_aligned(x, (const void*)w, (const void*)mean, (const void*)rstd, dout, dx, (void*)dw, (void*)dbias, ws))
+        return KLA_ERR_ALIGN;
+    if (!ws || ws_bytes < kla_layer_norm_workspace(n)) return KLA_ERR_WORKSPACE;
+    return kla::launch_layernorm_bwd((size_t)rows, n, dtype == KLA_BF16, x, w, mean, rstd, dout, dx, dw, dbias,
+                                     static_cast<float*>(ws), stream) == hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
+}
+
+// ---------------------------------------------------------------- log probabilities of tokens
+
+namespace {
+kla_status logp_shape(int32_t S, int64_t n, int32_t V, int32_t top) {
+    // one workgroup per row at least, indices of 32 bits within a row
+    if (S < 1 || n < 0 || V < 1 || V > (1 << 30) || top < 0 || top > 32 || top > V) return KLA_ERR_SHAPE;
+    return n > INT32_MAX / S ? KLA_ERR_SHAPE : KLA_OK;
+}
+}  // namespace
+
+size_t kla_token_logp_workspace(int32_t S, int64_t n, int32_t V, int32_t top) {
+    return logp_shape(S, n, V, top) == KLA_OK ? round_up(kla::logp_workspace((size_t)S * n, V, top)) : 0;
+}
+
+kla_status kla_token_logp_forward(int32_t S, int64_t n, int32_t V, int32_t top, int32_t dtype, const void* logits,
+                                  const int64_t* target, float* logp, float* entropy, float* stat, float* top_logp,
+                                  int64_t* top_index, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (dtype != KLA_F32 && dtype != KLA_BF16) return KLA_ERR_DTYPE;
+    const kla_status st = logp_shape(S, n, V, top);
+    if (st != KLA_OK) return st;
+    if (n > 0 && (!logits || !target || !logp || (top > 0 && (!top_logp || !top_index)))) return KLA_ERR_NULL;
+    if (!all_aligned(logits, (const void*)target, (void*)logp, (void*)entropy, (void*)stat, (void*)top_logp,
+                     (void*)top_index, ws))
+        return KLA_ERR_ALIGN;
+    const size_t need = kla_token_logp_workspace(S, n, V, top);
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    return kla::launch_logp_fwd(S, (size_t)n, V, top, dtype == KLA_BF16, logits, target, logp, entropy, stat, top_logp,
+                                top_index, ws, stream) == hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
+}
+
+kla_status kla_token_logp_backward(int32_t S, int64_t n, int32_t V, int32_t dtype, const void* logits,
+                                   const int64_t* target, const float* stat, const float* entropy, const float* dlogp,
+                                   const float* dentropy, void* dlogits, hipStream_t stream) {
+    if (dtype != KLA_F32 && dtype != KLA_BF16) return KLA_ERR_DTYPE;
+    const kla_status st = logp_shape(S, n, V, 0);
+    if (st != KLA_OK) return st;
+    if (n > 0 && (!logits || !target || !stat || !dlogits || (dentropy && !entropy))) return KLA_ERR_NULL;
+    if (!all_aligned(logits, (const void*)target, (const void*)stat, (const void*)entropy, (const void*)dlogp,
+                     (const void*)dentropy, dlogits))
+        return KLA_ERR_ALIGN;
+    return kla::launch_logp_bwd(S, (size_t)n, V, dtype == KLA_BF16, logits, target, stat, entropy, dlogp, dentropy,
+                                dlogits, stream) == hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
+}
+
 const char* kla_status_string(kla_status s) {
     switch (s) {
         case KLA_OK: return "KLA_OK";

@@ -164,6 +164,42 @@ hipError_t launch_mc_sample_bwd(int S, size_t nrow, int dv, bool bf16, uint64_t 
 hipError_t launch_mc_nll(int S, size_t n, const float* logp, float* nll, hipStream_t st);
 hipError_t launch_mc_nll_bwd(int S, size_t n, const float* logp, const float* dnll, float* dlogp, hipStream_t st);
 
+// Linear attention with a decay for each head (linattn.hip): one pass
+//   y_t = sum_{s <= t} e^{g (t-s)} (q_t . k_s) v_s + what the start state adds
+// over q, k [B, T, H, N] and v, y [B, T, H, D], or with rev the same over the tokens in reverse (the
+// start state then enters undecayed, and the final one is decayed once more).  flip_*: that state
+// is stored [D][N].  len: tokens per sequence [B], or none; rows past them are written as zeros.
+struct LinPass {
+    const void *q, *k, *v;
+    void* y;
+    int N, D;
+    bool rev;
+    const float* start;
+    float* end;
+    bool flip_start, flip_end;
+};
+size_t linattn_workspace(const Shape& s, bool backward);
+hipError_t launch_linattn(const Shape& s, const LinPass& p, const float* g, const int* len, void* ws, hipStream_t st);
+hipError_t launch_linattn_step(const Shape& s, const void* q, const void* k, const void* v, const float* g, float* state,
+                               void* y, hipStream_t st);
+
+// Layer norm over rows of n elements (layernorm.hip).
+size_t layernorm_parts_bytes(int n);
+hipError_t launch_layernorm_fwd(size_t rows, int n, bool bf16, const void* x, const float* w, const float* bias, float eps,
+                                void* out, float* mean, float* rstd, hipStream_t st);
+hipError_t launch_layernorm_bwd(size_t rows, int n, bool bf16, const void* x, const float* w, const float* mean,
+                                const float* rstd, const void* dout, void* dx, float* dw, float* dbias, float* part,
+                                hipStream_t st);
+
+// Log probabilities of tokens (logp.hip): logits [S, n, V], target [n].
+size_t logp_workspace(size_t rows, int V, int top);
+hipError_t launch_logp_fwd(int S, size_t n, int V, int top, bool bf16, const void* logits, const int64_t* target,
+                           float* logp, float* entropy, float* stat, float* top_logp, int64_t* top_index, void* ws,
+                           hipStream_t st);
+hipError_t launch_logp_bwd(int S, size_t n, int V, bool bf16, const void* logits, const int64_t* target,
+                           const float* stat, const float* entropy, const float* dlogp, const float* dentropy,
+                           void* dlogits, hipStream_t st);
+
 // OU gates: gradients of the parameters from the per-part gate-gradient sums (fp32
 // parts, or fp64 when part_f64)
 hipError_t launch_ou_param_grads(int H, int dk, int nparts, const void* part, bool part_f64, const float* a,
