@@ -751,8 +751,8 @@ kla_status kla_linear_attn_forward(const kla_desc* desc, const void* q, const vo
     if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
     st = lin_domain(g, desc->H, stream);
     if (st != KLA_OK) return st;
-    const kla::LinPass p{q, k, v, y, desc->dk, desc->dv, false, s0, sT, false, false};
-    return kla::launch_linattn(shape_of(desc), p, g, len, ws, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+    return kla::launch_linattn_fwd(shape_of(desc), q, k, v, g, s0, len, y, sT, ws, stream) == hipSuccess ? KLA_OK
+                                                                                                   : KLA_ERR_HIP;
 }
 
 kla_status kla_linear_attn_backward(const kla_desc* desc, const void* q, const void* k, const void* v, const float* g,
@@ -768,13 +768,10 @@ kla_status kla_linear_attn_backward(const kla_desc* desc, const void* q, const v
     if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
     st = lin_domain(g, desc->H, stream);
     if (st != KLA_OK) return st;
-    const kla::Shape s = shape_of(desc);
-    const kla::LinPass pass[3] = {{dy, v, k, dq, desc->dv, desc->dk, false, s0, nullptr, true, false},
-                                  {v, dy, q, dk, desc->dv, desc->dk, true, dsT, nullptr, true, false},
-                                  {k, q, dy, dv, desc->dk, desc->dv, true, dsT, ds0, false, false}};
-    for (const kla::LinPass& p : pass)
-        if (kla::launch_linattn(s, p, g, len, ws, stream) != hipSuccess) return KLA_ERR_HIP;
-    return KLA_OK;
+    return kla::launch_linattn_bwd(shape_of(desc), q, k, v, g, s0, len, dy, dsT, dq, dk, dv, ds0, ws, stream) ==
+                   hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
 }
 
 kla_status kla_linear_attn_step(int32_t S, int32_t H, int32_t dk, int32_t dv, int32_t dtype, const void* q, const void* k,

@@ -164,22 +164,13 @@ hipError_t launch_mc_sample_bwd(int S, size_t nrow, int dv, bool bf16, uint64_t 
 hipError_t launch_mc_nll(int S, size_t n, const float* logp, float* nll, hipStream_t st);
 hipError_t launch_mc_nll_bwd(int S, size_t n, const float* logp, const float* dnll, float* dlogp, hipStream_t st);
 
-// Linear attention with a decay for each head (linattn.hip): one pass
-//   y_t = sum_{s <= t} e^{g (t-s)} (q_t . k_s) v_s + what the start state adds
-// over q, k [B, T, H, N] and v, y [B, T, H, D], or with rev the same over the tokens in reverse (the
-// start state then enters undecayed, and the final one is decayed once more).  flip_*: that state
-// is stored [D][N].  len: tokens per sequence [B], or none; rows past them are written as zeros.
-struct LinPass {
-    const void *q, *k, *v;
-    void* y;
-    int N, D;
-    bool rev;
-    const float* start;
-    float* end;
-    bool flip_start, flip_end;
-};
+// Linear attention with a decay for each head (linattn.hip): g [H], len [B] or none (T), states fp32.
 size_t linattn_workspace(const Shape& s, bool backward);
-hipError_t launch_linattn(const Shape& s, const LinPass& p, const float* g, const int* len, void* ws, hipStream_t st);
+hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
+                              const int* len, void* y, float* sT, void* ws, hipStream_t st);
+hipError_t launch_linattn_bwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
+                              const int* len, const void* dy, const float* dsT, void* dq, void* dk, void* dv, float* ds0,
+                              void* ws, hipStream_t st);
 hipError_t launch_linattn_step(const Shape& s, const void* q, const void* k, const void* v, const float* g, float* state,
                                void* y, hipStream_t st);
 

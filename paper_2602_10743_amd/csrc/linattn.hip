@@ -13,11 +13,12 @@
 // start state.  All exponents are at least 0, so no factor exceeds 1 for g <= 0; e^{-inf * 0} is 1.
 //
 // A wave owns CW value columns of one sequence (or segment of one) and their state, in registers;
-// the waves of a workgroup share the chunk's Q, K and V in LDS, double buffered.  Operands: the
-// contraction index of a 32-deep product is {4g .. 4g+3} u {16+4g .. 16+4g+3} for lane group g in
-// every product, so that Q's fragments serve Q K^T and Q R, V's fragments (Q K^T) V and K^T V, and
-// accumulators are operands as they stand.  Rows are stored in 16-byte pieces, piece p of row r at
-// p ^ f(r), which spreads both the reads along rows and those across rows over the LDS banks.
+// the waves of a workgroup share the chunk's Q, K and V in LDS, loaded two chunks ahead.  Accumulators are
+// operands as they stand: over tokens, lane group g holds {4g .. 4g+3} u {16+4g .. 16+4g+3} of a 32-deep
+// product, and the 32 rows of two tiles of the state are dealt so that g holds 8g .. 8g+7 (slot_of),
+// which a lane reads of a row of Q or K with one access.  Q's fragments serve Q K^T and Q R, V's
+// (Q K^T) V and K^T V.  Rows are stored in 16-byte pieces, piece p of row r at p ^ f(r), which
+// spreads both the reads along rows and those across rows over the LDS banks.
 //
 // bf16: v_mfma_f32_16x16x32_bf16.  q, k, v are exact operands; fp32 factors are split into bf16
 // parts: the masked scores and the state (whose products are rounded to bf16 at the end) into two,
@@ -47,11 +48,19 @@ struct Tile {
         constexpr int MASK = NC >= 16 ? 15 : NC - 1;
         return r * NC * 16 + ((c ^ ((r >> SH) & MASK)) << 4);
     }
+    __device__ static int piece_at(int r, int place) { return piece(r, place) / 16 - r * NC; }   // its own inverse
     __device__ static int at(int r, int col) {
         constexpr int PER = 16 / (int)sizeof(E);
         return piece(r, col / PER) + (col % PER) * (int)sizeof(E);
     }
 };
+
+// Slot n of the state's row (tile rt, row m of 16): 32 slots over two tiles, 8g + 4 (rt & 1) + rr at row
+// 4g + rr; a width of 16 is one tile.
+template <int N>
+__device__ __forceinline__ int slot_of(int rt, int m) {
+    return N == 16 ? m : 32 * (rt >> 1) + 8 * (m >> 2) + 4 * (rt & 1) + (m & 3);
+}
 
 // Operands of a 32-deep product: eight values per lane.
 template <typename E>
@@ -61,17 +70,28 @@ template <>
 struct Op<uint16_t> {
     bf16x8 x;
     template <int W>
-    __device__ static Op row(const unsigned char* t, int r, int col, int g4) {   // along row r, from column col
+    __device__ static Op row(const unsigned char* t, int r, int ks, int g4) {   // slots of row r for step ks
         using TL = Tile<uint16_t, W>;
-        const uint2 a = *reinterpret_cast<const uint2*>(t + TL::at(r, col + 4 * g4));
-        uint2 b = {0u, 0u};
-        if constexpr (W > 16) b = *reinterpret_cast<const uint2*>(t + TL::at(r, col + 16 + 4 * g4));
-        return {__builtin_bit_cast(bf16x8, uint4{a.x, a.y, b.x, b.y})};
+        if constexpr (W == 16) {
+            const uint2 a = *reinterpret_cast<const uint2*>(t + TL::at(r, 4 * g4));
+            return {__builtin_bit_cast(bf16x8, uint4{a.x, a.y, 0u, 0u})};
+        } else {
+            return {__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + TL::piece(r, 4 * ks + g4)))};
+        }
+    }
+    template <int W>
+    __device__ static Op slots(const unsigned char* t, int rt, int g4, int l16) {   // down the slots of state tile rt
+        return W == 16 ? tr<W>(t, 4 * (l16 & 3), g4, l16) : tr<W>(t, 32 * (rt >> 1) + 8 * (l16 & 3) + 4 * (rt & 1), g4, l16);
     }
     template <int W>
     __device__ static Op col(const unsigned char* t, int col0, int g4, int l16) {   // down column col0 + l16
+        return tr<W>(t, col0 + 4 * (l16 & 3), g4, l16);
+    }
+    // lane i of 16 gets, over the tokens, column i % 4 of the four that lane i / 4 addresses at c
+    template <int W>
+    __device__ static Op tr(const unsigned char* t, int c, int g4, int l16) {
         using TL = Tile<uint16_t, W>;
-        const int r = 4 * g4 + (l16 >> 2), c = col0 + 4 * (l16 & 3);
+        const int r = 4 * g4 + (l16 >> 2);
         const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(t + TL::at(r, c)));
         const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(t + TL::at(r + 16, c)));
         return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
@@ -82,12 +102,20 @@ template <>
 struct Op<float> {
     float x[8];
     template <int W>
-    __device__ static Op row(const unsigned char* t, int r, int col, int g4) {
+    __device__ static Op row(const unsigned char* t, int r, int ks, int g4) {
         using TL = Tile<float, W>;
-        const float4 a = *reinterpret_cast<const float4*>(t + TL::at(r, col + 4 * g4));
-        float4 b = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (W > 16) b = *reinterpret_cast<const float4*>(t + TL::at(r, col + 16 + 4 * g4));
-        return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+        if constexpr (W == 16) {
+            const float4 a = *reinterpret_cast<const float4*>(t + TL::piece(r, g4));
+            return {{a.x, a.y, a.z, a.w, 0.f, 0.f, 0.f, 0.f}};
+        } else {
+            const float4 a = *reinterpret_cast<const float4*>(t + TL::piece(r, 8 * ks + 2 * g4));
+            const float4 b = *reinterpret_cast<const float4*>(t + TL::piece(r, 8 * ks + 2 * g4 + 1));
+            return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+        }
+    }
+    template <int W>
+    __device__ static Op slots(const unsigned char* t, int rt, int g4, int l16) {
+        return col<W>(t, slot_of<W>(rt, l16) - l16, g4, l16);
     }
     template <int W>
     __device__ static Op col(const unsigned char* t, int col0, int g4, int l16) {
@@ -99,23 +127,59 @@ struct Op<float> {
     }
 };
 
-// Accumulators (rows 4 g4 + rr of two 16-row tiles) as operands.
+// Accumulators (rows 4 g4 + rr of two 16-row tiles) as operands.  bf16: two parts, 16 bits.  What the first
+// leaves is formed by the matrix cores, tile - pick hi with pick[u] minus the unit that takes tile u's rows out
+// of the operand (exact: one product a sum); on the vector units, which bound this kernel, the same takes
+// four instructions for each pair of elements.
 template <typename E>
 struct Acc;
 template <>
 struct Acc<uint16_t> {
-    bf16x8 h, l;   // 16 bits
-    __device__ Acc(const f32x4& a, const f32x4& b) { split8(a, b, h, l); }
+    bf16x8 h, l;
+    struct Pick {
+        bf16x8 of[2];
+        __device__ Pick(int g4, int l16) {
+            uint32_t w[2][4];   // two elements a word
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int e = 2 * i - 4 * u;   // element 2 i is row 4 g4 + e of tile u
+                    w[u][i] = e >= 0 && e < 4 ? (4 * g4 + e == l16 ? 0xbf80u : 4 * g4 + e + 1 == l16 ? 0xbf800000u : 0u) : 0u;
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) of[u] = __builtin_bit_cast(bf16x8, uint4{w[u][0], w[u][1], w[u][2], w[u][3]});
+        }
+    };
+    __device__ Acc() {}
+    template <bool HALF = false>   // HALF: b is zero
+    __device__ static Acc from(const f32x4& a, const f32x4& b, const Pick& pick) {
+        Acc o;
+        const uint4 hi{cvt_pk_bf16(a[0], a[1]), cvt_pk_bf16(a[2], a[3]), HALF ? 0u : cvt_pk_bf16(b[0], b[1]),
+                       HALF ? 0u : cvt_pk_bf16(b[2], b[3])};
+        o.h = __builtin_bit_cast(bf16x8, hi);
+        const f32x4 la = mfma_bf16(pick.of[0], o.h, a), lb = HALF ? zero4() : mfma_bf16(pick.of[1], o.h, b);
+        o.l = __builtin_bit_cast(bf16x8, uint4{cvt_pk_bf16(la[0], la[1]), cvt_pk_bf16(la[2], la[3]),
+                                               HALF ? 0u : cvt_pk_bf16(lb[0], lb[1]), HALF ? 0u : cvt_pk_bf16(lb[2], lb[3])});
+        return o;
+    }
 };
 template <>
 struct Acc<float> {
     float x[8];
-    __device__ Acc(const f32x4& a, const f32x4& b) {
+    struct Pick {
+        __device__ Pick(int, int) {}
+    };
+    __device__ Acc() {}
+    template <bool HALF = false>
+    __device__ static Acc from(const f32x4& a, const f32x4& b, const Pick&) {
+        Acc o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            x[e] = a[e];
-            x[4 + e] = b[e];
+            o.x[e] = a[e];
+            o.x[4 + e] = b[e];
         }
+        return o;
     }
 };
 
@@ -125,6 +189,7 @@ struct Scaled;
 template <>
 struct Scaled<uint16_t> {
     bf16x8 p[3];   // 24 bits
+    __device__ Scaled() {}
     __device__ Scaled(const Op<uint16_t>& v, const float* w) {
         const uint4 u = __builtin_bit_cast(uint4, v.x);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
@@ -146,6 +211,7 @@ struct Scaled<uint16_t> {
 template <>
 struct Scaled<float> {
     float x[8];
+    __device__ Scaled() {}
     __device__ Scaled(const Op<float>& v, const float* w) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = v.x[e] * w[e];
@@ -165,15 +231,26 @@ template <int STEPS = 8>
 __device__ __forceinline__ f32x4 mma(const Op<uint16_t>& a, const Acc<uint16_t>& b, f32x4 c) {
     return mfma2b(a.x, b.h, b.l, c);
 }
-template <int STEPS = 8>
-__device__ __forceinline__ f32x4 mma(const Acc<uint16_t>& a, const Op<uint16_t>& b, f32x4 c) {
-    return mfma2a(a.h, a.l, b.x, c);
+// c[i][j] += a[i] b[j], part after part, so that no product waits for the one before it
+template <int STEPS, int NI>
+__device__ __forceinline__ void mma_each(const Acc<uint16_t> (&a)[NI], const Op<uint16_t> (&b)[2], f32x4 (&c)[NI][2]) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) c[i][j] = mfma_bf16(a[i].l, b[j].x, c[i][j]);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) c[i][j] = mfma_bf16(a[i].h, b[j].x, c[i][j]);
 }
-template <int STEPS = 8>
-__device__ __forceinline__ f32x4 mma(const Op<uint16_t>& a, const Scaled<uint16_t>& b, f32x4 c) {
-    c = mfma_bf16(a.x, b.p[2], c);
-    c = mfma_bf16(a.x, b.p[1], c);
-    return mfma_bf16(a.x, b.p[0], c);
+template <int NI, int NJ>
+__device__ __forceinline__ void mma_each(const Op<uint16_t> (&a)[NI], const Scaled<uint16_t> (&b)[NJ], f32x4 (*c)[NJ]) {
+#pragma unroll
+    for (int s = 2; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) c[i][j] = mfma_bf16(a[i].x, b[j].p[s], c[i][j]);
 }
 template <int STEPS>
 __device__ __forceinline__ f32x4 mma_f32(const float* a, const float* b, f32x4 c) {
@@ -189,13 +266,23 @@ template <int STEPS = 8>
 __device__ __forceinline__ f32x4 mma(const Op<float>& a, const Acc<float>& b, f32x4 c) {
     return mma_f32<STEPS>(a.x, b.x, c);
 }
-template <int STEPS = 8>
-__device__ __forceinline__ f32x4 mma(const Acc<float>& a, const Op<float>& b, f32x4 c) {
-    return mma_f32<STEPS>(a.x, b.x, c);
+template <int STEPS, int NI>
+__device__ __forceinline__ void mma_each(const Acc<float> (&a)[NI], const Op<float> (&b)[2], f32x4 (&c)[NI][2]) {
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) c[i][j] = mfma_f32(a[i].x[e], b[j].x[e], c[i][j]);
 }
-template <int STEPS = 8>
-__device__ __forceinline__ f32x4 mma(const Op<float>& a, const Scaled<float>& b, f32x4 c) {
-    return mma_f32<STEPS>(a.x, b.x, c);
+template <int NI, int NJ>
+__device__ __forceinline__ void mma_each(const Op<float> (&a)[NI], const Scaled<float> (&b)[NJ], f32x4 (*c)[NJ]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) c[i][j] = mfma_f32(a[i].x[e], b[j].x[e], c[i][j]);
 }
 
 // Four output values of one token.
@@ -215,9 +302,9 @@ __device__ __forceinline__ float lds_val(uint16_t, const unsigned char* p) {
 }
 __device__ __forceinline__ float lds_val(float, const unsigned char* p) { return *reinterpret_cast<const float*>(p); }
 
-// (Q K^T o D) V of a chunk again, where a product was not finite: a matrix instruction multiplies later
-// tokens' values by zero scores, and a value that is not finite must not reach the tokens before it.
-template <typename E, int N, int DT>
+// (Q K^T o D) V of a chunk again, where it was not finite: the mask and the matrix instruction multiply
+// later tokens' scores and values by zero, and what is not finite must not reach the tokens before it.
+template <typename E, int N, int D>
 __device__ __forceinline__ f32x4 masked_sums(const unsigned char* sQ, const unsigned char* sK, const unsigned char* sV,
                                              const float* pw, int col0, int i, int g4) {
     f32x4 y = zero4();
@@ -229,21 +316,27 @@ __device__ __forceinline__ f32x4 masked_sums(const unsigned char* sQ, const unsi
             s += lds_val(E(), sQ + Tile<E, N>::at(i, n)) * lds_val(E(), sK + Tile<E, N>::at(j, n));
         s *= pw[i - j];
 #pragma unroll
-        for (int rr = 0; rr < 4; ++rr) y[rr] += s * lds_val(E(), sV + Tile<E, DT>::at(j, col0 + 4 * g4 + rr));
+        for (int rr = 0; rr < 4; ++rr) y[rr] += s * lds_val(E(), sV + Tile<E, D>::at(j, col0 + 4 * g4 + rr));
     }
     return y;
 }
 
+// One pass: Q, K [B, T, H, N] and V, Y [B, T, H, D].
+struct LinJob {
+    const void *q, *k, *v;
+    const float* start;   // start states, or none (0): by sequence, or with ns > 1 by sequence and segment
+    void* y;
+    float* end;           // final states, or none; NOY: the segments' own, by sequence and segment
+    int rev;              // tokens from the last to the first
+    int flip;             // bit 0: the start states, bit 1: the final ones are stored [D][N] instead of [N][D]
+};
+
 struct LinArgs {
-    const void *q, *k, *v;   // Q, K [B, T, H, N], V [B, T, H, D]
-    const float* g;          // [H]
-    const int* len;          // [B] or none
-    const float* start;      // start states, or none (0): by sequence, or with ns > 1 by sequence and segment
-    void* y;                 // [B, T, H, D]
-    float* end;              // final states, or none; NOY: the segments' own, by sequence and segment
-    int B, T, H;
-    int ns, lc, run;         // segments per sequence, chunks in one, segments run
-    int flip;                // bit 0: the start states, bit 1: the final ones are stored [D][N] instead of [N][D]
+    LinJob job[3];        // passes run side by side
+    const float* g;       // [H]
+    const int* len;       // [B] or none
+    int B, T, H, jobs;
+    int ns, lc, run;      // segments per sequence, chunks in one, segments run
 };
 
 // Tokens of sequence b.
@@ -251,108 +344,154 @@ __device__ __forceinline__ int seq_len(const LinArgs& a, int b) {
     return a.len ? min(max(a.len[b], 0), a.T) : a.T;
 }
 
-template <typename E, int N, int NW, int CW>
-constexpr int kLinLds = 2 * (2 * Tile<E, N>::BYTES + Tile<E, NW * CW>::BYTES) + 2 * kLC * (int)sizeof(float);
+// 16 bytes a lane from r at voff into LDS at dst + 16 lane; lanes past the buffer's end write zeros.  Not the
+// compiler's builtin, behind which every transposing read of LDS waits for all loads in flight, the prefetch
+// among them: who reads the tile waits with wait_vm_le.  Nothing is loaded into registers, and nothing else
+// in this file uses m0.
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t words_t;
+__device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_t voff) {
+    words_t u;   // uniform: in scalar registers
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_readfirstlane(r[i]);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
+                 "s"(__builtin_amdgcn_readfirstlane(dst))
+                 : "memory");
+}
 
-template <typename E, int N, int D, int NW, int CW, bool REV, bool NOY>
-__global__ __launch_bounds__(NW * 64) void linattn_kernel(LinArgs a) {
-    constexpr int DT = NW * CW, NTILE = D / DT, NDT = CW / 16, NRT = N / 16, KS = (N + 31) / 32;
-    constexpr int O = REV ? 0 : 1, ES = (int)sizeof(E);
+// Waves of a workgroup, which takes all D columns: D / CW compute; where the rows of Q and K are long and
+// those waves few, others help with the loads.
+template <typename E, int N, int D>
+struct LinCfg {
+    static constexpr int CW = D >= 128 ? 32 : 16, NCW = D / CW, ROW = N * (int)sizeof(E);
+    static constexpr int LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1, NW = NCW > LW ? NCW : LW;
+    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, D>::BYTES, LDS = 3 * BUF + 2 * kLC * (int)sizeof(float);
+    // fp32 states and operands of 128 slots need more than the 256 registers of two waves per SIMD
+    static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 1 : 2;
+};
+
+template <typename E, int N, int D, bool NOY>
+__global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC)) void linattn_kernel(LinArgs a) {
+    using Cfg = LinCfg<E, N, D>;
+    constexpr int CW = Cfg::CW, NW = Cfg::NW, NDT = CW / 16, NRT = N / 16, KS = (N + 31) / 32;
+    constexpr int ES = (int)sizeof(E);
     using TQ = Tile<E, N>;
-    using TV = Tile<E, DT>;
+    using TV = Tile<E, D>;
     constexpr int UQ = NOY ? 0 : TQ::UNITS, UK = TQ::UNITS, UNITS = UQ + UK + TV::UNITS;
-    constexpr int NL = (UNITS + NW - 1) / NW;   // a wave's loads per chunk
-    constexpr int BUF = 2 * TQ::BYTES + TV::BYTES;
+    constexpr int NL = (UNITS + NW - 1) / NW, NLMIN = UNITS / NW;   // a wave's loads per chunk
+    constexpr int NST = NOY ? 0 : 2 * NDT;                          // and stores, of one that computes
+    constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
+    float* pw = reinterpret_cast<float*>(smem + 3 * BUF);   // e^{g n}
 
-    int vi, tile;   // the tiles of one sequence on one XCD: they read the same Q and K
+    int vi, ji;   // the passes over one sequence on one XCD: they read the same rows
     {
         const int i = blockIdx.x, nv = a.B * a.H * a.run;
         if (nv % 8 == 0) {
             const int slot = i / 8;
-            tile = slot % NTILE;
-            vi = (slot / NTILE) * 8 + i % 8;
+            ji = slot % a.jobs;
+            vi = (slot / a.jobs) * 8 + i % 8;
         } else {
-            tile = i % NTILE;
-            vi = i / NTILE;
+            ji = i % a.jobs;
+            vi = i / a.jobs;
         }
     }
+    const LinJob job = a.job[ji];
+    const bool rev = job.rev;
+    const int O = rev ? 0 : 1;
     const int bh = vi / a.run, seg = vi % a.run, b = bh / a.H, h = bh % a.H, H = a.H;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
     const float g = a.g[h];
-    const int Tb = seq_len(a, b);
+    const int Tb = __builtin_amdgcn_readfirstlane(seq_len(a, b));
     const int u0 = seg * a.lc * kLC, nu = min(max(Tb - u0, 0), a.lc * kLC);   // this segment's tokens, in walk order
     const int nchunk = (nu + kLC - 1) / kLC;
-    const int dm0 = tile * DT + wave * CW, dl0 = wave * CW;
+    const int dm0 = wave * CW;
+    const bool works = NW == Cfg::NCW || wave < Cfg::NCW;
 
     if (threadIdx.x < 2 * kLC) pw[threadIdx.x] = decay_pow(g, threadIdx.x);
 
-    // chunk c: its tokens n, and the first of them in memory
-    auto chunk_n = [&](int c) { return min(max(nu - c * kLC, 0), kLC); };
-    auto chunk_t0 = [&](int c, int n) {
-        const int u = u0 + c * kLC;
-        return REV ? Tb - u - n : u;
+    // Chunk c has n = min(nu - 32 c, 32) tokens.  Row r of a full one lies at r, walking backwards at 31 - r,
+    // rows after a place that moves on from chunk to chunk (at); a last one of fewer tokens starts `miss`
+    // rows later there when walking backwards.  Rows past the chunk's tokens fall outside the buffer: behind
+    // its end, or, walking backwards, before its start and so past 2^31.
+    const uint32_t sn = (uint32_t)(H * N * ES), sd = (uint32_t)(H * D * ES);   // bytes from token to token
+    auto row_off = [&](int r, uint32_t stride) { return (uint32_t)(rev ? kLC - 1 - r : r) * stride; };
+    const size_t t0 = (size_t)b * a.T + (rev ? Tb - u0 - kLC : u0);   // may wrap for a short sequence; used with n rows
+    auto at = [&](const void* p, uint32_t stride, int w) {
+        return reinterpret_cast<uintptr_t>(p) + t0 * stride + (uint32_t)(h * w * ES);
     };
-    auto row_off = [&](int r, int n, uint32_t stride) {   // rows past the chunk's tokens fall outside the buffer
-        return REV ? (r < n ? (uint32_t)(n - 1 - r) * stride : 0x80000000u) : (uint32_t)r * stride;
+    auto tokens = [&](int c) { return min(nu - c * kLC, kLC); };
+    // cols: bytes of a row that are read or written
+    auto rsrc_of = [&](uintptr_t p, uint32_t stride, int n, uint32_t cols) {
+        const uint32_t miss = (uint32_t)(kLC - n) * stride;
+        return make_rsrc(reinterpret_cast<const void*>(p + (rev ? miss : 0u)), (kLC - 1) * stride + cols - miss);
     };
-    auto rsrc_of = [&](const void* p, int w, int col, int t0, int n, int cols) {
-        const char* base = static_cast<const char*>(p) + (((size_t)b * a.T + t0) * H + h) * (size_t)(w * ES) + col * ES;
-        return make_rsrc(n > 0 ? base : p, n > 0 ? (uint32_t)(((n - 1) * H * w + cols) * ES) : 0u);
+    auto words_of = [&](uintptr_t p, uint32_t stride, int n, uint32_t cols) {   // the same, for load_lds
+        const uint32_t miss = (uint32_t)(kLC - n) * stride;
+        const uintptr_t q = p + (rev ? miss : 0u);
+        return words_t{(uint32_t)q, (uint32_t)(q >> 32) & 0xffffu, (kLC - 1) * stride + cols - miss, 0x00020000u};
     };
+    auto shift_of = [&](uint32_t stride, int n) { return rev ? (uint32_t)(kLC - n) * stride : 0u; };
+    uintptr_t pq = at(job.q, sn, N), pk = at(job.k, sn, N), pv = at(job.v, sd, D), py = at(job.y, sd, D) + dm0 * ES;
+    const intptr_t step_n = rev ? -(intptr_t)(kLC * (size_t)sn) : (intptr_t)(kLC * (size_t)sn);
+    const intptr_t step_d = rev ? -(intptr_t)(kLC * (size_t)sd) : (intptr_t)(kLC * (size_t)sd);
 
-    uint4 stage[NL];
-    auto load = [&](int c) {
-        const int n = chunk_n(c), t0 = n > 0 ? chunk_t0(c, n) : 0;
-        const rsrc_t rq = rsrc_of(a.q, N, 0, t0, NOY ? 0 : n, N), rk = rsrc_of(a.k, N, 0, t0, n, N);
-        const rsrc_t rv = rsrc_of(a.v, D, tile * DT, t0, n, DT);
+    // Wave load i: 64 pieces of Q, K or V; which, is known at compile time where the tiles are whole rounds
+    // of the workgroup's loads.
+    constexpr bool EVEN = UQ % NW == 0 && UK % NW == 0 && UNITS % NW == 0;
+    auto part_of = [&](int i) { return EVEN ? i * NW : i * NW + wave; };
+    uint32_t goff[NL];   // in a full chunk; the piece that belongs at the lane's place in the tile
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        const int u = i * NW + wave;
+        if (part_of(i) < UQ + UK) {
+            const int x = (part_of(i) < UQ ? u : u - UQ) * 64 + lane;
+            goff[i] = row_off(x / TQ::NC, sn) + (uint32_t)TQ::piece_at(x / TQ::NC, x % TQ::NC) * 16;
+        } else {
+            const int x = (u - UQ - UK) * 64 + lane;
+            goff[i] = row_off(x / TV::NC, sd) + (uint32_t)TV::piece_at(x / TV::NC, x % TV::NC) * 16;
+        }
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    int into = 0;                // the buffer of the next load
+    auto load = [&](int c) {     // chunks in order, each once
+        const int n = tokens(c);
+        const words_t rk = words_of(pk, sn, n, N * ES), rq = NOY ? rk : words_of(pq, sn, n, N * ES);
+        const words_t rv = words_of(pv, sd, n, D * ES);
+        const uint32_t hn = shift_of(sn, n), hd = shift_of(sd, n);
+        pq += step_n;
+        pk += step_n;
+        pv += step_d;
+        const uint32_t dst = lds0 + (NOY ? TQ::BYTES : 0) + into * BUF + wave * 1024;   // tiles follow each other
+        into = into == 2 ? 0 : into + 1;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int u = i * NW + wave;
-            if (u < UQ + UK) {
-                const int x = (u < UQ ? u : u - UQ) * 64 + lane;
-                const uint32_t off = row_off(x / TQ::NC, n, (uint32_t)(H * N * ES)) + (uint32_t)(x % TQ::NC) * 16;
-                stage[i] = buf_ld128(u < UQ ? rq : rk, off, 0);
-            } else if (u < UNITS) {
-                const int x = (u - UQ - UK) * 64 + lane;
-                const uint32_t off = row_off(x / TV::NC, n, (uint32_t)(H * D * ES)) + (uint32_t)(x % TV::NC) * 16;
-                stage[i] = buf_ld128(rv, off, 0);
-            }
-        }
-    };
-    auto put = [&](int c) {
-        unsigned char* buf = smem + (c & 1) * BUF;
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int u = i * NW + wave;
-            if (u < UQ + UK) {
-                const int x = (u < UQ ? u : u - UQ) * 64 + lane;
-                *reinterpret_cast<uint4*>(buf + (u < UQ ? 0 : TQ::BYTES) + TQ::piece(x / TQ::NC, x % TQ::NC)) = stage[i];
-            } else if (u < UNITS) {
-                const int x = (u - UQ - UK) * 64 + lane;
-                *reinterpret_cast<uint4*>(buf + 2 * TQ::BYTES + TV::piece(x / TV::NC, x % TV::NC)) = stage[i];
-            }
+            if (part_of(i) < UQ)
+                load_lds(rq, dst + i * NW * 1024, goff[i] - hn);
+            else if (part_of(i) < UQ + UK)
+                load_lds(rk, dst + i * NW * 1024, goff[i] - hn);
+            else if (part_of(i) < UNITS)
+                load_lds(rv, dst + i * NW * 1024, goff[i] - hd);
         }
     };
 
-    // state R[n, d], n = 16 rt + 4 g4 + rr, d = dm0 + 16 dt + l16
+    // state R[n, d], n = slot_of(rt, 4 g4 + rr), d = dm0 + 16 dt + l16
     const size_t srow = (size_t)bh * a.ns + seg;
     f32x4 R[NRT][NDT];
     auto state_at = [&](int rt, int dt, int rr, bool flip) {
-        const int n = 16 * rt + 4 * g4 + rr, d = dm0 + 16 * dt + l16;
+        const int n = slot_of<N>(rt, 4 * g4 + rr), d = dm0 + 16 * dt + l16;
         return flip ? d * N + n : n * D + d;
     };
     if (nchunk > 0) load(0);
+    if (nchunk > 1) load(1);
     {
-        const float* s0 = NOY || !a.start ? nullptr : a.start + srow * (size_t)(N * D);
+        const float* s0 = NOY || !job.start || !works ? nullptr : job.start + srow * (size_t)(N * D);
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt)
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] = s0 ? s0[state_at(rt, dt, rr, a.flip & 1)] : 0.f;
+                for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] = s0 ? s0[state_at(rt, dt, rr, job.flip & 1)] : 0.f;
     }
     __syncthreads();   // pw
     float dia[4], off[4], rd[2], kw[8];
@@ -368,118 +507,172 @@ __global__ __launch_bounds__(NW * 64) void linattn_kernel(LinArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) kw[e] = pw[max(n - O - (4 * g4 + (e & 3) + (e & 4) * 4), 0)];
     };
+    const typename Acc<E>::Pick pick(g4, l16);
+    const uint32_t yoff[2] = {row_off(l16, sd) + (uint32_t)(4 * g4 * ES), row_off(16 + l16, sd) + (uint32_t)(4 * g4 * ES)};
     weights(kLC);
-    float gn = pw[kLC];
-    if (nchunk > 0) put(0);
-    if (nchunk > 1) load(1);
-    __syncthreads();
-
-    for (int c = 0; c < nchunk; ++c) {
-        const int n = chunk_n(c);
-        const unsigned char* buf = smem + (c & 1) * BUF;
-        const unsigned char *sQ = buf, *sK = buf + TQ::BYTES, *sV = buf + 2 * TQ::BYTES;
-        if (n < kLC) {
-            weights(n);
-            gn = pw[n];
-        }
-        Op<E> vf[NDT];
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) vf[dt] = Op<E>::template col<DT>(sV, dl0 + 16 * dt, g4, l16);
-
-        if constexpr (!NOY) {
-            // S^T[j, i] = K_j . Q_i, tiles (jt, it) = (0,0), (0,1), (1,1); Y^T[d, i] from the state
-            f32x4 s00 = zero4(), s01 = zero4(), s11 = zero4(), y[NDT][2];
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) y[dt][0] = y[dt][1] = zero4();
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                constexpr int ST = N == 16 ? 4 : 8;
-                const Op<E> q0 = Op<E>::template row<N>(sQ, l16, 32 * ks, g4), q1 = Op<E>::template row<N>(sQ, 16 + l16, 32 * ks, g4);
-                const Op<E> k0 = Op<E>::template row<N>(sK, l16, 32 * ks, g4), k1 = Op<E>::template row<N>(sK, 16 + l16, 32 * ks, g4);
-                s00 = mma<ST>(k0, q0, s00);
-                s01 = mma<ST>(k0, q1, s01);
-                s11 = mma<ST>(k1, q1, s11);
-#pragma unroll
-                for (int dt = 0; dt < NDT; ++dt) {
-                    const Acc<E> r(R[2 * ks][dt], N == 16 ? zero4() : R[N == 16 ? 0 : 2 * ks + 1][dt]);
-                    y[dt][0] = mma<ST>(r, q0, y[dt][0]);
-                    y[dt][1] = mma<ST>(r, q1, y[dt][1]);
-                }
-            }
-#pragma unroll
-            for (int rr = 0; rr < 4; ++rr) {   // scores of later tokens are no factor, whatever they are
-                s00[rr] = l16 >= 4 * g4 + rr ? s00[rr] * dia[rr] : 0.f;
-                s01[rr] *= off[rr];
-                s11[rr] = l16 >= 4 * g4 + rr ? s11[rr] * dia[rr] : 0.f;
-            }
-            const Acc<E> p0(s00, zero4()), p1(s01, s11);
-            const int t0 = chunk_t0(c, n);
-            const rsrc_t ry = rsrc_of(a.y, D, dm0, t0, n, CW);
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) {
-                f32x4 in[2] = {mma<4>(vf[dt], p0, zero4()), mma<8>(vf[dt], p1, zero4())};
-                float fin = 0.f;
-#pragma unroll
-                for (int rr = 0; rr < 4; ++rr) fin += 0.f * in[0][rr] + 0.f * in[1][rr];
-                if (__any(fin != 0.f))
-#pragma unroll
-                    for (int it = 0; it < 2; ++it)
-                        in[it] = masked_sums<E, N, DT>(sQ, sK, sV, pw, dl0 + 16 * dt, 16 * it + l16, g4);
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {
-#pragma unroll
-                    for (int rr = 0; rr < 4; ++rr) y[dt][it][rr] = y[dt][it][rr] * rd[it] + in[it][rr];
-                    store4(E(), y[dt][it], ry,
-                           row_off(16 * it + l16, n, (uint32_t)(H * D * ES)) + (uint32_t)((16 * dt + 4 * g4) * ES));
-                }
-            }
-        }
-
-        // R <- e^{g n} R + K^T (w V)
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-            const Scaled<E> vs(vf[dt], kw);
-#pragma unroll
-            for (int rt = 0; rt < NRT; ++rt) {
-#pragma unroll
-                for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] *= gn;
-                R[rt][dt] = mma<8>(Op<E>::template col<N>(sK, 16 * rt, g4, l16), vs, R[rt][dt]);
-            }
-        }
-        if (c + 1 < nchunk) put(c + 1);
-        if (c + 2 < nchunk) load(c + 2);
-        __syncthreads();
-    }
-
-    if (a.end && (NOY || seg == a.ns - 1)) {
-        float* o = a.end + (NOY ? srow : (size_t)bh) * (size_t)(N * D);
+    // The state is rho R, so that its decay is one product a chunk and not one an element, until rho is small.
+    // Uniform: the branches on them are the wave's.
+    auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
+    float gn = uniform(pw[kLC]), rho = 1.f;
+    auto scale = [&](float f) {
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt)
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) o[state_at(rt, dt, rr, !NOY && (a.flip & 2))] = R[rt][dt][rr];
+                for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] *= f;
+    };
+    // the start state has arrived: without this the loop would wait at the state's first use for every
+    // access in flight, in each round
+    wait_vm_all();
+
+    int from = 0;   // this chunk's buffer
+    for (int c = 0; c < nchunk; ++c) {
+        const int n = tokens(c);
+        // this chunk's loads have ended, of this wave and behind the barrier of all: younger are the stores
+        // of two chunks and the loads of one
+        if (c + 1 == nchunk) wait_vm_le<0>();
+        else if (c == 0) wait_vm_le<NLMIN>();
+        else if (!works) wait_vm_le<NLMIN>();
+        else if (c == 1) wait_vm_le<NLMIN + NST>();
+        else wait_vm_le<NLMIN + 2 * NST>();
+        __syncthreads();
+        if (c + 2 < nchunk) load(c + 2);   // into the buffer of the chunk before this one
+        const unsigned char* buf = smem + from * BUF;
+        from = from == 2 ? 0 : from + 1;
+        const unsigned char *sQ = buf, *sK = buf + TQ::BYTES, *sV = buf + 2 * TQ::BYTES;
+        if (n < kLC) {
+            weights(n);
+            gn = uniform(pw[n]);
+        }
+        f32x4 y[NDT][2], in[NDT][2];
+        float rs[2];
+        if (works) {
+            Op<E> vf[NDT];
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) vf[dt] = Op<E>::template col<D>(sV, dm0 + 16 * dt, g4, l16);
+            f32x4 s00 = zero4(), s01 = zero4(), s11 = zero4();
+            if constexpr (!NOY) {
+                // S^T[j, i] = K_j . Q_i, tiles (jt, it) = (0,0), (0,1), (1,1); Y^T[d, i] from the state
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt) y[dt][0] = y[dt][1] = zero4();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    constexpr int ST = N == 16 ? 4 : 8;
+                    const Op<E> qs[2] = {Op<E>::template row<N>(sQ, l16, ks, g4), Op<E>::template row<N>(sQ, 16 + l16, ks, g4)};
+                    const Op<E> k0 = Op<E>::template row<N>(sK, l16, ks, g4), k1 = Op<E>::template row<N>(sK, 16 + l16, ks, g4);
+                    s00 = mma<ST>(k0, qs[0], s00);
+                    s01 = mma<ST>(k0, qs[1], s01);
+                    s11 = mma<ST>(k1, qs[1], s11);
+                    Acc<E> r[NDT];
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+                        r[dt] = Acc<E>::template from<N == 16>(R[2 * ks][dt], N == 16 ? zero4() : R[N == 16 ? 0 : 2 * ks + 1][dt], pick);
+                    mma_each<ST>(r, qs, y);
+                }
+            }
+
+            // R <- e^{g n} R + K^T (w V)
+            const float was = rho;
+            float w[8];
+            rho *= gn;
+            float inv = 1.f;
+            if (rho >= 0x1p-20f) {
+                inv = 1.f / rho;
+            } else {
+                scale(rho);
+                rho = 1.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = kw[e] * inv;
+            Scaled<E> vs[NDT];
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) vs[dt] = Scaled<E>(vf[dt], w);
+            constexpr int RT = NRT >= 2 ? 2 : 1;
+#pragma unroll
+            for (int rt = 0; rt < NRT; rt += RT) {
+                Op<E> kt[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) kt[i] = Op<E>::template slots<N>(sK, rt + i, g4, l16);
+                mma_each<RT, NDT>(kt, vs, R + rt);
+            }
+
+            if constexpr (!NOY) {
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) {
+                    s00[rr] *= dia[rr];
+                    s01[rr] *= off[rr];
+                    s11[rr] *= dia[rr];
+                }
+                const Acc<E> p0 = Acc<E>::template from<true>(s00, zero4(), pick), p1 = Acc<E>::from(s01, s11, pick);
+                float sum = 0.f;   // not finite where a value is not
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt) {
+                    in[dt][0] = mma<4>(vf[dt], p0, zero4());
+                    in[dt][1] = mma<8>(vf[dt], p1, zero4());
+#pragma unroll
+                    for (int rr = 0; rr < 4; ++rr) sum += in[dt][0][rr] + in[dt][1][rr];
+                }
+                rs[0] = rd[0] * was;
+                rs[1] = rd[1] * was;
+                if (__any(!(fabsf(sum) <= 3.4e38f)))
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                        for (int it = 0; it < 2; ++it)
+                            in[dt][it] = masked_sums<E, N, D>(sQ, sK, sV, pw, dm0 + 16 * dt, 16 * it + l16, g4);
+            }
+        }
+        if constexpr (!NOY) {
+            if (works) {
+                const rsrc_t ry = rsrc_of(py, sd, n, CW * ES);
+                const uint32_t hd = shift_of(sd, n);
+                py += step_d;
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const uint32_t to = yoff[it] - hd;
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt) {
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) y[dt][it][rr] = y[dt][it][rr] * rs[it] + in[dt][it][rr];
+                        store4(E(), y[dt][it], ry, to + 16 * dt * ES);
+                    }
+                }
+            }
+        }
+    }
+
+    if (works && job.end && (NOY || seg == a.ns - 1)) {
+        scale(rho);
+        float* o = job.end + (NOY ? srow : (size_t)bh) * (size_t)(N * D);
+#pragma unroll
+        for (int rt = 0; rt < NRT; ++rt)
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) o[state_at(rt, dt, rr, !NOY && (job.flip & 2))] = R[rt][dt][rr];
     }
     if constexpr (!NOY) {   // rows past the sequence's length are zero
         const int z1 = min(a.T, u0 + a.lc * kLC);
-        constexpr int PV = DT * ES / 16;
-        char* y0 = static_cast<char*>(a.y);
+        constexpr int PV = D * ES / 16;
+        char* y0 = static_cast<char*>(job.y);
         for (size_t x = (size_t)max(Tb, u0) * PV + threadIdx.x; x < (size_t)z1 * PV; x += NW * 64)
-            *reinterpret_cast<uint4*>(y0 + ((((size_t)b * a.T + x / PV) * H + h) * D + tile * DT) * ES + (x % PV) * 16) =
+            *reinterpret_cast<uint4*>(y0 + ((((size_t)b * a.T + x / PV) * H + h) * D) * ES + (x % PV) * 16) =
                 uint4{0u, 0u, 0u, 0u};
     }
 }
 
 // Start states of the segments from their own end states, in place: a workgroup takes 256 elements of
-// one sequence's state through its segments.
-__global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int D, const float* __restrict__ s0,
-                                                           float* __restrict__ ends) {
-    const int per = N * D / 256, bh = blockIdx.x / per, x = (blockIdx.x % per) * 256 + threadIdx.x;
+// one sequence's state through its segments.  job.k: the states before the first segments.
+__global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int D) {
+    const int per = N * D / 256, nbh = a.B * a.H;
+    const int bh = blockIdx.x / per % nbh, x = (blockIdx.x % per) * 256 + threadIdx.x;
+    const LinJob& job = a.job[blockIdx.x / per / nbh];
+    const float* s0 = static_cast<const float*>(job.k);
     const int Tb = seq_len(a, bh / a.H), L = a.lc * kLC;
     const float g = a.g[bh % a.H];
-    float* e = ends + (size_t)bh * a.ns * N * D + x;
-    const int sx = a.flip & 1 ? (x % D) * N + x / D : x;
-    float R = s0 ? s0[(size_t)bh * N * D + sx] : 0.f;
+    float* e = job.end + (size_t)bh * a.ns * N * D + x;
+    float R = s0 ? s0[(size_t)bh * N * D + x] : 0.f;
     const float whole = decay_pow(g, L);
     for (int s = 0; s < a.ns; ++s) {
         const float own = s < a.ns - 1 ? e[(size_t)s * N * D] : 0.f;
@@ -489,53 +682,32 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int
     }
 }
 
-template <typename E, int N, int D, int NW, int CW, bool REV, bool NOY>
+template <typename E, int N, int D, bool NOY>
 hipError_t launch(const LinArgs& a, hipStream_t st) {
-    auto kern = linattn_kernel<E, N, D, NW, CW, REV, NOY>;
-    constexpr int LDS = kLinLds<E, N, NW, CW>;
+    using Cfg = LinCfg<E, N, D>;
+    auto kern = linattn_kernel<E, N, D, NOY>;
     // more than 64 KiB of LDS must be opted into once per kernel (thread-safe static init)
     static const hipError_t attr =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS);
     if (attr != hipSuccess) return attr;
-    const unsigned grid = (unsigned)((size_t)a.B * a.H * a.run * (D / (NW * CW)));
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(NW * 64), LDS, st, a);
+    const size_t grid = (size_t)a.B * a.H * a.run * a.jobs;
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::NW * 64), Cfg::LDS, st, a);
     return hipGetLastError();
 }
 
-template <typename E, int N, int D, bool REV>
-hipError_t run_pass(LinArgs a, const float* s0, float* ws, hipStream_t st) {
-    constexpr int CW = 16, NW = D >= 64 ? 4 : D / 16;
-    a.run = a.ns;
-    a.start = s0;
-    if (a.ns > 1) {   // the segments' own end states, their start states from those, then the segments
-        LinArgs p = a;
-        p.run = a.ns - 1;
-        p.end = ws;
-        hipError_t e = launch<E, N, D, NW, CW, REV, true>(p, st);
-        if (e != hipSuccess) return e;
-        linattn_join_kernel<<<dim3((unsigned)((size_t)a.B * a.H * (N * D / 256))), dim3(256), 0, st>>>(a, N, D, s0, ws);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        a.start = ws;
-        a.flip &= 2;
-    }
-    return launch<E, N, D, NW, CW, REV, false>(a, st);
-}
-
-template <typename E, int N, int D>
-hipError_t run_dir(const LinArgs& a, bool rev, const float* s0, float* ws, hipStream_t st) {
-    return rev ? run_pass<E, N, D, true>(a, s0, ws, st) : run_pass<E, N, D, false>(a, s0, ws, st);
-}
-
 template <typename E>
-hipError_t run(const LinArgs& a, int N, int D, bool rev, const float* s0, float* ws, hipStream_t st) {
+hipError_t run(const LinArgs& a, int N, int D, bool noy, hipStream_t st) {
 #define KLA_LIN(N_, D_) \
-    if (N == N_ && D == D_) return run_dir<E, N_, D_>(a, rev, s0, ws, st);
+    if (N == N_ && D == D_) return noy ? launch<E, N_, D_, true>(a, st) : launch<E, N_, D_, false>(a, st);
 #define KLA_LIN_ROW(N_) KLA_LIN(N_, 16) KLA_LIN(N_, 32) KLA_LIN(N_, 64) KLA_LIN(N_, 128)
     KLA_LIN_ROW(16) KLA_LIN_ROW(32) KLA_LIN_ROW(64) KLA_LIN_ROW(128)
 #undef KLA_LIN_ROW
 #undef KLA_LIN
     return hipErrorInvalidValue;
+}
+
+hipError_t run(const Shape& s, const LinArgs& a, int N, int D, bool noy, hipStream_t st) {
+    return s.bf16 ? run<uint16_t>(a, N, D, noy, st) : run<float>(a, N, D, noy, st);
 }
 
 // One token: state <- e^g state + k v^T in place, y = state^T q.  A workgroup of 256 threads takes CT
@@ -616,46 +788,102 @@ hipError_t step(const Shape& s, const void* q, const void* k, const void* v, con
     }
 }
 
-// Segments of a pass whose values are D wide, and chunks in one.
-void segments(const Shape& s, int D, int& ns, int& lc) {
+// Segments per sequence and chunks in one, for passes whose workgroups number `groups` without.  Segments
+// cost a pass over K and V for their states and two launches more, so a sequence of fewer than 16 chunks
+// is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, us: the backward of B = 8,
+// T = 2048, H = 16, 384 workgroups, 228 whole and 252 in two; the forward, 128 workgroups, 142 whole, 124
+// in two, 109 in four).  Otherwise two workgroups a CU, of two chunks at least (B = 3, T = 777, H = 5, 64
+// and 128 wide, forward: 32 whole, 21 in twelve, 29 in 25 segments).
+void segments(const Shape& s, long groups, int& ns, int& lc) {
     const int nc = (s.T + kLC - 1) / kLC;
-    const long groups = (long)s.B * s.H * (D >= 64 ? D / 64 : 1);
     ns = 1;
-    while (groups * ns < 512 && nc / (2 * ns) >= 8) ns *= 2;
+    lc = nc;
+    if (nc < 16 || groups >= 256) return;
+    const long want = (512 + groups - 1) / groups;
+    ns = (int)(want < nc / 2 ? want : nc / 2);
     lc = (nc + ns - 1) / ns;
-    ns = lc > 0 ? (nc + lc - 1) / lc : 1;
-    if (ns < 1) ns = 1;
+    ns = (nc + lc - 1) / lc;
+}
+
+LinArgs args_of(const Shape& s, const float* g, const int* len, long groups) {
+    LinArgs a{};
+    a.g = g;
+    a.len = len;
+    a.B = s.B;
+    a.T = s.T;
+    a.H = s.H;
+    segments(s, groups, a.ns, a.lc);
+    return a;
+}
+
+// States before the segments of `jobs` passes over [dk][dv] states, from q, k, v and start states as in job:
+// into st0[j], by sequence and segment.
+hipError_t start_states(const Shape& s, const LinArgs& a, const LinJob* job, float* const* st0, int jobs, hipStream_t st) {
+    LinArgs p = a;
+    p.jobs = jobs;
+    p.run = a.ns - 1;
+    for (int j = 0; j < jobs; ++j) {
+        p.job[j] = job[j];
+        p.job[j].end = st0[j];
+    }
+    hipError_t e = run(s, p, s.dk, s.dv, true, st);
+    if (e != hipSuccess) return e;
+    for (int j = 0; j < jobs; ++j) p.job[j].k = job[j].start;
+    const size_t grid = (size_t)s.B * s.H * (s.dk * s.dv / 256) * jobs;
+    linattn_join_kernel<<<dim3((unsigned)grid), dim3(256), 0, st>>>(p, s.dk, s.dv);
+    return hipGetLastError();
+}
+
+size_t states_bytes(const Shape& s, int ns) {
+    return ns > 1 ? (size_t)s.B * s.H * ns * s.dk * s.dv * sizeof(float) : 0;
 }
 
 }  // namespace
 
 size_t linattn_workspace(const Shape& s, bool backward) {
-    size_t most = 0;
-    for (int D : {s.dv, backward ? s.dk : s.dv}) {
-        int ns, lc;
-        segments(s, D, ns, lc);
-        const size_t n = ns > 1 ? (size_t)s.B * s.H * ns * s.dk * s.dv * sizeof(float) : 0;
-        most = n > most ? n : most;
-    }
-    return most;
+    const LinArgs a = args_of(s, nullptr, nullptr, (backward ? 3L : 1L) * s.B * s.H);
+    return (backward ? 2 : 1) * states_bytes(s, a.ns);
 }
 
-hipError_t launch_linattn(const Shape& s, const LinPass& p, const float* g, const int* len, void* ws, hipStream_t st) {
-    LinArgs a{};
-    a.q = p.q;
-    a.k = p.k;
-    a.v = p.v;
-    a.g = g;
-    a.len = len;
-    a.y = p.y;
-    a.end = p.end;
-    a.B = s.B;
-    a.T = s.T;
-    a.H = s.H;
-    a.flip = (p.flip_start ? 1 : 0) | (p.flip_end ? 2 : 0);
-    segments(s, p.D, a.ns, a.lc);
-    return s.bf16 ? run<uint16_t>(a, p.N, p.D, p.rev, p.start, static_cast<float*>(ws), st)
-                  : run<float>(a, p.N, p.D, p.rev, p.start, static_cast<float*>(ws), st);
+hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
+                              const int* len, void* y, float* sT, void* ws, hipStream_t st) {
+    LinArgs a = args_of(s, g, len, (long)s.B * s.H);
+    a.jobs = 1;
+    a.run = a.ns;
+    a.job[0] = LinJob{q, k, v, s0, y, sT, 0, 0};
+    if (a.ns > 1) {
+        float* st0 = static_cast<float*>(ws);
+        const hipError_t e = start_states(s, a, a.job, &st0, 1, st);
+        if (e != hipSuccess) return e;
+        a.job[0].start = st0;
+    }
+    return run(s, a, s.dk, s.dv, false, st);
+}
+
+hipError_t launch_linattn_bwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
+                              const int* len, const void* dy, const float* dsT, void* dq, void* dk, void* dv, float* ds0,
+                              void* ws, hipStream_t st) {
+    LinArgs a = args_of(s, g, len, 3L * s.B * s.H);
+    a.run = a.ns;
+    const float *first = s0, *last = dsT;
+    if (a.ns > 1) {   // the states before the segments, and their adjoints behind them
+        float* st0[2] = {static_cast<float*>(ws), static_cast<float*>(ws) + states_bytes(s, a.ns) / sizeof(float)};
+        const LinJob j[2] = {{nullptr, k, v, s0, nullptr, nullptr, 0, 0}, {nullptr, q, dy, dsT, nullptr, nullptr, 1, 0}};
+        const hipError_t e = start_states(s, a, j, st0, 2, st);
+        if (e != hipSuccess) return e;
+        first = st0[0];
+        last = st0[1];
+    }
+    // the states of dq and dk are the transposes [dv][dk]
+    a.job[0] = LinJob{dy, v, k, first, dq, nullptr, 0, 1};
+    a.job[1] = LinJob{v, dy, q, last, dk, nullptr, 1, 1};
+    a.job[2] = LinJob{k, q, dy, last, dv, ds0, 1, 0};
+    a.jobs = s.dk == s.dv ? 3 : 2;
+    const hipError_t e = run(s, a, s.dv, s.dk, false, st);
+    if (e != hipSuccess || a.jobs == 3) return e;
+    a.job[0] = a.job[2];
+    a.jobs = 1;
+    return run(s, a, s.dk, s.dv, false, st);
 }
 
 hipError_t launch_linattn_step(const Shape& s, const void* q, const void* k, const void* v, const float* g, float* state,
