@@ -29,9 +29,9 @@ __all__ = ["kla_forward", "kla_backward", "kla_backward_noalloc", "kla_decode_st
            "kla_gate_forward", "kla_gate_backward",
            "kla_mc_sample", "kla_mc_sample_backward", "kla_mc_nll", "kla_mc_nll_backward", "KLAMCSample",
            "KLAMCNLL", "kla_mc_nll_loss",
-           "kla_linear_attn_forward", "kla_linear_attn_backward", "kla_linear_attn_step", "KLALinearAttn",
-           "kla_linear_attn", "kla_layer_norm_forward", "kla_layer_norm_backward", "KLALayerNorm", "kla_layer_norm",
-           "kla_token_logp_forward", "kla_token_logp_backward", "KLATokenLogp", "kla_token_logp",
+           "kla_linear_attn_forward", "kla_linear_attn_backward", "kla_linear_attn_step", "kla_linear_attn",
+           "kla_layer_norm_forward", "kla_layer_norm_backward", "kla_layer_norm",
+           "kla_token_logp_forward", "kla_token_logp_backward", "kla_token_logp",
            "KLAError", "KLAFilter", "kla_filter", "KLAFilterOU", "kla_filter_ou", "library_path"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -790,92 +790,49 @@ def kla_filter_pc_ou(q, k, v, a, p, delta, r):
 
 
 # ------------------------------------------------------------------ linear attention with a decay per head
-def _ok(out, where: str):
-    if isinstance(out, int):
-        raise KLAError(out, where)
-    return out
-
-
 def kla_linear_attn_forward(q, k, v, g, s0=None, lengths=None, *, want_state: bool = True, y=None) -> dict:
     """S_t = exp(g) S_{t-1} + k_t v_t^T, y_t = S_t^T q_t over a whole sequence.  q, k [B, T, H, dk] and
     v [B, T, H, dv] in one dtype (fp32 or bf16), g [H] fp32 (log decays, <= 0), s0 [B, H, dk, dv] fp32
     or None (zero), lengths [B] int32 or None: sequence b has lengths[b] tokens, y is zero past them.
     Returns y and, as asked, the state sT after the last token."""
-    y, sT = _ok(_native().linear_attn_forward(q, k, v, g, s0, lengths, y, want_state), "kla_linear_attn_forward")
+    y, sT = _native().linear_attn_forward(q, k, v, g, s0, lengths, y, want_state)
     return {"y": y, "sT": sT}
 
 
 def kla_linear_attn_backward(q, k, v, g, s0, lengths, dy, dsT=None, *, want_init_grads: bool = True) -> dict:
     """Gradients of kla_linear_attn_forward's (y, sT): dq, dk, dv in the input dtype (zero past a
     sequence's tokens) and, when asked, ds0 [B, H, dk, dv] fp32."""
-    out = _ok(_native().linear_attn_backward(q, k, v, g, s0, lengths, dy, dsT, want_init_grads),
-              "kla_linear_attn_backward")
+    out = _native().linear_attn_backward(q, k, v, g, s0, lengths, dy, dsT, want_init_grads)
     return dict(zip(("dq", "dk", "dv", "ds0"), out))
 
 
 def kla_linear_attn_step(q, k, v, g, state, *, y=None) -> dict:
     """One token for S sequences: q, k [S, H, dk]; v [S, H, dv]; g [H] fp32; state [S, H, dk, dv] fp32 is
     updated in place."""
-    return {"y": _ok(_native().linear_attn_step(q, k, v, g, state, y), "kla_linear_attn_step"), "state": state}
-
-
-class KLALinearAttn(torch.autograd.Function):
-    """Autograd wrapper: y, sT = linear attention(q, k, v, g, s0, lengths)."""
-
-    @staticmethod
-    def forward(ctx, q, k, v, g, s0, lengths):
-        if ctx.needs_input_grad[3]:
-            raise ValueError("g holds constants: the decays take no gradient")
-        out = kla_linear_attn_forward(q, k, v, g, s0, lengths)
-        ctx.save_for_backward(q, k, v, g, s0, lengths)
-        ctx.set_materialize_grads(False)
-        return out["y"], out["sT"]
-
-    @staticmethod
-    def backward(ctx, dy, dsT):
-        q, k, v, g, s0, lengths = ctx.saved_tensors
-        dy, _, dsT, _ = _split_grads(q, v, False, (dy, dsT, None))
-        out = kla_linear_attn_backward(q, k, v, g, s0, lengths, dy, dsT, want_init_grads=ctx.needs_input_grad[4])
-        return out["dq"], out["dk"], out["dv"], None, out["ds0"], None
+    return {"y": _native().linear_attn_step(q, k, v, g, state, y), "state": state}
 
 
 def kla_linear_attn(q, k, v, g, s0=None, lengths=None):
-    """Differentiable linear attention with a decay for each head: returns (y, sT)."""
-    return KLALinearAttn.apply(q, k, v, g, s0, lengths)
+    """Differentiable linear attention with a decay for each head: returns (y, sT).  The decays are
+    constants: a g that requires a gradient is refused."""
+    return _native().linear_attn(q, k, v, g, s0, lengths)
 
 
 # ------------------------------------------------------------------ layer norm
 def kla_layer_norm_forward(x, w, bias=None, eps: float = 1e-5):
     """Layer norm of the rows (last dimension n, at most 16384) of x with w [n] and bias [n] fp32 or None;
     returns (out, mean, rstd)."""
-    return _ok(_native().layer_norm_forward(x, w, bias, float(eps)), "kla_layer_norm_forward")
+    return _native().layer_norm_forward(x, w, bias, float(eps))
 
 
 def kla_layer_norm_backward(x, w, mean, rstd, dout, *, want_bias: bool = True):
     """(dx, dw, dbias) of kla_layer_norm_forward; dbias is None unless asked for."""
-    return _ok(_native().layer_norm_backward(x, w, mean, rstd, dout, want_bias), "kla_layer_norm_backward")
-
-
-class KLALayerNorm(torch.autograd.Function):
-    """Autograd wrapper: out = layer norm(x, w, bias)."""
-
-    @staticmethod
-    def forward(ctx, x, w, bias, eps):
-        x = x.contiguous()
-        out, mean, rstd = kla_layer_norm_forward(x, w, bias, eps)
-        ctx.save_for_backward(x, w, mean, rstd)
-        return out
-
-    @staticmethod
-    def backward(ctx, dout):
-        x, w, mean, rstd = ctx.saved_tensors
-        dx, dw, db = kla_layer_norm_backward(x, w, mean, rstd, dout.contiguous(), want_bias=ctx.needs_input_grad[2])
-        return dx, dw, db, None
+    return _native().layer_norm_backward(x, w, mean, rstd, dout, want_bias)
 
 
 def kla_layer_norm(x, w, bias=None, eps: float = 1e-5):
     """Differentiable layer norm over the last dimension."""
-    return KLALayerNorm.apply(x, w, bias, eps)
+    return _native().layer_norm(x, w, bias, float(eps))
 
 
 # ------------------------------------------------------------------ log probabilities of tokens
@@ -884,35 +841,17 @@ def kla_token_logp_forward(logits, target, *, want_entropy: bool = False, top: i
     them (fp32 or bf16); a negative target is none (0).  Returns logp and, as asked, the entropies, the
     top <= 32 most probable tokens (top_logp, top_index; the lower index first among equals) and stat for
     kla_token_logp_backward."""
-    out = _ok(_native().token_logp_forward(logits, target, want_entropy, int(top), save), "kla_token_logp_forward")
+    out = _native().token_logp_forward(logits, target, want_entropy, int(top), save)
     return dict(zip(("logp", "entropy", "stat", "top_logp", "top_index"), out))
 
 
 def kla_token_logp_backward(logits, target, stat, entropy, dlogp, dentropy=None):
     """dlogits of kla_token_logp_forward for the gradients of logp and of the entropy (either may be None;
     entropy, the forward's, is needed with dentropy)."""
-    return _ok(_native().token_logp_backward(logits, target, stat, entropy, dlogp, dentropy), "kla_token_logp_backward")
-
-
-class KLATokenLogp(torch.autograd.Function):
-    """Autograd wrapper: logp[, entropy] of the tokens target under the logits."""
-
-    @staticmethod
-    def forward(ctx, want_entropy, logits, target):
-        logits, target = logits.contiguous(), target.contiguous()
-        out = kla_token_logp_forward(logits, target, want_entropy=want_entropy, save=True)
-        ctx.save_for_backward(logits, target, out["stat"], out["entropy"])
-        ctx.set_materialize_grads(False)
-        return (out["logp"], out["entropy"]) if want_entropy else out["logp"]
-
-    @staticmethod
-    def backward(ctx, dlogp, dentropy=None):
-        logits, target, stat, entropy = ctx.saved_tensors
-        c = lambda t: None if t is None else t.contiguous()
-        return None, kla_token_logp_backward(logits, target, stat, entropy, c(dlogp), c(dentropy)), None
+    return _native().token_logp_backward(logits, target, stat, entropy, dlogp, dentropy)
 
 
 def kla_token_logp(logits, target, *, want_entropy: bool = False):
     """Differentiable log probabilities of the tokens target, or (logp, entropy) with want_entropy; the
     logp of S draws [S, n] is what kla_mc_nll takes."""
-    return KLATokenLogp.apply(bool(want_entropy), logits, target)
+    return _native().token_logp(logits, target, bool(want_entropy))

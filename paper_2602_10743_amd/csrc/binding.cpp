@@ -8,6 +8,7 @@
 // up the interpreter lock, as ctypes does: allocations and a full launch queue can block, and under
 // KLA_CHECK=1 the library waits for the stream.
 #include <array>
+#include <stdexcept>
 #include <string>
 #include <vector>
 
@@ -259,54 +260,113 @@ kla_desc check_lin(const Tensor& q, const Tensor& k, const Tensor& v, const Tens
     return kla_desc{int32_of(B, "B"), int32_of(T, "T"), int32_of(H, "H"), int32_of(dk, "dk"), int32_of(dv, "dv"), (kla_dtype)dt};
 }
 
-// (y, sT) or a status
+// A call the library refused: KLAError in Python (the translator below).
+struct Refused : std::runtime_error {
+    kla_status status;
+    const char* where;
+    Refused(kla_status s, const char* w) : std::runtime_error(std::string(w) + ": " + kla_status_string(s)), status(s), where(w) {}
+};
+
+void ok(kla_status s, const char* where) {
+    if (s != KLA_OK) throw Refused(s, where);
+}
+
+using Tensors = torch::autograd::variable_list;
+using Ctx = torch::autograd::AutogradContext;
+Opt some(const Tensor& t) { return t.defined() ? Opt(t) : Opt(); }
+Tensor or_undefined(const Opt& t) { return t ? *t : Tensor(); }
+// An upstream gradient as the library takes it.
+Tensor dense(const Tensor& t) { return t.defined() ? t.contiguous() : t; }
+
+// The raw calls take checked tensors and need no interpreter lock.
+Tensors lin_forward(const kla_desc& d, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+                    const Opt& len, const Opt& y_in, bool want_state) {
+    const c10::hip::HIPGuard on(q.device().index());
+    const Tensor y = y_in ? *y_in : at::empty({d.B, d.T, d.H, d.dv}, q.options());
+    Opt sT, ws;
+    if (want_state) sT = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
+    const size_t nw = kla_linear_attn_workspace(&d);
+    if (nw) ws = bytes(nw, q);
+    ok(kla_linear_attn_forward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len), ptr(y),
+                               fptr(sT), ptr(ws), nw, stream_of(q)),
+       "kla_linear_attn_forward");
+    return {y, or_undefined(sT)};
+}
+
+Tensors lin_backward(const kla_desc& d, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+                     const Opt& len, const Tensor& dy, const Opt& dsT, bool want_init) {
+    const c10::hip::HIPGuard on(q.device().index());
+    const Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
+    Opt ds0, ws;
+    if (want_init) ds0 = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
+    const size_t nw = kla_linear_attn_backward_workspace(&d);
+    if (nw) ws = bytes(nw, q);
+    ok(kla_linear_attn_backward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len), ptr(dy),
+                                fptr(dsT), ptr(dq), ptr(dk), ptr(dv), fptr(ds0), ptr(ws), nw, stream_of(q)),
+       "kla_linear_attn_backward");
+    return {dq, dk, dv, or_undefined(ds0)};
+}
+
+// (y, sT)
 py::object linear_attn_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
                                const Opt& len, const Opt& y_in, bool want_state) {
     const kla_desc d = check_lin(q, k, v, g, s0, len);
     if (y_in) check_like(*y_in, {d.B, d.T, d.H, d.dv}, q, "y");
-    Tensor y;
-    Opt sT;
-    kla_status st;
+    Tensors out;
     {
         py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(q.device().index());
-        y = y_in ? *y_in : at::empty({d.B, d.T, d.H, d.dv}, q.options());
-        if (want_state) sT = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
-        const size_t nw = kla_linear_attn_workspace(&d);
-        Opt ws;
-        if (nw) ws = bytes(nw, q);
-        st = kla_linear_attn_forward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len),
-                                     ptr(y), fptr(sT), ptr(ws), nw, stream_of(q));
+        out = lin_forward(d, q, k, v, g, s0, len, y_in, want_state);
     }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::make_tuple(y, obj(sT));
+    return py::make_tuple(out[0], obj(some(out[1])));
 }
 
-// (dq, dk, dv, ds0) or a status
+// (dq, dk, dv, ds0)
 py::object linear_attn_backward(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
                                 const Opt& len, const Tensor& dy, const Opt& dsT, bool want_init) {
     const kla_desc d = check_lin(q, k, v, g, s0, len);
     check_like(dy, {d.B, d.T, d.H, d.dv}, q, "dy");
     check_f32(dsT, {d.B, d.H, d.dk, d.dv}, q, "dsT");
-    Tensor dq, dk, dv;
-    Opt ds0;
-    kla_status st;
+    Tensors out;
     {
         py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(q.device().index());
-        dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
-        if (want_init) ds0 = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
-        const size_t nw = kla_linear_attn_backward_workspace(&d);
-        Opt ws;
-        if (nw) ws = bytes(nw, q);
-        st = kla_linear_attn_backward(&d, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), fptr(s0), (const int32_t*)ptr(len),
-                                      ptr(dy), fptr(dsT), ptr(dq), ptr(dk), ptr(dv), fptr(ds0), ptr(ws), nw, stream_of(q));
+        out = lin_backward(d, q, k, v, g, s0, len, dy, dsT, want_init);
     }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::make_tuple(dq, dk, dv, obj(ds0));
+    return py::make_tuple(out[0], out[1], out[2], obj(some(out[3])));
 }
 
-// y or a status; state updated in place
+// y, sT with their gradients.  Nodes in C++: through Python's they took most of a small training step.
+struct LinearAttn : torch::autograd::Function<LinearAttn> {
+    static Tensors forward(Ctx* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+                           const Opt& len, const kla_desc& d) {
+        ctx->save_for_backward({q, k, v, g, or_undefined(s0), or_undefined(len)});
+        ctx->set_materialize_grads(false);   // an unused output's gradient stays undefined: nothing to fill or read
+        ctx->saved_data["init"] = s0 && s0->requires_grad();
+        return lin_forward(d, q, k, v, g, s0, len, c10::nullopt, true);
+    }
+    static Tensors backward(Ctx* ctx, Tensors up) {
+        const Tensors x = ctx->get_saved_variables();
+        const Tensor &q = x[0], &v = x[2];
+        const kla_desc d{(int32_t)q.size(0), (int32_t)q.size(1), (int32_t)q.size(2), (int32_t)q.size(3), (int32_t)v.size(3),
+                         q.scalar_type() == at::kFloat ? KLA_F32 : KLA_BF16};
+        const Tensor dy = up[0].defined() ? up[0].contiguous() : at::zeros_like(v);
+        const Tensors out = lin_backward(d, q, x[1], v, x[3], some(x[4]), some(x[5]), dy, some(dense(up[1])),
+                                         ctx->saved_data["init"].toBool());
+        return {out[0], out[1], out[2], Tensor(), out[3], Tensor(), Tensor()};
+    }
+};
+
+py::object linear_attn(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0, const Opt& len) {
+    const kla_desc d = check_lin(q, k, v, g, s0, len);
+    if (g.requires_grad()) value_error("g holds constants: the decays take no gradient");
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = LinearAttn::apply(q, k, v, g, s0, len, d);
+    }
+    return py::make_tuple(out[0], out[1]);
+}
+
+// y; state updated in place
 py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Tensor& state,
                             const Opt& y_in) {
     check_gpu(q, "q");
@@ -318,16 +378,16 @@ py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, c
     check_f32(g, {H}, q, "g");
     check_f32(state, {S, H, dk, dv}, q, "state");
     if (y_in) check_like(*y_in, {S, H, dv}, q, "y");
+    const int32_t s32 = int32_of(S, "S"), h32 = int32_of(H, "H"), dk32 = int32_of(dk, "dk"), dv32 = int32_of(dv, "dv");
     Tensor y;
-    kla_status st;
     {
         py::gil_scoped_release unlocked;
         const c10::hip::HIPGuard on(q.device().index());
         y = y_in ? *y_in : at::empty({S, H, dv}, q.options());
-        st = kla_linear_attn_step(int32_of(S, "S"), int32_of(H, "H"), int32_of(dk, "dk"), int32_of(dv, "dv"), dt, ptr(q), ptr(k),
-                                  ptr(v), (const float*)ptr(g), (float*)ptr(state), ptr(y), stream_of(q));
+        ok(kla_linear_attn_step(s32, h32, dk32, dv32, dt, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), (float*)ptr(state),
+                                ptr(y), stream_of(q)),
+           "kla_linear_attn_step");
     }
-    if (st != KLA_OK) return py::int_((int)st);
     return py::cast(y);
 }
 
@@ -338,10 +398,10 @@ struct Rows {
     std::vector<int64_t> lead;
 };
 
-Rows check_rows(const Tensor& x, const char* name) {
-    check_gpu(x, name);
+Rows rows_of(const Tensor& x, const char* name) {
+    if (!x.is_cuda()) value_error(std::string(name) + " must live on a GPU; there is no CPU path");
     const int dt = dtype_of(x);
-    if (x.dim() < 1) value_error(std::string(name) + " must have a dimension to normalise over");
+    if (x.dim() < 1) value_error(std::string(name) + " must have a last dimension");
     const int64_t n = x.size(-1);
     std::vector<int64_t> lead(x.sizes().begin(), x.sizes().end() - 1);
     int64_t rows = 1;
@@ -349,27 +409,49 @@ Rows check_rows(const Tensor& x, const char* name) {
     return {rows, int32_of(n, "the row length"), dt, lead};
 }
 
-// (out, mean, rstd) or a status
+Rows check_rows(const Tensor& x, const char* name) {
+    const Rows r = rows_of(x, name);
+    check_gpu(x, name);
+    return r;
+}
+
+Tensors norm_forward(const Rows& r, const Tensor& x, const Tensor& w, const Opt& bias, double eps) {
+    const c10::hip::HIPGuard on(x.device().index());
+    const Tensor out = at::empty_like(x), mean = at::empty(r.lead, x.options().dtype(at::kFloat)), rstd = at::empty_like(mean);
+    ok(kla_layer_norm_forward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), fptr(bias), (float)eps, ptr(out),
+                              (float*)ptr(mean), (float*)ptr(rstd), stream_of(x)),
+       "kla_layer_norm_forward");
+    return {out, mean, rstd};
+}
+
+Tensors norm_backward(const Rows& r, const Tensor& x, const Tensor& w, const Tensor& mean, const Tensor& rstd,
+                      const Tensor& dout, bool want_bias) {
+    const c10::hip::HIPGuard on(x.device().index());
+    const Tensor dx = at::empty_like(x), dw = at::empty_like(w);
+    Opt db;
+    if (want_bias) db = at::empty_like(w);
+    const size_t nw = kla_layer_norm_workspace(r.n);
+    const Tensor ws = bytes(nw, x);
+    ok(kla_layer_norm_backward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), (const float*)ptr(mean),
+                               (const float*)ptr(rstd), ptr(dout), ptr(dx), (float*)ptr(dw), fptr(db), ptr(ws), nw, stream_of(x)),
+       "kla_layer_norm_backward");
+    return {dx, dw, or_undefined(db)};
+}
+
+// (out, mean, rstd)
 py::object layer_norm_forward(const Tensor& x, const Tensor& w, const Opt& bias, double eps) {
     const Rows r = check_rows(x, "x");
     check_f32(w, {r.n}, x, "w");
     check_f32(bias, {r.n}, x, "bias");
-    Tensor out, mean, rstd;
-    kla_status st;
+    Tensors out;
     {
         py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(x.device().index());
-        out = at::empty_like(x);
-        mean = at::empty(r.lead, x.options().dtype(at::kFloat));
-        rstd = at::empty_like(mean);
-        st = kla_layer_norm_forward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), fptr(bias), (float)eps, ptr(out),
-                                    (float*)ptr(mean), (float*)ptr(rstd), stream_of(x));
+        out = norm_forward(r, x, w, bias, eps);
     }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::make_tuple(out, mean, rstd);
+    return py::make_tuple(out[0], out[1], out[2]);
 }
 
-// (dx, dw, dbias) or a status
+// (dx, dw, dbias)
 py::object layer_norm_backward(const Tensor& x, const Tensor& w, const Tensor& mean, const Tensor& rstd, const Tensor& dout,
                                bool want_bias) {
     const Rows r = check_rows(x, "x");
@@ -377,23 +459,36 @@ py::object layer_norm_backward(const Tensor& x, const Tensor& w, const Tensor& m
     check_f32(mean, r.lead, x, "mean");
     check_f32(rstd, r.lead, x, "rstd");
     check_like(dout, x.sizes(), x, "dout");
-    Tensor dx, dw;
-    Opt db;
-    kla_status st;
+    Tensors out;
     {
         py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(x.device().index());
-        dx = at::empty_like(x);
-        dw = at::empty_like(w);
-        if (want_bias) db = at::empty_like(w);
-        const size_t nw = kla_layer_norm_workspace(r.n);
-        const Tensor ws = bytes(nw, x);
-        st = kla_layer_norm_backward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), (const float*)ptr(mean),
-                                     (const float*)ptr(rstd), ptr(dout), ptr(dx), (float*)ptr(dw), fptr(db), ptr(ws), nw,
-                                     stream_of(x));
+        out = norm_backward(r, x, w, mean, rstd, dout, want_bias);
     }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::make_tuple(dx, dw, obj(db));
+    return py::make_tuple(out[0], out[1], obj(some(out[2])));
+}
+
+struct LayerNorm : torch::autograd::Function<LayerNorm> {
+    static Tensor forward(Ctx* ctx, const Tensor& x_in, const Tensor& w, const Opt& bias, double eps) {
+        const Tensor x = x_in.contiguous();
+        const Tensors out = norm_forward(rows_of(x, "x"), x, w, bias, eps);
+        ctx->save_for_backward({x, w, out[1], out[2]});
+        ctx->saved_data["bias"] = bias && bias->requires_grad();
+        return out[0];
+    }
+    static Tensors backward(Ctx* ctx, Tensors up) {
+        const Tensors s = ctx->get_saved_variables();
+        const Tensors out = norm_backward(rows_of(s[0], "x"), s[0], s[1], s[2], s[3], up[0].contiguous(),
+                                          ctx->saved_data["bias"].toBool());
+        return {out[0], out[1], out[2], Tensor()};
+    }
+};
+
+Tensor layer_norm(const Tensor& x, const Tensor& w, const Opt& bias, double eps) {
+    const Rows r = rows_of(x, "x");
+    check_f32(w, {r.n}, x, "w");
+    check_f32(bias, {r.n}, x, "bias");
+    py::gil_scoped_release unlocked;
+    return LayerNorm::apply(x, w, bias, eps);
 }
 
 struct Logits {
@@ -404,80 +499,128 @@ struct Logits {
 };
 
 // logits [*lead, V], target [*tail] with lead ending in tail: the dimensions before it are draws
-Logits check_logits(const Tensor& x, const Tensor& target) {
-    const Rows r = check_rows(x, "logits");
+Logits logits_of(const Tensor& x, const Tensor& target) {
+    const Rows r = rows_of(x, "logits");
     const at::IntArrayRef lead(r.lead), t = target.sizes();
     if (t.size() > lead.size() || lead.slice(lead.size() - t.size()) != t)
         value_error("target has shape " + shape_str(t) + ", expected the last dimensions of " + shape_str(lead));
-    check_int(target, at::kLong, t, x, "target");
     int64_t S = 1;
     for (size_t i = 0; i < lead.size() - t.size(); ++i) S *= lead[i];
     return {int32_of(S, "the number of draws"), r.n, target.numel(), r.dtype, r.lead};
 }
 
-// (logp, entropy, stat, top_logp, top_index) or a status
-py::object token_logp_forward(const Tensor& x, const Tensor& target, bool want_entropy, int64_t top, bool want_stat) {
-    const Logits l = check_logits(x, target);
-    if (top < 0 || top > INT32_MAX) value_error("top must not be negative");
-    Tensor logp;
-    Opt entropy, stat, top_logp, top_index;
-    kla_status st;
-    {
-        py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(x.device().index());
-        const auto f32 = x.options().dtype(at::kFloat);
-        logp = at::empty(l.lead, f32);
-        auto with = [&](int64_t n) {
-            std::vector<int64_t> s = l.lead;
-            s.push_back(n);
-            return s;
-        };
-        if (want_entropy) entropy = at::empty(l.lead, f32);
-        if (want_stat) stat = at::empty(with(2), f32);
-        if (top > 0) {
-            top_logp = at::empty(with(top), f32);
-            top_index = at::empty(with(top), x.options().dtype(at::kLong));
-        }
-        const size_t nw = kla_token_logp_workspace(l.S, l.n, l.V, (int32_t)top);
-        Opt ws;
-        if (nw) ws = bytes(nw, x);
-        st = logp.numel() == 0 ? KLA_OK   // nothing to do, and no draws at all are allowed here
-                               : kla_token_logp_forward(l.S, l.n, l.V, (int32_t)top, l.dtype, ptr(x), (const int64_t*)ptr(target),
-                                                        (float*)ptr(logp), fptr(entropy), fptr(stat), fptr(top_logp),
-                                                        (int64_t*)ptr(top_index), ptr(ws), nw, stream_of(x));
-    }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::make_tuple(logp, obj(entropy), obj(stat), obj(top_logp), obj(top_index));
+Logits check_logits(const Tensor& x, const Tensor& target) {
+    const Logits l = logits_of(x, target);
+    check_gpu(x, "logits");
+    check_int(target, at::kLong, target.sizes(), x, "target");
+    return l;
 }
 
-// dlogits or a status
-py::object token_logp_backward(const Tensor& x, const Tensor& target, const Tensor& stat, const Opt& entropy,
-                               const Opt& dlogp, const Opt& dentropy) {
+std::vector<int64_t> with(std::vector<int64_t> lead, int64_t n) {
+    lead.push_back(n);
+    return lead;
+}
+
+// logp, entropy, stat, top_logp, top_index.  No rows, or no draws of them: nothing to do.
+Tensors logp_forward(const Logits& l, const Tensor& x, const Tensor& target, bool want_entropy, int32_t top, bool want_stat) {
+    const c10::hip::HIPGuard on(x.device().index());
+    const auto f32 = x.options().dtype(at::kFloat);
+    const Tensor logp = at::empty(l.lead, f32);
+    Opt entropy, stat, top_logp, top_index, ws;
+    if (want_entropy) entropy = at::empty(l.lead, f32);
+    if (want_stat) stat = at::empty(with(l.lead, 2), f32);
+    if (top > 0) {
+        top_logp = at::empty(with(l.lead, top), f32);
+        top_index = at::empty(with(l.lead, top), x.options().dtype(at::kLong));
+    }
+    const size_t nw = kla_token_logp_workspace(l.S, l.n, l.V, top);
+    if (nw) ws = bytes(nw, x);
+    if (logp.numel() > 0)
+        ok(kla_token_logp_forward(l.S, l.n, l.V, top, l.dtype, ptr(x), (const int64_t*)ptr(target), (float*)ptr(logp),
+                                  fptr(entropy), fptr(stat), fptr(top_logp), (int64_t*)ptr(top_index), ptr(ws), nw, stream_of(x)),
+           "kla_token_logp_forward");
+    return {logp, or_undefined(entropy), or_undefined(stat), or_undefined(top_logp), or_undefined(top_index)};
+}
+
+Tensor logp_backward(const Logits& l, const Tensor& x, const Tensor& target, const Tensor& stat, const Opt& entropy,
+                     const Opt& dlogp, const Opt& dentropy) {
+    const c10::hip::HIPGuard on(x.device().index());
+    const Tensor dx = at::empty_like(x);
+    if (x.numel() > 0)
+        ok(kla_token_logp_backward(l.S, l.n, l.V, l.dtype, ptr(x), (const int64_t*)ptr(target), (const float*)ptr(stat),
+                                   fptr(entropy), fptr(dlogp), fptr(dentropy), ptr(dx), stream_of(x)),
+           "kla_token_logp_backward");
+    return dx;
+}
+
+// (logp, entropy, stat, top_logp, top_index)
+py::object token_logp_forward(const Tensor& x, const Tensor& target, bool want_entropy, int64_t top, bool want_stat) {
     const Logits l = check_logits(x, target);
-    std::vector<int64_t> two = l.lead;
-    two.push_back(2);
-    check_f32(stat, two, x, "stat");
+    if (top < 0) value_error("top must not be negative");
+    const int32_t top32 = int32_of(top, "top");
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = logp_forward(l, x, target, want_entropy, top32, want_stat);
+    }
+    return py::make_tuple(out[0], obj(some(out[1])), obj(some(out[2])), obj(some(out[3])), obj(some(out[4])));
+}
+
+// dlogits
+Tensor token_logp_backward(const Tensor& x, const Tensor& target, const Tensor& stat, const Opt& entropy,
+                           const Opt& dlogp, const Opt& dentropy) {
+    const Logits l = check_logits(x, target);
+    check_f32(stat, with(l.lead, 2), x, "stat");
     check_f32(entropy, l.lead, x, "entropy");
     check_f32(dlogp, l.lead, x, "dlogp");
     check_f32(dentropy, l.lead, x, "dentropy");
-    Tensor dx;
-    kla_status st;
+    py::gil_scoped_release unlocked;
+    return logp_backward(l, x, target, stat, entropy, dlogp, dentropy);
+}
+
+struct TokenLogp : torch::autograd::Function<TokenLogp> {
+    static Tensors forward(Ctx* ctx, const Tensor& x_in, const Tensor& target_in, bool want_entropy) {
+        const Tensor x = x_in.contiguous(), target = target_in.contiguous();
+        const Tensors out = logp_forward(logits_of(x, target), x, target, want_entropy, 0, true);
+        ctx->save_for_backward({x, target, out[2], out[1]});
+        ctx->set_materialize_grads(false);
+        return want_entropy ? Tensors{out[0], out[1]} : Tensors{out[0]};
+    }
+    static Tensors backward(Ctx* ctx, Tensors up) {
+        const Tensors s = ctx->get_saved_variables();
+        const Tensor dentropy = up.size() > 1 ? dense(up[1]) : Tensor();
+        return {logp_backward(logits_of(s[0], s[1]), s[0], s[1], s[2], some(s[3]), some(dense(up[0])), some(dentropy)), Tensor(),
+                Tensor()};
+    }
+};
+
+py::object token_logp(const Tensor& x, const Tensor& target, bool want_entropy) {
+    logits_of(x, target);
+    if (target.scalar_type() != at::kLong || target.device() != x.device())
+        value_error("target must be an int64 tensor on " + x.device().str());
+    Tensors out;
     {
         py::gil_scoped_release unlocked;
-        const c10::hip::HIPGuard on(x.device().index());
-        dx = at::empty_like(x);
-        st = x.numel() == 0 ? KLA_OK
-                            : kla_token_logp_backward(l.S, l.n, l.V, l.dtype, ptr(x), (const int64_t*)ptr(target),
-                                                      (const float*)ptr(stat), fptr(entropy), fptr(dlogp), fptr(dentropy),
-                                                      ptr(dx), stream_of(x));
+        out = TokenLogp::apply(x, target, want_entropy);
     }
-    if (st != KLA_OK) return py::int_((int)st);
-    return py::cast(dx);
+    if (!want_entropy) return py::cast(out[0]);
+    return py::make_tuple(out[0], out[1]);
 }
 
 }  // namespace
 
 PYBIND11_MODULE(_kla_torch, m) {
+    py::register_exception_translator([](std::exception_ptr p) {
+        try {
+            if (p) std::rethrow_exception(p);
+        } catch (const Refused& e) {
+            const py::object type = py::module_::import("paper_2602_10743_amd").attr("KLAError");
+            PyErr_SetObject(type.ptr(), type((int)e.status, e.where).ptr());
+        }
+    });
+    m.def("linear_attn", &linear_attn);
+    m.def("layer_norm", &layer_norm);
+    m.def("token_logp", &token_logp);
     m.def("linear_attn_forward", &linear_attn_forward);
     m.def("linear_attn_backward", &linear_attn_backward);
     m.def("linear_attn_step", &linear_attn_step);

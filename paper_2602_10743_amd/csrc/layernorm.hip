@@ -67,6 +67,29 @@ __device__ __forceinline__ void store_vec(E* p, const float* f) {
     }
 }
 
+// VEC fp32 values of a weight, zero where there is none (none are read past a row's end: VEC divides n).
+template <int VEC>
+__device__ __forceinline__ void load_w(const float* w, int c, int n, float* f) {
+    if (w && c < n) {
+        if constexpr (VEC % 4 == 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(w + c + e);
+                f[e] = v.x;
+                f[e + 1] = v.y;
+                f[e + 2] = v.z;
+                f[e + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = w[c + e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = 0.f;
+    }
+}
+
 // Two sums over the TPR lanes of a row, in every lane.  buf: LDS for groups of several waves, two
 // slots of 2 x TPR / 64 floats taken in turn, so that one barrier per call is enough.
 template <int TPR>
@@ -119,13 +142,10 @@ __global__ __launch_bounds__(kFwdThreads<TPR>) void layernorm_fwd_kernel(size_t 
     const float inv = 1.f / (float)n;
     float wr[EPT], br[EPT];
 #pragma unroll
-    for (int i = 0; i < HB; ++i)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const int c = (i * TPR + tl) * VEC + e;
-            wr[i * VEC + e] = c < n ? w[c] : 0.f;
-            br[i * VEC + e] = bias && c < n ? bias[c] : 0.f;
-        }
+    for (int i = 0; i < HB; ++i) {
+        load_w<VEC>(w, (i * TPR + tl) * VEC, n, wr + i * VEC);
+        load_w<VEC>(bias, (i * TPR + tl) * VEC, n, br + i * VEC);
+    }
     int turn = 0;
     // every group of the workgroup takes part in each round: the sums hold barriers
     for (size_t r0 = (size_t)blockIdx.x * RPB; r0 < rows; r0 += (size_t)gridDim.x * RPB) {
@@ -190,13 +210,11 @@ __global__ __launch_bounds__(kBwdThreads<TPR>) void layernorm_bwd_kernel(size_t 
     const float inv = 1.f / (float)n;
     float wr[EPT], sw[EPT], sb[EPT];
 #pragma unroll
-    for (int i = 0; i < HB; ++i)
+    for (int i = 0; i < HB; ++i) {
+        load_w<VEC>(w, (i * TPR + tl) * VEC, n, wr + i * VEC);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const int c = (i * TPR + tl) * VEC + e;
-            wr[i * VEC + e] = c < n ? w[c] : 0.f;
-            sw[i * VEC + e] = sb[i * VEC + e] = 0.f;
-        }
+        for (int e = 0; e < VEC; ++e) sw[i * VEC + e] = sb[i * VEC + e] = 0.f;
+    }
     int turn = 0;
     for (size_t r0 = (size_t)blockIdx.x * RPB; r0 < rows; r0 += (size_t)gridDim.x * RPB) {
         const size_t r = r0 + group;
@@ -298,14 +316,15 @@ __global__ __launch_bounds__(512) void layernorm_parts_kernel(int nparts, int n,
 constexpr unsigned kParts = 256;   // workgroups of the backward, one per CU
 
 // Calls f<VEC, EPT, TPR> for a row of n elements: the widest vectors that rows of n keep aligned, and the
-// fewest lanes that hold a row in 32 registers each.
+// fewest lanes that hold a row in 16 registers each (16384 x 2048 bf16, forward: 24 us with 16 elements on
+// 128 lanes, 24 with 8 on 256, 27 with 32 on 64; backward, whose lanes hold five such rows: 52, 56, 52).
 template <typename E, typename F>
 hipError_t by_shape(int n, F&& f) {
 #define KLA_LN_SHAPES(V_)                                                               \
     if (n <= 128) return f.template run<E, V_, 8, 16>();                       \
     if (n <= 512) return f.template run<E, V_, 8, 64>();                                  \
     if (n <= 1024) return f.template run<E, V_, 16, 64>();                                \
-    if (n <= 2048) return f.template run<E, V_, 32, 64>();                                \
+    if (n <= 2048) return f.template run<E, V_, 16, 128>();                                \
     if (n <= 4096) return f.template run<E, V_, 16, 256>();                               \
     if (n <= 8192) return f.template run<E, V_, 16, 512>();                               \
     return f.template run<E, V_, 16, 1024>();
@@ -336,7 +355,7 @@ struct Fwd {
     hipError_t run() {
         constexpr int RPB = kFwdThreads<TPR> / TPR;
         const size_t blocks = (rows + RPB - 1) / RPB;
-        const unsigned grid = (unsigned)(blocks < 2048 ? blocks : 2048);
+        const unsigned grid = (unsigned)(blocks < 4096 ? blocks : 4096);
         layernorm_fwd_kernel<E, VEC, EPT, TPR><<<dim3(grid), dim3(kFwdThreads<TPR>), 0, st>>>(
             rows, n, static_cast<const E*>(x), w, bias, eps, static_cast<E*>(out), mean, rstd);
         return hipGetLastError();

@@ -29,6 +29,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTop = 32;
 constexpr int kRoom = 1024;     // collected elements
+constexpr int kMaxParts = 64;   // of a row
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -306,23 +307,42 @@ __global__ __launch_bounds__(kThreads) void logp_fwd_kernel(LogpArgs a) {
     }
 }
 
-// The parts of one row.
+// The parts of one row: at most 64, whose lists are in order.  The top-th largest of the parts' first keys is
+// at most the top-th largest of all, so only the keys from it on are ranked.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void logp_join_kernel(LogpArgs a) {
-    __shared__ uint64_t best[kMaxTop];
+    __shared__ uint64_t best[kMaxTop], keys[kMaxParts * kMaxTop];
+    __shared__ uint64_t least;
+    __shared__ uint32_t count;
     const size_t r = blockIdx.x;
     Sums t = a.sums[r * a.parts];
     for (int p = 1; p < a.parts; ++p) t = joined(t, a.sums[r * a.parts + p]);
     if (a.top > 0) {
         const int n = a.parts * a.top;
-        const uint64_t* keys = a.keys + r * n;
+        const uint64_t* in = a.keys + r * n;
         if ((int)threadIdx.x < a.top) best[threadIdx.x] = 0;
+        if (threadIdx.x == 0) {
+            least = 1;   // 0 is no key
+            count = 0;
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const uint64_t mine = keys[i];
-            if (mine == 0) continue;
+        if (threadIdx.x < 64 && a.parts >= a.top) {
+            const uint64_t first = (int)threadIdx.x < a.parts ? in[threadIdx.x * a.top] : 0;
             int rank = 0;
-            for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+            for (int p = 0; p < a.parts; ++p)
+                rank += ((uint64_t)__builtin_amdgcn_readlane((int)(first >> 32), p) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)first, p)) > first;
+            if (rank == a.top - 1 && first) least = first;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += kThreads)
+            if (in[i] >= least) keys[atomicAdd(&count, 1u)] = in[i];
+        __syncthreads();
+        const int m = (int)count;
+        for (int i = threadIdx.x; i < m; i += kThreads) {
+            const uint64_t mine = keys[i];
+            int rank = 0;
+            for (int j = 0; j < m; ++j) rank += keys[j] > mine;
             if (rank < a.top) best[rank] = mine;
         }
         __syncthreads();
@@ -369,10 +389,10 @@ __global__ __launch_bounds__(kThreads) void logp_bwd_kernel(LogpArgs a, const fl
     }
 }
 
-// Parts a row is cut into: enough workgroups to fill the chip, none with less than 2048 elements.
+// Parts a row is cut into: three workgroups a CU, none with less than 2048 elements.
 int parts_of(size_t rows, int V) {
     int p = 1;
-    while (rows * p < 1024 && V / (2 * p) >= 2048) p *= 2;
+    while (rows * p < 768 && p < kMaxParts && V / (2 * p) >= 2048) p *= 2;
     return p;
 }
 
