@@ -13,7 +13,7 @@
 // start state.  All exponents are at least 0, so no factor exceeds 1 for g <= 0; e^{-inf * 0} is 1.
 //
 // A wave owns CW value columns of one sequence (or segment of one) and their state, in registers;
-// the waves of a workgroup share the chunk's Q, K and V in LDS, loaded two chunks ahead.  Accumulators are
+// the waves of a workgroup share the chunk's Q, K and V in LDS, loaded a chunk ahead.  Accumulators are
 // operands as they stand: over tokens, lane group g holds {4g .. 4g+3} u {16+4g .. 16+4g+3} of a 32-deep
 // product, and the 32 rows of two tiles of the state are dealt so that g holds 8g .. 8g+7 (slot_of),
 // which a lane reads of a row of Q or K with one access.  Q's fragments serve Q K^T and Q R, V's
@@ -304,7 +304,7 @@ __device__ __forceinline__ float lds_val(float, const unsigned char* p) { return
 
 // (Q K^T o D) V of a chunk again, where it was not finite: the mask and the matrix instruction multiply
 // later tokens' scores and values by zero, and what is not finite must not reach the tokens before it.
-template <typename E, int N, int D>
+template <typename E, int N, int DT>
 __device__ __forceinline__ f32x4 masked_sums(const unsigned char* sQ, const unsigned char* sK, const unsigned char* sV,
                                              const float* pw, int col0, int i, int g4) {
     f32x4 y = zero4();
@@ -316,7 +316,7 @@ __device__ __forceinline__ f32x4 masked_sums(const unsigned char* sQ, const unsi
             s += lds_val(E(), sQ + Tile<E, N>::at(i, n)) * lds_val(E(), sK + Tile<E, N>::at(j, n));
         s *= pw[i - j];
 #pragma unroll
-        for (int rr = 0; rr < 4; ++rr) y[rr] += s * lds_val(E(), sV + Tile<E, D>::at(j, col0 + 4 * g4 + rr));
+        for (int rr = 0; rr < 4; ++rr) y[rr] += s * lds_val(E(), sV + Tile<E, DT>::at(j, col0 + 4 * g4 + rr));
     }
     return y;
 }
@@ -358,42 +358,42 @@ __device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_
                  : "memory");
 }
 
-// Waves of a workgroup, which takes all D columns: D / CW compute; where the rows of Q and K are long and
-// those waves few, others help with the loads.
-template <typename E, int N, int D>
+// A workgroup takes DT of the D columns, a wave CW of them.  Where the rows of Q and K are long and the waves
+// that compute (NCW) few, others help with the loads.  64 columns in waves of 16 leave 168 registers and 53 KiB of
+// LDS, so three workgroups of 128-wide bf16 passes share a CU (B = 8, T = 2048, H = 16: forward 108 us and
+// backward 215, against 138 and 227 with 128 columns in waves of 32, whose scores are formed half as
+// often but which one or two waves a SIMD have to hide).  The states' pass forms no scores: all columns.
+template <typename E, int N, int D, bool NOY>
 struct LinCfg {
-    static constexpr int CW = D >= 128 ? 32 : 16, NCW = D / CW, ROW = N * (int)sizeof(E);
-    static constexpr int LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1, NW = NCW > LW ? NCW : LW;
-    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, D>::BYTES, LDS = 3 * BUF + 2 * kLC * (int)sizeof(float);
-    // fp32 states and operands of 128 slots need more than the 256 registers of two waves per SIMD
-    static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 1 : 2;
+    static constexpr int CW = NOY && D == 128 ? 32 : 16, DT = NOY || D <= 64 ? D : 64, NTILE = D / DT, NCW = DT / CW;
+    static constexpr int ROW = N * (int)sizeof(E), LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1, NW = NCW > LW ? NCW : LW;
+    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES, LDS = 2 * BUF + 2 * kLC * (int)sizeof(float);
+    // waves per SIMD: fp32 states and operands of 128 slots need more than the registers of three
+    static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : 3;
 };
 
 template <typename E, int N, int D, bool NOY>
-__global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC)) void linattn_kernel(LinArgs a) {
-    using Cfg = LinCfg<E, N, D>;
+__global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, NOY>::OCC)) void linattn_kernel(LinArgs a) {
+    using Cfg = LinCfg<E, N, D, NOY>;
     constexpr int CW = Cfg::CW, NW = Cfg::NW, NDT = CW / 16, NRT = N / 16, KS = (N + 31) / 32;
     constexpr int ES = (int)sizeof(E);
     using TQ = Tile<E, N>;
-    using TV = Tile<E, D>;
+    constexpr int DT = Cfg::DT, NTILE = Cfg::NTILE;
+    using TV = Tile<E, DT>;
     constexpr int UQ = NOY ? 0 : TQ::UNITS, UK = TQ::UNITS, UNITS = UQ + UK + TV::UNITS;
-    constexpr int NL = (UNITS + NW - 1) / NW, NLMIN = UNITS / NW;   // a wave's loads per chunk
+    constexpr int NL = (UNITS + NW - 1) / NW;   // a wave's loads per chunk
     constexpr int NST = NOY ? 0 : 2 * NDT;                          // and stores, of one that computes
     constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* pw = reinterpret_cast<float*>(smem + 3 * BUF);   // e^{g n}
+    float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
 
-    int vi, ji;   // the passes over one sequence on one XCD: they read the same rows
+    int vi, ji, tile;   // the passes and tiles of one sequence on one XCD: they read the same rows
     {
-        const int i = blockIdx.x, nv = a.B * a.H * a.run;
-        if (nv % 8 == 0) {
-            const int slot = i / 8;
-            ji = slot % a.jobs;
-            vi = (slot / a.jobs) * 8 + i % 8;
-        } else {
-            ji = i % a.jobs;
-            vi = i / a.jobs;
-        }
+        const int i = blockIdx.x, nv = a.B * a.H * a.run, each = a.jobs * NTILE;
+        const int slot = nv % 8 == 0 ? i / 8 : i;
+        vi = nv % 8 == 0 ? slot / each * 8 + i % 8 : slot / each;
+        ji = slot % each / NTILE;
+        tile = slot % NTILE;
     }
     const LinJob job = a.job[ji];
     const bool rev = job.rev;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
     const int Tb = __builtin_amdgcn_readfirstlane(seq_len(a, b));
     const int u0 = seg * a.lc * kLC, nu = min(max(Tb - u0, 0), a.lc * kLC);   // this segment's tokens, in walk order
     const int nchunk = (nu + kLC - 1) / kLC;
-    const int dm0 = wave * CW;
+    const int dl0 = wave * CW, dm0 = tile * DT + dl0;   // the wave's first column, in the tile and of all
     const bool works = NW == Cfg::NCW || wave < Cfg::NCW;
 
     if (threadIdx.x < 2 * kLC) pw[threadIdx.x] = decay_pow(g, threadIdx.x);
@@ -432,7 +432,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
         return words_t{(uint32_t)q, (uint32_t)(q >> 32) & 0xffffu, (kLC - 1) * stride + cols - miss, 0x00020000u};
     };
     auto shift_of = [&](uint32_t stride, int n) { return rev ? (uint32_t)(kLC - n) * stride : 0u; };
-    uintptr_t pq = at(job.q, sn, N), pk = at(job.k, sn, N), pv = at(job.v, sd, D), py = at(job.y, sd, D) + dm0 * ES;
+    uintptr_t pq = at(job.q, sn, N), pk = at(job.k, sn, N), pv = at(job.v, sd, D) + tile * DT * ES, py = at(job.y, sd, D) + dm0 * ES;
     const intptr_t step_n = rev ? -(intptr_t)(kLC * (size_t)sn) : (intptr_t)(kLC * (size_t)sn);
     const intptr_t step_d = rev ? -(intptr_t)(kLC * (size_t)sd) : (intptr_t)(kLC * (size_t)sd);
 
@@ -457,13 +457,13 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
     auto load = [&](int c) {     // chunks in order, each once
         const int n = tokens(c);
         const words_t rk = words_of(pk, sn, n, N * ES), rq = NOY ? rk : words_of(pq, sn, n, N * ES);
-        const words_t rv = words_of(pv, sd, n, D * ES);
+        const words_t rv = words_of(pv, sd, n, DT * ES);
         const uint32_t hn = shift_of(sn, n), hd = shift_of(sd, n);
         pq += step_n;
         pk += step_n;
         pv += step_d;
         const uint32_t dst = lds0 + (NOY ? TQ::BYTES : 0) + into * BUF + wave * 1024;   // tiles follow each other
-        into = into == 2 ? 0 : into + 1;
+        into ^= 1;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             if (part_of(i) < UQ)
@@ -483,7 +483,6 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
         return flip ? d * N + n : n * D + d;
     };
     if (nchunk > 0) load(0);
-    if (nchunk > 1) load(1);
     {
         const float* s0 = NOY || !job.start || !works ? nullptr : job.start + srow * (size_t)(N * D);
 #pragma unroll
@@ -529,17 +528,14 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
     int from = 0;   // this chunk's buffer
     for (int c = 0; c < nchunk; ++c) {
         const int n = tokens(c);
-        // this chunk's loads have ended, of this wave and behind the barrier of all: younger are the stores
-        // of two chunks and the loads of one
-        if (c + 1 == nchunk) wait_vm_le<0>();
-        else if (c == 0) wait_vm_le<NLMIN>();
-        else if (!works) wait_vm_le<NLMIN>();
-        else if (c == 1) wait_vm_le<NLMIN + NST>();
-        else wait_vm_le<NLMIN + 2 * NST>();
+        // this chunk's loads have ended, of this wave and behind the barrier of all: younger are the last
+        // chunk's stores
+        if (works) wait_vm_le<NST>();
+        else wait_vm_le<0>();
         __syncthreads();
-        if (c + 2 < nchunk) load(c + 2);   // into the buffer of the chunk before this one
+        if (c + 1 < nchunk) load(c + 1);   // into the last chunk's buffer
         const unsigned char* buf = smem + from * BUF;
-        from = from == 2 ? 0 : from + 1;
+        from ^= 1;
         const unsigned char *sQ = buf, *sK = buf + TQ::BYTES, *sV = buf + 2 * TQ::BYTES;
         if (n < kLC) {
             weights(n);
@@ -550,7 +546,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
         if (works) {
             Op<E> vf[NDT];
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) vf[dt] = Op<E>::template col<D>(sV, dm0 + 16 * dt, g4, l16);
+            for (int dt = 0; dt < NDT; ++dt) vf[dt] = Op<E>::template col<DT>(sV, dl0 + 16 * dt, g4, l16);
             f32x4 s00 = zero4(), s01 = zero4(), s11 = zero4();
             if constexpr (!NOY) {
                 // S^T[j, i] = K_j . Q_i, tiles (jt, it) = (0,0), (0,1), (1,1); Y^T[d, i] from the state
@@ -620,7 +616,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
                     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
                         for (int it = 0; it < 2; ++it)
-                            in[dt][it] = masked_sums<E, N, D>(sQ, sK, sV, pw, dm0 + 16 * dt, 16 * it + l16, g4);
+                            in[dt][it] = masked_sums<E, N, DT>(sQ, sK, sV, pw, dl0 + 16 * dt, 16 * it + l16, g4);
             }
         }
         if constexpr (!NOY) {
@@ -654,10 +650,10 @@ __global__ __launch_bounds__((LinCfg<E, N, D>::NW * 64), (LinCfg<E, N, D>::OCC))
     }
     if constexpr (!NOY) {   // rows past the sequence's length are zero
         const int z1 = min(a.T, u0 + a.lc * kLC);
-        constexpr int PV = D * ES / 16;
+        constexpr int PV = DT * ES / 16;
         char* y0 = static_cast<char*>(job.y);
         for (size_t x = (size_t)max(Tb, u0) * PV + threadIdx.x; x < (size_t)z1 * PV; x += NW * 64)
-            *reinterpret_cast<uint4*>(y0 + ((((size_t)b * a.T + x / PV) * H + h) * D) * ES + (x % PV) * 16) =
+            *reinterpret_cast<uint4*>(y0 + ((((size_t)b * a.T + x / PV) * H + h) * D + tile * DT) * ES + (x % PV) * 16) =
                 uint4{0u, 0u, 0u, 0u};
     }
 }
@@ -674,23 +670,30 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int
     float* e = job.end + (size_t)bh * a.ns * N * D + x;
     float R = s0 ? s0[(size_t)bh * N * D + x] : 0.f;
     const float whole = decay_pow(g, L);
-    for (int s = 0; s < a.ns; ++s) {
-        const float own = s < a.ns - 1 ? e[(size_t)s * N * D] : 0.f;
-        e[(size_t)s * N * D] = R;
-        const int n = min(max(Tb - s * L, 0), L);
-        R = (n == L ? whole : decay_pow(g, n)) * R + own;
+    constexpr int U = 8;   // segments in flight: the states are read and written in place
+    for (int s1 = 0; s1 < a.ns; s1 += U) {
+        float own[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) own[i] = s1 + i < a.ns - 1 ? e[(size_t)(s1 + i) * N * D] : 0.f;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (s1 + i < a.ns) {
+                e[(size_t)(s1 + i) * N * D] = R;
+                const int n = min(max(Tb - (s1 + i) * L, 0), L);
+                R = (n == L ? whole : decay_pow(g, n)) * R + own[i];
+            }
     }
 }
 
 template <typename E, int N, int D, bool NOY>
 hipError_t launch(const LinArgs& a, hipStream_t st) {
-    using Cfg = LinCfg<E, N, D>;
+    using Cfg = LinCfg<E, N, D, NOY>;
     auto kern = linattn_kernel<E, N, D, NOY>;
     // more than 64 KiB of LDS must be opted into once per kernel (thread-safe static init)
     static const hipError_t attr =
         hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS);
     if (attr != hipSuccess) return attr;
-    const size_t grid = (size_t)a.B * a.H * a.run * a.jobs;
+    const size_t grid = (size_t)a.B * a.H * a.run * a.jobs * Cfg::NTILE;
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::NW * 64), Cfg::LDS, st, a);
     return hipGetLastError();
 }
@@ -788,22 +791,26 @@ hipError_t step(const Shape& s, const void* q, const void* k, const void* v, con
     }
 }
 
-// Segments per sequence and chunks in one, for passes whose workgroups number `groups` without.  Segments
-// cost a pass over K and V for their states and two launches more, so a sequence of fewer than 16 chunks
-// is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, us: the backward of B = 8,
-// T = 2048, H = 16, 384 workgroups, 228 whole and 252 in two; the forward, 128 workgroups, 142 whole, 124
-// in two, 109 in four).  Otherwise two workgroups a CU, of two chunks at least (B = 3, T = 777, H = 5, 64
-// and 128 wide, forward: 32 whole, 21 in twelve, 29 in 25 segments).
+// Segments per sequence and chunks in one, for passes of `groups` workgroups where no sequence is cut.
+// Segments cost a pass over K and V for their states and two launches more, so a sequence of fewer than 16
+// chunks is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, B = 8, T = 2048,
+// H = 16, us whole, in two, in three: forward, 256 workgroups, 108, 131, 118; backward, 768, 215, 274, 282).
+// Otherwise three workgroups a CU, of two chunks at least (B = 1, T = 65536, forward: 471 in 16 segments, 442
+// in 24, 460 in 32; B = 3, T = 777, H = 5, 64 and 128 wide: 30 in two, 19 in twelve, 22 in 25).
 void segments(const Shape& s, long groups, int& ns, int& lc) {
     const int nc = (s.T + kLC - 1) / kLC;
     ns = 1;
     lc = nc;
     if (nc < 16 || groups >= 256) return;
-    const long want = (512 + groups - 1) / groups;
+    const long want = (768 + groups - 1) / groups;
     ns = (int)(want < nc / 2 ? want : nc / 2);
     lc = (nc + ns - 1) / ns;
     ns = (nc + lc - 1) / lc;
 }
+
+long tiles(int D) { return D > 64 ? 2 : 1; }   // workgroups of a pass over one sequence
+long fwd_groups(const Shape& s) { return (long)s.B * s.H * tiles(s.dv); }
+long bwd_groups(const Shape& s) { return (long)s.B * s.H * (2 * tiles(s.dk) + tiles(s.dv)); }
 
 LinArgs args_of(const Shape& s, const float* g, const int* len, long groups) {
     LinArgs a{};
@@ -841,13 +848,13 @@ size_t states_bytes(const Shape& s, int ns) {
 }  // namespace
 
 size_t linattn_workspace(const Shape& s, bool backward) {
-    const LinArgs a = args_of(s, nullptr, nullptr, (backward ? 3L : 1L) * s.B * s.H);
+    const LinArgs a = args_of(s, nullptr, nullptr, backward ? bwd_groups(s) : fwd_groups(s));
     return (backward ? 2 : 1) * states_bytes(s, a.ns);
 }
 
 hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
                               const int* len, void* y, float* sT, void* ws, hipStream_t st) {
-    LinArgs a = args_of(s, g, len, (long)s.B * s.H);
+    LinArgs a = args_of(s, g, len, fwd_groups(s));
     a.jobs = 1;
     a.run = a.ns;
     a.job[0] = LinJob{q, k, v, s0, y, sT, 0, 0};
@@ -863,7 +870,7 @@ hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, cons
 hipError_t launch_linattn_bwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
                               const int* len, const void* dy, const float* dsT, void* dq, void* dk, void* dv, float* ds0,
                               void* ws, hipStream_t st) {
-    LinArgs a = args_of(s, g, len, 3L * s.B * s.H);
+    LinArgs a = args_of(s, g, len, bwd_groups(s));
     a.run = a.ns;
     const float *first = s0, *last = dsT;
     if (a.ns > 1) {   // the states before the segments, and their adjoints behind them
