@@ -275,8 +275,16 @@ using Tensors = torch::autograd::variable_list;
 using Ctx = torch::autograd::AutogradContext;
 Opt some(const Tensor& t) { return t.defined() ? Opt(t) : Opt(); }
 Tensor or_undefined(const Opt& t) { return t ? *t : Tensor(); }
-// An upstream gradient as the library takes it.
-Tensor dense(const Tensor& t) { return t.defined() ? t.contiguous() : t; }
+// A tensor as the library takes it: dense, and on 16 bytes, which a slice of a larger one need not be.
+Tensor dense(const Tensor& t) {
+    if (!t.defined()) return t;
+    const Tensor c = t.contiguous();
+    return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 ? c.clone() : c;
+}
+// The nodes' backward passes are not differentiable themselves.
+void once() {
+    TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), "second derivatives (create_graph=True) are not available");
+}
 
 // The raw calls take checked tensors and need no interpreter lock.
 Tensors lin_forward(const kla_desc& d, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
@@ -344,11 +352,12 @@ struct LinearAttn : torch::autograd::Function<LinearAttn> {
         return lin_forward(d, q, k, v, g, s0, len, c10::nullopt, true);
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors x = ctx->get_saved_variables();
         const Tensor &q = x[0], &v = x[2];
         const kla_desc d{(int32_t)q.size(0), (int32_t)q.size(1), (int32_t)q.size(2), (int32_t)q.size(3), (int32_t)v.size(3),
                          q.scalar_type() == at::kFloat ? KLA_F32 : KLA_BF16};
-        const Tensor dy = up[0].defined() ? up[0].contiguous() : at::zeros_like(v);
+        const Tensor dy = up[0].defined() ? dense(up[0]) : at::zeros_like(v);
         const Tensors out = lin_backward(d, q, x[1], v, x[3], some(x[4]), some(x[5]), dy, some(dense(up[1])),
                                          ctx->saved_data["init"].toBool());
         return {out[0], out[1], out[2], Tensor(), out[3], Tensor(), Tensor()};
@@ -469,15 +478,16 @@ py::object layer_norm_backward(const Tensor& x, const Tensor& w, const Tensor& m
 
 struct LayerNorm : torch::autograd::Function<LayerNorm> {
     static Tensor forward(Ctx* ctx, const Tensor& x_in, const Tensor& w, const Opt& bias, double eps) {
-        const Tensor x = x_in.contiguous();
+        const Tensor x = dense(x_in);
         const Tensors out = norm_forward(rows_of(x, "x"), x, w, bias, eps);
         ctx->save_for_backward({x, w, out[1], out[2]});
         ctx->saved_data["bias"] = bias && bias->requires_grad();
         return out[0];
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors s = ctx->get_saved_variables();
-        const Tensors out = norm_backward(rows_of(s[0], "x"), s[0], s[1], s[2], s[3], up[0].contiguous(),
+        const Tensors out = norm_backward(rows_of(s[0], "x"), s[0], s[1], s[2], s[3], dense(up[0]),
                                           ctx->saved_data["bias"].toBool());
         return {out[0], out[1], out[2], Tensor()};
     }
@@ -580,13 +590,14 @@ Tensor token_logp_backward(const Tensor& x, const Tensor& target, const Tensor& 
 
 struct TokenLogp : torch::autograd::Function<TokenLogp> {
     static Tensors forward(Ctx* ctx, const Tensor& x_in, const Tensor& target_in, bool want_entropy) {
-        const Tensor x = x_in.contiguous(), target = target_in.contiguous();
+        const Tensor x = dense(x_in), target = dense(target_in);
         const Tensors out = logp_forward(logits_of(x, target), x, target, want_entropy, 0, true);
         ctx->save_for_backward({x, target, out[2], out[1]});
         ctx->set_materialize_grads(false);
         return want_entropy ? Tensors{out[0], out[1]} : Tensors{out[0]};
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors s = ctx->get_saved_variables();
         const Tensor dentropy = up.size() > 1 ? dense(up[1]) : Tensor();
         return {logp_backward(logits_of(s[0], s[1]), s[0], s[1], s[2], some(s[3]), some(dense(up[0])), some(dentropy)), Tensor(),

@@ -708,12 +708,12 @@ kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const fl
 // ---------------------------------------------------------------- linear attention with a decay per head
 
 namespace {
-// Row offsets inside a 32-token chunk are 32-bit.
+// Row offsets inside a 32-token chunk are 32-bit, and so is a launch's number of threads.
 kla_status lin_desc(const kla_desc* d) {
     const kla_status st = check_desc(d);
     if (st != KLA_OK) return st;
     const int w = d->dk > d->dv ? d->dk : d->dv;
-    return (int64_t)d->H * w > (1 << 24) || d->T > (1 << 30) ? KLA_ERR_SHAPE : KLA_OK;
+    return (int64_t)d->H * w > (1 << 24) || d->T > (1 << 30) || (int64_t)d->B * d->H > (1 << 21) ? KLA_ERR_SHAPE : KLA_OK;
 }
 
 // KLA_CHECK=1: g <= 0 for every head (synchronous).
@@ -777,7 +777,7 @@ kla_status kla_linear_attn_backward(const kla_desc* desc, const void* q, const v
 kla_status kla_linear_attn_step(int32_t S, int32_t H, int32_t dk, int32_t dv, int32_t dtype, const void* q, const void* k,
                                 const void* v, const float* g, float* state, void* y, hipStream_t stream) {
     const kla_desc d{S, 1, H, dk, dv, dtype};
-    kla_status st = check_desc(&d);
+    kla_status st = lin_desc(&d);
     if (st != KLA_OK) return st;
     if (!q || !k || !v || !g || !state || !y) return KLA_ERR_NULL;
     if (!all_aligned(q, k, v, (const void*)g, (void*)state, y)) return KLA_ERR_ALIGN;
@@ -830,9 +830,9 @@ kla_status kla_layer_norm_backward(int64_t rows, int32_t n, int32_t dtype, const
 
 namespace {
 kla_status logp_shape(int32_t S, int64_t n, int32_t V, int32_t top) {
-    // one workgroup per row at least, indices of 32 bits within a row
+    // a workgroup of 256 threads per row at least, and 32 bits for a launch's threads and for a row's indices
     if (S < 1 || n < 0 || V < 1 || V > (1 << 30) || top < 0 || top > 32 || top > V) return KLA_ERR_SHAPE;
-    return n > INT32_MAX / S ? KLA_ERR_SHAPE : KLA_OK;
+    return n > ((1 << 24) - 1) / S ? KLA_ERR_SHAPE : KLA_OK;
 }
 }  // namespace
 

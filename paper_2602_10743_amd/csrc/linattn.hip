@@ -24,6 +24,8 @@
 // parts: the masked scores and the state (whose products are rounded to bf16 at the end) into two,
 // 16 bits, the decayed values that are added to the fp32 state into three, its 24 bits.
 // fp32: v_mfma_f32_16x16x4_f32.
+#include <atomic>
+
 #include "kla_buf.hpp"
 #include "kla_internal.hpp"
 #include "kla_mfma.hpp"
@@ -689,10 +691,18 @@ template <typename E, int N, int D, bool NOY>
 hipError_t launch(const LinArgs& a, hipStream_t st) {
     using Cfg = LinCfg<E, N, D, NOY>;
     auto kern = linattn_kernel<E, N, D, NOY>;
-    // more than 64 KiB of LDS must be opted into once per kernel (thread-safe static init)
-    static const hipError_t attr =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS);
-    if (attr != hipSuccess) return attr;
+    if constexpr (Cfg::LDS > 64 * 1024) {   // must be opted into, once per kernel and device
+        static std::atomic<uint64_t> done{0};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (!(done.load() & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS);
+            if (e != hipSuccess) return e;
+            done.fetch_or(bit);
+        }
+    }
     const size_t grid = (size_t)a.B * a.H * a.run * a.jobs * Cfg::NTILE;
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::NW * 64), Cfg::LDS, st, a);
     return hipGetLastError();

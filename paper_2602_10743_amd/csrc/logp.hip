@@ -12,14 +12,17 @@
 // kernel joins the parts in a fixed order.
 //
 // The top alternatives come from a threshold: the K-th largest of 64 lanes' maxima is at most the
-// K-th largest element, so the elements above it, of which there are few more than K, are collected
-// on a second reading of the row (from the caches) and ranked by a key that is larger for a larger
-// value and, among equals, for the lower index; keys are unique, so the order in which they were
-// collected does not matter.  Where that finds fewer than K elements or more than there is room for
-// (rows with fewer than K elements above -inf, rows of equal elements), K readings take one each.
+// K-th largest element.  It is taken after each thread's first blocks; the elements from it on are
+// collected as the rest is read, and from the first blocks again.  They are ranked by a key that is
+// larger for a larger value and, among equals, for the lower index; keys are unique, so the order in
+// which they were collected does not matter.  Where there are more than there is room for, the row is
+// read again with the threshold of all its elements, and where that does not help either (rows of
+// equal elements) or too few lie above it (fewer than K above -inf), K readings take one each.
 //
 // Rows may start anywhere: threads read the aligned 16-byte blocks that lie inside the row whole, and
 // the elements of the two at its ends one by one.
+#include <type_traits>
+
 #include "kla_device.hpp"
 #include "kla_internal.hpp"
 
@@ -67,20 +70,24 @@ struct Span {
     __device__ bool whole(size_t blk) const { return blk * kVec<E> >= a && (blk + 1) * kVec<E> <= b; }
 };
 
-// f(x, v) for the elements x of this part that a thread takes (v: its index in the row).
+// f(x, v) for the elements x of a block that are the row's (v: its index in the row).
 template <typename E, typename F>
-__device__ __forceinline__ void each(const E* x, const Span<E>& s, F&& f) {
+__device__ __forceinline__ void one_block(const E* x, const Span<E>& s, size_t blk, F&& f) {
     constexpr int N = kVec<E>;
-    for (size_t blk = s.lo + threadIdx.x; blk < s.hi; blk += kThreads) {
-        if (s.whole(blk)) {
-            float v[N];
-            unpack(reinterpret_cast<const uint4*>(x)[blk], v, E());
+    if (s.whole(blk)) {
+        float v[N];
+        unpack(reinterpret_cast<const uint4*>(x)[blk], v, E());
 #pragma unroll
-            for (int e = 0; e < N; ++e) f(v[e], (uint32_t)(blk * N + e - s.a));
-        } else {
-            for (size_t i = blk * N > s.a ? blk * N : s.a; i < (blk + 1) * N && i < s.b; ++i) f(ld(x, i), (uint32_t)(i - s.a));
-        }
+        for (int e = 0; e < N; ++e) f(v[e], (uint32_t)(blk * N + e - s.a));
+    } else {
+        for (size_t i = blk * N > s.a ? blk * N : s.a; i < (blk + 1) * N && i < s.b; ++i) f(ld(x, i), (uint32_t)(i - s.a));
     }
+}
+
+// The same for the blocks of this part before `hi` that a thread takes.
+template <typename E, typename F>
+__device__ __forceinline__ void each(const E* x, const Span<E>& s, size_t hi, F&& f) {
+    for (size_t blk = s.lo + threadIdx.x; blk < hi; blk += kThreads) one_block<E>(x, s, blk, f);
 }
 
 // Running maximum m (finite) and the sums about it.
@@ -112,10 +119,15 @@ __device__ __forceinline__ Sums joined(const Sums& a, const Sums& b) {
     return {m, p.s + q.s, p.u + q.u};
 }
 
-// Over the workgroup's threads, in every thread.
-__device__ __forceinline__ Sums block_join(Sums t, Sums* buf) {
+__device__ __forceinline__ Sums wave_join(Sums t) {
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) t = joined(t, Sums{__shfl_xor(t.m, k), __shfl_xor(t.s, k), __shfl_xor(t.u, k)});
+    return t;
+}
+
+// Over the workgroup's threads, in every thread.
+__device__ __forceinline__ Sums block_join(Sums t, Sums* buf) {
+    t = wave_join(t);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x / 64] = t;
     __syncthreads();
     t = buf[0];
@@ -142,10 +154,9 @@ struct TopScratch {
     float least;
 };
 
-// The K largest keys of this part's elements, in order, into out (0 where there are fewer).  m: the
-// maximum of the thread's own elements.
-template <typename E>
-__device__ void top_keys(const E* x, const Span<E>& sp, int K, float m, TopScratch& t, uint64_t* out) {
+// A bound at or below the K-th largest of the elements seen so far, m their maximum in this thread; the
+// list is emptied.
+__device__ __forceinline__ void set_least(int K, float m, TopScratch& t) {
     t.lane[threadIdx.x] = m;
     if (threadIdx.x == 0) t.count = 0;
     __syncthreads();
@@ -164,14 +175,27 @@ __device__ void top_keys(const E* x, const Span<E>& sp, int K, float m, TopScrat
         if (threadIdx.x == 0) t.least = value_of(pre);
     }
     __syncthreads();
-    const float least = t.least;
-    each<E>(x, sp, [&](float v, uint32_t i) {
-        if (v >= least) {
-            const uint32_t at = atomicAdd(&t.count, 1u);
-            if (at < kRoom) t.keys[at] = key_of(v, i);
-        }
-    });
+}
+
+__device__ __forceinline__ void collect(TopScratch& t, float least, float v, uint32_t i) {
+    if (v >= least) {
+        const uint32_t at = atomicAdd(&t.count, 1u);
+        if (at < kRoom) t.keys[at] = key_of(v, i);
+    }
+}
+
+// The K largest keys of this part's elements, in order, into out (0 where there are fewer), from those
+// collected with a bound of the first blocks.  m: the maximum of the thread's own elements.
+template <typename E>
+__device__ void top_keys(const E* x, const Span<E>& sp, int K, float m, TopScratch& t, uint64_t* out) {
     __syncthreads();
+    if (t.count > kRoom) {
+        __syncthreads();   // every thread has read the count
+        set_least(K, m, t);
+        const float least = t.least;
+        each<E>(x, sp, sp.hi, [&](float v, uint32_t i) { collect(t, least, v, i); });
+        __syncthreads();
+    }
     const int n = (int)t.count;
     if (n >= K && n <= kRoom) {
         for (int i = threadIdx.x; i < n; i += kThreads) {
@@ -185,7 +209,7 @@ __device__ void top_keys(const E* x, const Span<E>& sp, int K, float m, TopScrat
     uint64_t last = ~0ull;
     for (int k = 0; k < K; ++k) {
         uint64_t best = 0;
-        each<E>(x, sp, [&](float v, uint32_t i) {
+        each<E>(x, sp, sp.hi, [&](float v, uint32_t i) {
             const uint64_t key = key_of(v, i);
             if (key < last && key > best) best = key;
         });
@@ -215,18 +239,25 @@ struct LogpArgs {
     uint64_t* keys;           // [rows][parts][top]
 };
 
-// What is written of a row: t and best in every thread, the row's keys in LDS.
+// A row's target and its logit; rows are less than 2^31.
+struct Hot {
+    int64_t at;
+    float x;
+};
+__device__ __forceinline__ int64_t target_of(const LogpArgs& a, size_t r) { return a.target[(uint32_t)r % (uint32_t)a.n]; }
 template <typename E>
-__device__ __forceinline__ void finish(const LogpArgs& a, size_t r, const Sums& t, const uint64_t* best) {
+__device__ __forceinline__ Hot hot_of(const LogpArgs& a, size_t r) {
+    const int64_t tg = target_of(a, r);
+    return {tg, tg >= 0 && tg < a.V ? ld(static_cast<const E*>(a.logits), r * a.V + (size_t)tg) : 0.f};
+}
+
+// What is written of a row: t in every thread, the row's keys in LDS, h in thread 0.
+__device__ __forceinline__ void finish(const LogpArgs& a, size_t r, const Sums& t, const Hot& h, const uint64_t* best) {
     const float ls = logf(t.s);   // -inf for a row of -inf
     if (threadIdx.x == 0) {
-        const int64_t tg = a.target[r % a.n];
         float lp = 0.f;           // no target
-        if (tg >= a.V) lp = __uint_as_float(0x7fc00000u);
-        else if (tg >= 0) {
-            const float x = ld(static_cast<const E*>(a.logits), r * a.V + (size_t)tg);
-            lp = t.s == 0.f ? -__builtin_inff() : x - t.m - ls;
-        }
+        if (h.at >= a.V) lp = __uint_as_float(0x7fc00000u);
+        else if (h.at >= 0) lp = t.s == 0.f ? -__builtin_inff() : h.x - t.m - ls;
         a.logp[r] = lp;
         if (a.entropy) a.entropy[r] = t.s == 0.f ? 0.f : ls - t.u / t.s;
         if (a.stat) {
@@ -254,13 +285,17 @@ __global__ __launch_bounds__(kThreads) void logp_fwd_kernel(LogpArgs a) {
     const int part = blockIdx.x % a.parts;
     const E* x = static_cast<const E*>(a.logits);
     const Span<E> sp(r, a.V, part, a.parts);
+    TopScratch& ts = *reinterpret_cast<TopScratch*>(scratch);
+    Hot hot{-1, 0.f};   // asked for first: at the end nothing would hide the two reads
+    if (threadIdx.x == 0 && a.parts == 1) hot = hot_of<E>(a, r);
     Sums t{kLowest, 0.f, 0.f};
     constexpr int U = 4;   // blocks in flight per thread
-    size_t blk = sp.lo + threadIdx.x;
-    for (; blk + (U - 1) * kThreads < sp.hi; blk += U * kThreads) {
-        float v[U * N];
+    // M blocks of this thread from blk on, kThreads apart
+    auto take = [&](size_t blk, auto count, float least) __attribute__((always_inline)) {
+        constexpr int M = decltype(count)::value;
+        float v[M * N];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
+        for (int i = 0; i < M; ++i) {
             const size_t bi = blk + (size_t)i * kThreads;
             if (sp.whole(bi)) {
                 unpack(reinterpret_cast<const uint4*>(x)[bi], v + i * N, E());
@@ -272,38 +307,52 @@ __global__ __launch_bounds__(kThreads) void logp_fwd_kernel(LogpArgs a) {
                 }
             }
         }
-        float m = t.m;
+        float m = -__builtin_inff();
 #pragma unroll
-        for (int e = 0; e < U * N; ++e) m = fmaxf(m, v[e]);
-        rise(t, m);
+        for (int i = 0; i < M; ++i) {
+            float bm = v[i * N];
 #pragma unroll
-        for (int e = 0; e < U * N; ++e) add<ENT>(t, v[e]);
-    }
-    for (; blk < sp.hi; blk += kThreads) {
-        float v[N];
+            for (int e = 1; e < N; ++e) bm = fmaxf(bm, v[i * N + e]);
+            if constexpr (TOP) {
+                if (bm >= least)
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const size_t at = blk * N + e;
-            v[e] = at >= sp.a && at < sp.b ? ld(x, at) : -__builtin_inff();
+                    for (int e = 0; e < N; ++e) {
+                        const size_t at = (blk + (size_t)i * kThreads) * N + e;
+                        if (at >= sp.a && at < sp.b) collect(ts, least, v[i * N + e], (uint32_t)(at - sp.a));
+                    }
+            }
+            m = fmaxf(m, bm);
         }
-        float m = t.m;
+        rise(t, fmaxf(t.m, m));
 #pragma unroll
-        for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
-        rise(t, m);
-#pragma unroll
-        for (int e = 0; e < N; ++e) add<ENT>(t, v[e]);
+        for (int e = 0; e < M * N; ++e) add<ENT>(t, v[e]);
+    };
+    size_t blk = sp.lo + threadIdx.x;
+    auto rest = [&](size_t hi, float least) __attribute__((always_inline)) {
+        for (; blk + (U - 1) * kThreads < hi; blk += U * kThreads) take(blk, std::integral_constant<int, U>(), least);
+        for (; blk < hi; blk += kThreads) take(blk, std::integral_constant<int, 1>(), least);
+    };
+    if constexpr (TOP) {
+        const size_t first = sp.lo + U * kThreads < sp.hi ? sp.lo + U * kThreads : sp.hi;
+        rest(first, __uint_as_float(0x7fc00000u));   // a bound that nothing reaches
+        set_least(a.top, t.m, ts);
+        const float least = ts.least;
+        rest(sp.hi, least);
+        each<E>(x, sp, first, [&](float v, uint32_t i) { collect(ts, least, v, i); });
+    } else {
+        rest(sp.hi, 0.f);
     }
     const float own = t.m;
     t = block_join(t, buf);
     if constexpr (TOP) {
         uint64_t* out = a.parts > 1 ? a.keys + (size_t)blockIdx.x * a.top : best;
-        top_keys<E>(x, sp, a.top, own, *reinterpret_cast<TopScratch*>(scratch), out);
+        top_keys<E>(x, sp, a.top, own, ts, out);
         __syncthreads();
     }
     if (a.parts > 1) {
         if (threadIdx.x == 0) a.sums[blockIdx.x] = t;
     } else {
-        finish<E>(a, r, t, best);
+        finish(a, r, t, hot, best);
     }
 }
 
@@ -315,8 +364,11 @@ __global__ __launch_bounds__(kThreads) void logp_join_kernel(LogpArgs a) {
     __shared__ uint64_t least;
     __shared__ uint32_t count;
     const size_t r = blockIdx.x;
-    Sums t = a.sums[r * a.parts];
-    for (int p = 1; p < a.parts; ++p) t = joined(t, a.sums[r * a.parts + p]);
+    Hot hot{-1, 0.f};
+    if (threadIdx.x == 0) hot = hot_of<E>(a, r);
+    Sums t{kLowest, 0.f, 0.f};   // a part a lane, in every wave
+    if ((int)(threadIdx.x & 63) < a.parts) t = a.sums[r * a.parts + (threadIdx.x & 63)];
+    t = wave_join(t);
     if (a.top > 0) {
         const int n = a.parts * a.top;
         const uint64_t* in = a.keys + r * n;
@@ -347,7 +399,7 @@ __global__ __launch_bounds__(kThreads) void logp_join_kernel(LogpArgs a) {
         }
         __syncthreads();
     }
-    finish<E>(a, r, t, best);
+    finish(a, r, t, hot, best);
 }
 
 // dlogits of one part of one row.
@@ -360,7 +412,7 @@ __global__ __launch_bounds__(kThreads) void logp_bwd_kernel(LogpArgs a, const fl
     E* o = static_cast<E*>(dlogits);
     const Span<E> sp(r, a.V, blockIdx.x % a.parts, a.parts);
     const float m = a.stat[2 * r], s = a.stat[2 * r + 1], ls = logf(s), inv = 1.f / s;
-    const int64_t tg = a.target[r % a.n];
+    const int64_t tg = target_of(a, r);
     const float dl = tg < 0 || !dlogp ? 0.f : tg < a.V ? dlogp[r] : __uint_as_float(0x7fc00000u);
     const float de = dent ? dent[r] : 0.f;
     // dlogp + dent (log p_v + entropy) = base + dent (x_v - m)

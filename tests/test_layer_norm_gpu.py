@@ -152,6 +152,10 @@ def test_autograd(kla):
     ref = formula(x3.detach().double().reshape(24, 96), w.detach().double(), b.detach().double(), 1e-5, dy.double())
     for got, want in zip((y.detach(), dx, dw, db), ref):
         assert torch.allclose(got.double().reshape(want.shape), want, rtol=1e-5, atol=1e-5)
+    odd = torch.empty(24 * 96 + 1, device=DEV)[1:].view(12, 2, 96).copy_(d3)   # off 16 bytes
+    assert torch.equal(torch.autograd.grad(kla.kla_layer_norm(x3, w, b), w, odd)[0], dw)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(kla.kla_layer_norm(x3, w, b), w, d3, create_graph=True)
     (dw2,) = torch.autograd.grad(kla.kla_layer_norm(x3, w), w, d3)
     assert torch.equal(dw2, dw)
 

@@ -248,6 +248,11 @@ def test_autograd(kla):
     (g1,) = torch.autograd.grad(sT, one, d["ds"])
     want = (torch.exp(d["g"].double()[:, None, None] * d["len"].view(-1, 1, 1, 1)) * d["ds"].double()).sum(0, keepdim=True)
     assert torch.allclose(g1.double(), want, rtol=1e-5, atol=1e-6)
+    y, _ = kla.kla_linear_attn(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"])
+    odd = torch.empty(d["dy"].numel() + 1, device=DEV)[1:].view_as(d["dy"]).copy_(d["dy"])   # off 16 bytes
+    assert torch.equal(torch.autograd.grad(y, d["q"], odd, retain_graph=True)[0], torch.autograd.grad(y, d["q"], d["dy"])[0])
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(kla.kla_linear_attn(d["q"], d["k"], d["v"], d["g"])[0], d["q"], d["dy"], create_graph=True)
     with pytest.raises(ValueError, match="constants"):
         kla.kla_linear_attn(d["q"], d["k"], d["v"], d["g"].clone().requires_grad_(True))
 

@@ -45,6 +45,7 @@ def test_linear_attn(lib):
     fwd = lambda d, a, n=0: lib.kla_linear_attn_forward(d, *a, n, None)
     assert fwd(desc(dk=24), ok) == 2 and fwd(desc(B=0), ok) == 2 and fwd(desc(T=-1), ok) == 2
     assert fwd(desc(H=1 << 24, dk=32), ok) == 2           # row offsets of a chunk past 32 bits
+    assert fwd(desc(B=1 << 20, H=4), ok) == 2             # a launch's threads past 32 bits
     assert fwd(desc(dtype=3), ok) == 3 and fwd(None, ok) == 1
     for i in (0, 1, 2, 3, 6):
         assert fwd(desc(), put(ok, i, None)) == 1, i
@@ -65,7 +66,7 @@ def test_linear_attn(lib):
         assert bwd(desc(), put(ok, i, ODD)) == 4, i
     ok = [FAKE] * 6
     step = lambda a, S=2, H=1, dk=16, dv=16, t=0: lib.kla_linear_attn_step(S, H, dk, dv, t, *a, None)
-    assert step(ok, dk=48) == 2 and step(ok, S=0) == 2 and step(ok, t=2) == 3
+    assert step(ok, dk=48) == 2 and step(ok, S=0) == 2 and step(ok, S=1 << 20, H=4) == 2 and step(ok, t=2) == 3
     for i in range(6):
         assert step(put(ok, i, None)) == 1 and step(put(ok, i, ODD)) == 4, i
 
@@ -97,7 +98,7 @@ def test_token_logp(lib):
     fwd = lambda a, S=1, n=2, V=50, top=0, t=0, ws=0: lib.kla_token_logp_forward(S, n, V, top, t, *a, ws, None)
     ok = [FAKE] * 3 + [None] * 5
     assert fwd(ok, S=0) == 2 and fwd(ok, n=-1) == 2 and fwd(ok, V=0) == 2 and fwd(ok, top=33) == 2 and fwd(ok, top=-1) == 2
-    assert fwd(ok, V=4, top=5) == 2 and fwd(ok, S=4, n=1 << 30) == 2 and fwd(ok, t=2) == 3
+    assert fwd(ok, V=4, top=5) == 2 and fwd(ok, S=4, n=1 << 22) == 2 and fwd(ok, t=2) == 3
     for i in range(3):
         assert fwd(put(ok, i, None)) == 1, i
     assert fwd(ok, top=1) == 1

@@ -175,6 +175,16 @@ def test_ties(kla, dtype):
     check(kla, x.repeat(1, 8)[:2].contiguous(), target[:2], top=20)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rising_rows(kla, dtype):
+    """Rows in order, whose first elements say nothing about the largest."""
+    x, target = make((3,), 40000, dtype, 5)
+    x = x.sort(-1).values.contiguous()
+    x[1] = x[1].flip(0)
+    check(kla, x, target, top=8)
+    check(kla, x.repeat(300, 1), target.repeat(300), top=32)
+
+
 def test_large_logits(kla):
     for scale, at in ((1.0, 3e4), (100.0, 0.0), (1.0, -1e6)):
         x, target = make((7,), 1500, "f32", 9, scale)
@@ -231,6 +241,11 @@ def test_autograd(kla):
     assert torch.allclose(dx.double(), f(dlogp, dent), atol=1e-5)
     (de,) = torch.autograd.grad(ent, x, dent)   # one of the two alone
     assert torch.allclose(de.double(), f(0 * dlogp, dent), atol=1e-5)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(ent, x, dent, create_graph=True)
+    # slices that start off 16 bytes, of the logits, the targets and the gradients
+    (do,) = torch.autograd.grad(kla.kla_token_logp(x[1, 1:], target[1:]), x, torch.cat([dlogp[1], dlogp[0]])[1:8])
+    assert torch.allclose(do[1, 1:].double(), f(dlogp, 0 * dent)[1, 1:], atol=1e-5) and not do[0].any()
     (dl,) = torch.autograd.grad(kla.kla_token_logp(x, target), x, dlogp)
     assert torch.allclose(dl.double(), f(dlogp, 0 * dent), atol=1e-5)
 
