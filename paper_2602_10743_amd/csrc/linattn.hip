@@ -349,21 +349,22 @@ __device__ __forceinline__ int seq_len(const LinArgs& a, int b) {
 // 16 bytes a lane from r at voff into LDS at dst + 16 lane; lanes past the buffer's end write zeros.  Not the
 // compiler's builtin, behind which every transposing read of LDS waits for all loads in flight, the prefetch
 // among them: who reads the tile waits with wait_vm_le.  Nothing is loaded into registers, and nothing else
-// in this file uses m0.
+// in this file uses m0.  The wait states are those between a vector instruction that writes a scalar register
+// (readfirstlane) and a memory access that reads it, which the compiler does not count inside.
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t words_t;
 __device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_t voff) {
     words_t u;   // uniform: in scalar registers
 #pragma unroll
     for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_readfirstlane(r[i]);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
                  "s"(__builtin_amdgcn_readfirstlane(dst))
                  : "memory");
 }
 
 // A workgroup takes DT of the D columns, a wave CW of them.  Where the rows of Q and K are long and the waves
 // that compute (NCW) few, others help with the loads.  64 columns in waves of 16 leave 168 registers and 53 KiB of
-// LDS, so three workgroups of 128-wide bf16 passes share a CU (B = 8, T = 2048, H = 16: forward 108 us and
-// backward 215, against 138 and 227 with 128 columns in waves of 32, whose scores are formed half as
+// LDS, so three workgroups of 128-wide bf16 passes share a CU (B = 8, T = 2048, H = 16: forward 100 us and
+// backward 196, against 139 and 226 with 128 columns in waves of 32, whose scores are formed half as
 // often but which one or two waves a SIMD have to hide).  The states' pass forms no scores: all columns.
 template <typename E, int N, int D, bool NOY>
 struct LinCfg {
@@ -384,7 +385,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
     using TV = Tile<E, DT>;
     constexpr int UQ = NOY ? 0 : TQ::UNITS, UK = TQ::UNITS, UNITS = UQ + UK + TV::UNITS;
     constexpr int NL = (UNITS + NW - 1) / NW;   // a wave's loads per chunk
-    constexpr int NST = NOY ? 0 : 2 * NDT;                          // and stores, of one that computes
+    constexpr int NST = NOY ? 0 : 2 * NDT;      // and stores, of one that computes
     constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
     float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
@@ -801,35 +802,42 @@ hipError_t step(const Shape& s, const void* q, const void* k, const void* v, con
     }
 }
 
-// Segments per sequence and chunks in one, for passes of `groups` workgroups where no sequence is cut.
-// Segments cost a pass over K and V for their states and two launches more, so a sequence of fewer than 16
-// chunks is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, B = 8, T = 2048,
-// H = 16, us whole, in two, in three: forward, 256 workgroups, 108, 131, 118; backward, 768, 215, 274, 282).
-// Otherwise three workgroups a CU, of two chunks at least (B = 1, T = 65536, forward: 471 in 16 segments, 442
-// in 24, 460 in 32; B = 3, T = 777, H = 5, 64 and 128 wide: 30 in two, 19 in twelve, 22 in 25).
-void segments(const Shape& s, long groups, int& ns, int& lc) {
+// Segments per sequence and chunks in one, for passes of `groups` workgroups where no sequence is cut, to
+// make `want`, or `more` where segments would be longer than 96 chunks.  Segments cost a pass over K and V for their states and two launches more, so a sequence of
+// fewer than 16 chunks is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, B = 8,
+// T = 2048, H = 16, us whole and in two: forward, 256 workgroups, 100 and 135; backward, 768, 196 and 282).
+// Otherwise the forward makes two workgroups a CU and the backward, whose passes share their reads,
+// three (us in 4, 8, 16, 24 segments, B = 1, T = 16384, H = 16, forward 295, 158, 117, 119, backward 381,
+// 282, 277, 294; B = 4, T = 4096, H = 8, forward 88, 71, 73, 80, backward 147, 147, 168, 196), but none
+// shorter than two chunks; where they are long, one and three workgroups a CU more (T = 65536 in 8, 16, 24,
+// 32: forward 582, 447, 427, 457, backward 1170, 1054, 1071, 1083).
+void segments(const Shape& s, long groups, long want, long more, int& ns, int& lc) {
     const int nc = (s.T + kLC - 1) / kLC;
     ns = 1;
     lc = nc;
     if (nc < 16 || groups >= 256) return;
-    const long want = (768 + groups - 1) / groups;
-    ns = (int)(want < nc / 2 ? want : nc / 2);
+    ns = (int)((want + groups - 1) / groups);
+    if (nc > 96 * ns) ns = (int)((more + groups - 1) / groups);
+    if (ns > nc / 2) ns = nc / 2;
     lc = (nc + ns - 1) / ns;
     ns = (nc + lc - 1) / lc;
 }
 
 long tiles(int D) { return D > 64 ? 2 : 1; }   // workgroups of a pass over one sequence
-long fwd_groups(const Shape& s) { return (long)s.B * s.H * tiles(s.dv); }
-long bwd_groups(const Shape& s) { return (long)s.B * s.H * (2 * tiles(s.dk) + tiles(s.dv)); }
+void fwd_segments(const Shape& s, int& ns, int& lc) { segments(s, (long)s.B * s.H * tiles(s.dv), 512, 768, ns, lc); }
+void bwd_segments(const Shape& s, int& ns, int& lc) {
+    segments(s, (long)s.B * s.H * (2 * tiles(s.dk) + tiles(s.dv)), 768, 1536, ns, lc);
+}
 
-LinArgs args_of(const Shape& s, const float* g, const int* len, long groups) {
+LinArgs args_of(const Shape& s, const float* g, const int* len, bool backward) {
     LinArgs a{};
     a.g = g;
     a.len = len;
     a.B = s.B;
     a.T = s.T;
     a.H = s.H;
-    segments(s, groups, a.ns, a.lc);
+    if (backward) bwd_segments(s, a.ns, a.lc);
+    else fwd_segments(s, a.ns, a.lc);
     return a;
 }
 
@@ -858,13 +866,13 @@ size_t states_bytes(const Shape& s, int ns) {
 }  // namespace
 
 size_t linattn_workspace(const Shape& s, bool backward) {
-    const LinArgs a = args_of(s, nullptr, nullptr, backward ? bwd_groups(s) : fwd_groups(s));
+    const LinArgs a = args_of(s, nullptr, nullptr, backward);
     return (backward ? 2 : 1) * states_bytes(s, a.ns);
 }
 
 hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
                               const int* len, void* y, float* sT, void* ws, hipStream_t st) {
-    LinArgs a = args_of(s, g, len, fwd_groups(s));
+    LinArgs a = args_of(s, g, len, false);
     a.jobs = 1;
     a.run = a.ns;
     a.job[0] = LinJob{q, k, v, s0, y, sT, 0, 0};
@@ -880,7 +888,7 @@ hipError_t launch_linattn_fwd(const Shape& s, const void* q, const void* k, cons
 hipError_t launch_linattn_bwd(const Shape& s, const void* q, const void* k, const void* v, const float* g, const float* s0,
                               const int* len, const void* dy, const float* dsT, void* dq, void* dk, void* dv, float* ds0,
                               void* ws, hipStream_t st) {
-    LinArgs a = args_of(s, g, len, bwd_groups(s));
+    LinArgs a = args_of(s, g, len, true);
     a.run = a.ns;
     const float *first = s0, *last = dsT;
     if (a.ns > 1) {   // the states before the segments, and their adjoints behind them
