@@ -301,6 +301,7 @@ __global__ __launch_bounds__(512) void layernorm_parts_kernel(int nparts, int n,
     const size_t c = (size_t)blockIdx.x * 32 + col, n2 = 2 * (size_t)n;
     float t = 0.f;
     if (c < n2)
+#pragma unroll 8
         for (int p = k; p < nparts; p += 16) t += part[p * n2 + c];
     s[k][col] = t;
     __syncthreads();

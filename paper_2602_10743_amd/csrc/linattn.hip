@@ -165,6 +165,18 @@ struct Acc<uint16_t> {
                                                HALF ? 0u : cvt_pk_bf16(lb[0], lb[1]), HALF ? 0u : cvt_pk_bf16(lb[2], lb[3])});
         return o;
     }
+    // One tile's parts as 16 bytes of a lane, and the operands of (tile, nothing) or two tiles from them.
+    __device__ static uint4 packed(const f32x4& a, const Pick& pick) {
+        const Acc o = from<true>(a, zero4(), pick);
+        const uint4 h = __builtin_bit_cast(uint4, o.h), l = __builtin_bit_cast(uint4, o.l);
+        return uint4{h.x, h.y, l.x, l.y};
+    }
+    __device__ static Acc of(const uint4& a, const uint4& b) {
+        Acc o;
+        o.h = __builtin_bit_cast(bf16x8, uint4{a.x, a.y, b.x, b.y});
+        o.l = __builtin_bit_cast(bf16x8, uint4{a.z, a.w, b.z, b.w});
+        return o;
+    }
 };
 template <>
 struct Acc<float> {
@@ -182,6 +194,10 @@ struct Acc<float> {
             o.x[4 + e] = b[e];
         }
         return o;
+    }
+    __device__ static uint4 packed(const f32x4& a, const Pick&) { return __builtin_bit_cast(uint4, a); }
+    __device__ static Acc of(const uint4& a, const uint4& b) {
+        return from(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, b), Pick(0, 0));
     }
 };
 
@@ -296,8 +312,12 @@ __device__ __forceinline__ void store4(float, const f32x4& y, rsrc_t r, uint32_t
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), r, voff, 0, 0);
 }
 
-// e^{g n}, 1 for n = 0 whatever g is; formed in fp64 because g n may be large where g has few digits left
-__device__ __forceinline__ float decay_pow(float g, int n) { return n == 0 ? 1.f : (float)exp((double)g * n); }
+// e^{g n}, 1 for n = 0 whatever g is.  The exponent is formed in fp64, where g n keeps its digits, and its
+// fraction is an argument of at most 1/2 of the hardware's 2^x (1 ulp): every workgroup begins with these.
+__device__ __forceinline__ float decay_pow(float g, int n) {
+    const double x = fmin(fmax((double)g * (double)n * 1.4426950408889634, -300.0), 300.0), i = rint(x);
+    return n == 0 ? 1.f : ldexpf(__builtin_amdgcn_exp2f((float)(x - i)), (int)i);
+}
 
 __device__ __forceinline__ float lds_val(uint16_t, const unsigned char* p) {
     return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p));
@@ -370,7 +390,7 @@ template <typename E, int N, int D, bool NOY>
 struct LinCfg {
     static constexpr int CW = NOY && D == 128 ? 32 : 16, DT = NOY || D <= 64 ? D : 64, NTILE = D / DT, NCW = DT / CW;
     static constexpr int ROW = N * (int)sizeof(E), LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1, NW = NCW > LW ? NCW : LW;
-    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES, LDS = 2 * BUF + 2 * kLC * (int)sizeof(float);
+    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES, LDS = 2 * BUF + 2 * kLC * (int)sizeof(float) + 3 * 1024;
     // waves per SIMD: fp32 states and operands of 128 slots need more than the registers of three
     static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : 3;
 };
@@ -389,6 +409,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
     constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
     float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
+    uint4* scores = reinterpret_cast<uint4*>(pw + 2 * kLC);   // of the chunk, three tiles
 
     int vi, ji, tile;   // the passes and tiles of one sequence on one XCD: they read the same rows
     {
@@ -544,25 +565,32 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             weights(n);
             gn = uniform(pw[n]);
         }
-        f32x4 y[NDT][2], in[NDT][2];
-        float rs[2];
+        constexpr int ST = N == 16 ? 4 : 8;
+        if constexpr (!NOY) {
+            // the waves share the scores S^T[j, i] = K_j . Q_i, masked: tiles (jt, it) = (0,0), (0,1), (1,1)
+            for (int t = wave; t < 3; t += NW) {
+                f32x4 s = zero4();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    s = mma<ST>(Op<E>::template row<N>(sK, (t == 2 ? 16 : 0) + l16, ks, g4),
+                                Op<E>::template row<N>(sQ, (t > 0 ? 16 : 0) + l16, ks, g4), s);
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) s[rr] *= t == 1 ? off[rr] : dia[rr];
+                scores[t * 64 + lane] = Acc<E>::packed(s, pick);
+            }
+        }
+        Op<E> vf[NDT];
+        f32x4 y[NDT][2];
+        const float was = rho;
         if (works) {
-            Op<E> vf[NDT];
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) vf[dt] = Op<E>::template col<DT>(sV, dl0 + 16 * dt, g4, l16);
-            f32x4 s00 = zero4(), s01 = zero4(), s11 = zero4();
-            if constexpr (!NOY) {
-                // S^T[j, i] = K_j . Q_i, tiles (jt, it) = (0,0), (0,1), (1,1); Y^T[d, i] from the state
+            if constexpr (!NOY) {   // Y^T[d, i] from the state
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) y[dt][0] = y[dt][1] = zero4();
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    constexpr int ST = N == 16 ? 4 : 8;
                     const Op<E> qs[2] = {Op<E>::template row<N>(sQ, l16, ks, g4), Op<E>::template row<N>(sQ, 16 + l16, ks, g4)};
-                    const Op<E> k0 = Op<E>::template row<N>(sK, l16, ks, g4), k1 = Op<E>::template row<N>(sK, 16 + l16, ks, g4);
-                    s00 = mma<ST>(k0, qs[0], s00);
-                    s01 = mma<ST>(k0, qs[1], s01);
-                    s11 = mma<ST>(k1, qs[1], s11);
                     Acc<E> r[NDT];
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt)
@@ -572,7 +600,6 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             }
 
             // R <- e^{g n} R + K^T (w V)
-            const float was = rho;
             float w[8];
             rho *= gn;
             float inv = 1.f;
@@ -595,15 +622,13 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
                 for (int i = 0; i < RT; ++i) kt[i] = Op<E>::template slots<N>(sK, rt + i, g4, l16);
                 mma_each<RT, NDT>(kt, vs, R + rt);
             }
-
-            if constexpr (!NOY) {
-#pragma unroll
-                for (int rr = 0; rr < 4; ++rr) {
-                    s00[rr] *= dia[rr];
-                    s01[rr] *= off[rr];
-                    s11[rr] *= dia[rr];
-                }
-                const Acc<E> p0 = Acc<E>::template from<true>(s00, zero4(), pick), p1 = Acc<E>::from(s01, s11, pick);
+        }
+        if constexpr (!NOY) {
+            __syncthreads();   // the scores are there
+            if (works) {
+                const uint4 none{0u, 0u, 0u, 0u};
+                const Acc<E> p0 = Acc<E>::of(scores[lane], none), p1 = Acc<E>::of(scores[64 + lane], scores[128 + lane]);
+                f32x4 in[NDT][2];
                 float sum = 0.f;   // not finite where a value is not
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt) {
@@ -612,28 +637,23 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
 #pragma unroll
                     for (int rr = 0; rr < 4; ++rr) sum += in[dt][0][rr] + in[dt][1][rr];
                 }
-                rs[0] = rd[0] * was;
-                rs[1] = rd[1] * was;
                 if (__any(!(fabsf(sum) <= 3.4e38f)))
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
                         for (int it = 0; it < 2; ++it)
                             in[dt][it] = masked_sums<E, N, DT>(sQ, sK, sV, pw, dl0 + 16 * dt, 16 * it + l16, g4);
-            }
-        }
-        if constexpr (!NOY) {
-            if (works) {
                 const rsrc_t ry = rsrc_of(py, sd, n, CW * ES);
                 const uint32_t hd = shift_of(sd, n);
                 py += step_d;
 #pragma unroll
                 for (int it = 0; it < 2; ++it) {
                     const uint32_t to = yoff[it] - hd;
+                    const float f = rd[it] * was;
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt) {
 #pragma unroll
-                        for (int rr = 0; rr < 4; ++rr) y[dt][it][rr] = y[dt][it][rr] * rs[it] + in[dt][it][rr];
+                        for (int rr = 0; rr < 4; ++rr) y[dt][it][rr] = y[dt][it][rr] * f + in[dt][it][rr];
                         store4(E(), y[dt][it], ry, to + 16 * dt * ES);
                     }
                 }

@@ -150,7 +150,8 @@ def test_ragged_batch(kla, state, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,T,H,dk,dv,ragged", [(1, 2100, 1, 64, 64, False), (2, 1111, 1, 32, 128, True),
-                                                (3, 1300, 2, 16, 16, True), (1, 1025, 3, 128, 64, False)])
+                                                (3, 1300, 2, 16, 16, True), (1, 1025, 3, 128, 64, False),
+                                                (1, 1056, 1, 128, 128, False)])
 def test_few_long_sequences(kla, B, T, H, dk, dv, ragged, dtype):
     """Enough chunks and few enough sequences that they are cut into segments."""
     x = make(B, T, H, dk, dv, dtype, True, ragged, T)
