@@ -124,11 +124,12 @@ __device__ __forceinline__ void group_sum2(float& a, float& b, float* buf, int& 
     }
 }
 
-// Workgroup sizes: forward 256 threads, backward 512, 1024 for rows of 1024 lanes.
+// Workgroup sizes: forward 256 threads, more for rows of more lanes; backward 1024, one workgroup a CU, so that
+// there are few parts (16384 x 2048 bf16: 46 us; 50 with 512 threads, 54 with two such workgroups a CU;
+// 65536 x 256: 28, 37, 27).
 template <int TPR>
 constexpr int kFwdThreads = TPR > 256 ? TPR : 256;
-template <int TPR>
-constexpr int kBwdThreads = TPR > 512 ? TPR : 512;
+constexpr int kBwdThreads = 1024;
 
 template <typename E, int VEC, int EPT, int TPR>
 __global__ __launch_bounds__(kFwdThreads<TPR>) void layernorm_fwd_kernel(size_t rows, int n, const E* __restrict__ x,
@@ -197,15 +198,16 @@ __global__ __launch_bounds__(kFwdThreads<TPR>) void layernorm_fwd_kernel(size_t 
 
 // part: [gridDim.x][2][n], the workgroups' sums of dw and dbias.
 template <typename E, int VEC, int EPT, int TPR>
-__global__ __launch_bounds__(kBwdThreads<TPR>) void layernorm_bwd_kernel(size_t rows, int n, const E* __restrict__ x,
+__global__ __launch_bounds__(kBwdThreads) void layernorm_bwd_kernel(size_t rows, int n, const E* __restrict__ x,
                                                                        const float* __restrict__ w,
                                                                        const float* __restrict__ mean,
                                                                        const float* __restrict__ rstd,
                                                                        const E* __restrict__ dout, E* __restrict__ dx,
                                                                        float* __restrict__ part) {
-    constexpr int HB = EPT / VEC, RPB = kBwdThreads<TPR> / TPR;
+    constexpr int HB = EPT / VEC, RPB = kBwdThreads / TPR;
     __shared__ float buf[TPR > 64 ? 2 * RPB * 2 * (TPR / 64) : 1];
-    __shared__ float join[RPB > 1 ? 2 * EPT * TPR : 1];
+    constexpr int JG = kBwdThreads / (TPR < 64 ? 64 : TPR);   // groups that join: of a wave at least
+    __shared__ float join[JG > 1 ? 2 * EPT * TPR : 1];
     const int tl = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const float inv = 1.f / (float)n;
     float wr[EPT], sw[EPT], sb[EPT];
@@ -261,10 +263,21 @@ __global__ __launch_bounds__(kBwdThreads<TPR>) void layernorm_bwd_kernel(size_t 
             }
         }
     }
+    if constexpr (TPR < 64) {   // a wave's groups
+#pragma unroll
+        for (int m = TPR; m < 64; m *= 2)
+#pragma unroll
+            for (int j = 0; j < EPT; ++j) {
+                sw[j] += __shfl_xor(sw[j], m);
+                sb[j] += __shfl_xor(sb[j], m);
+            }
+    }
+    const int jg = threadIdx.x / (TPR < 64 ? 64 : TPR);
+    const bool first = TPR >= 64 || (threadIdx.x & 63) < TPR;   // of its wave's groups
     // the groups' sums one after another into LDS, the last group's into the part
-    if constexpr (RPB > 1) {
-        for (int k = 0; k < RPB; ++k) {
-            if (group == k) {
+    if constexpr (JG > 1) {
+        for (int k = 0; k < JG; ++k) {
+            if (jg == k && first) {
 #pragma unroll
                 for (int j = 0; j < EPT; ++j) {
                     if (k > 0) {
@@ -278,7 +291,7 @@ __global__ __launch_bounds__(kBwdThreads<TPR>) void layernorm_bwd_kernel(size_t 
             __syncthreads();
         }
     }
-    if (group == RPB - 1) {
+    if (jg == JG - 1 && first) {
         float* p = part + (size_t)blockIdx.x * 2 * n;
 #pragma unroll
         for (int i = 0; i < HB; ++i)
@@ -374,10 +387,10 @@ struct Bwd {
     hipStream_t st;
     template <typename E, int VEC, int EPT, int TPR>
     hipError_t run() {
-        constexpr int RPB = kBwdThreads<TPR> / TPR;
+        constexpr int RPB = kBwdThreads / TPR;
         const size_t blocks = (rows + RPB - 1) / RPB;
         const unsigned grid = (unsigned)(blocks < 1 ? 1 : blocks < kParts ? blocks : kParts);
-        layernorm_bwd_kernel<E, VEC, EPT, TPR><<<dim3(grid), dim3(kBwdThreads<TPR>), 0, st>>>(
+        layernorm_bwd_kernel<E, VEC, EPT, TPR><<<dim3(grid), dim3(kBwdThreads), 0, st>>>(
             rows, n, static_cast<const E*>(x), w, mean, rstd, static_cast<const E*>(dout), static_cast<E*>(dx), part);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
