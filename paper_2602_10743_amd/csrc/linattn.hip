@@ -533,8 +533,8 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
     const typename Acc<E>::Pick pick(g4, l16);
     const uint32_t yoff[2] = {row_off(l16, sd) + (uint32_t)(4 * g4 * ES), row_off(16 + l16, sd) + (uint32_t)(4 * g4 * ES)};
     weights(kLC);
-    // The state is rho R, so that its decay is one product a chunk and not one an element, until rho is small.
-    // Uniform: the branches on them are the wave's.
+    // The state is rho R, so that its decay is one product a chunk and not one an element, until rho is under
+    // 2^-8 (which leaves R all but 8 of the exponents).  Uniform: the branches on them are the wave's.
     auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
     float gn = uniform(pw[kLC]), rho = 1.f;
     auto scale = [&](float f) {
@@ -603,7 +603,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             float w[8];
             rho *= gn;
             float inv = 1.f;
-            if (rho >= 0x1p-20f) {
+            if (rho >= 0x1p-8f) {
                 inv = 1.f / rho;
             } else {
                 scale(rho);

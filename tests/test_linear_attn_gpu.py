@@ -87,11 +87,11 @@ def run(kla, x):
     return out
 
 
-def check(got, x, what=""):
+def check(got, x, what="", names=("y", "sT", "dq", "dk", "dv", "ds0")):
     ref, mass = expected(x), expected(x, torch.abs)
     T = x["q"].shape[1]
     N = max(x["q"].shape[-1], x["v"].shape[-1])
-    for n in ("y", "sT", "dq", "dk", "dv", "ds0"):
+    for n in names:
         out = got[n].double().cpu()
         assert torch.isfinite(out).all(), f"{n} is not finite {what}"
         tol = (N + 64 + 4 * (T // 32 + 1)) * 2.0 ** -24 * mass[n] + 1e-30
@@ -179,14 +179,55 @@ def test_no_tokens(kla):
     assert not got["sT"].any() and not got["ds0"].any()
 
 
+def test_lengths_are_taken_into_the_sequence(kla):
+    x = make(3, 40, 2, 32, 16, "f32", True, True, 2)
+    x["len"] = torch.tensor([-7, 33, 41], dtype=torch.int32)
+    got = run(kla, x)
+    x["len"] = torch.tensor([0, 33, 40], dtype=torch.int32)
+    want = run(kla, x)
+    check(want, x)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+def test_heads_by_eight_and_a_given_output(kla):
+    """Sequences in groups of eight go to the dies in another order; the output may be the caller's."""
+    x = make(4, 50, 4, 128, 128, "bf16", True, True, 6)
+    check(run(kla, x), x)
+    d = {n: None if u is None else u.to(DEV) for n, u in x.items()}
+    want = kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"])
+    y = torch.full_like(d["v"], math.nan)
+    got = kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"], want_state=False, y=y)
+    assert got["y"] is not None and torch.equal(y, want["y"]) and got["sT"] is None
+    ys = torch.full_like(d["v"][:, 0], math.nan)
+    s = d["s0"].clone()
+    out = kla.kla_linear_attn_step(*(d[n][:, 0].contiguous() for n in ("q", "k", "v")), d["g"], s, y=ys)
+    assert torch.isfinite(ys).all() and torch.equal(out["y"], ys) and out["state"] is s
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_and_small_values(kla, dtype):
+    """States near the ends of fp32's range, fast and slow decays.
+
+    dq is the product of dy and the state: about 1e17 * 1e34 = 1e51 at the large scale, past the 3.4e38 of either
+    type, so the formula itself has no finite value there and the others are checked."""
+    for g in (-0.01, -0.3):
+        for scale in (1e17, 1e-17):
+            x = make(1, 200, 1, 16, 16, dtype, True, False, 3, g)
+            for n in ("k", "v", "dy"):
+                x[n] = x[n] * scale
+            x["s0"], x["ds"] = x["s0"] * scale ** 2, x["ds"] * scale
+            names = ("y", "sT", "dk", "dv", "ds0") if scale > 1 else ("y", "sT", "dq", "dk", "dv", "ds0")
+            check(run(kla, x), x, f"g {g} scale {scale}", names)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at", [1, 45, 98])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_values_that_are_not_finite_stay_in_their_future(kla, dtype, bad):
+def test_values_that_are_not_finite_stay_in_their_future(kla, dtype, bad, at):
     """A bad value at one token leaves the outputs of earlier ones as they are, and in the backward the
     gradients of later ones."""
     clean = make(1, 100, 2, 32, 32, dtype, True, False, 9)
     want = run(kla, clean)
-    at = 45
     for name in ("q", "k", "v", "dy"):
         x = {n: None if u is None else u.clone() for n, u in clean.items()}
         x[name][0, at, 1] = bad
@@ -282,6 +323,32 @@ def test_repeats_bit_for_bit_and_in_a_graph(kla):
         assert all(torch.equal(want[n], out[n]) for n in want), i
         call()
         torch.randn(1 << 20, device=DEV).sum().item()
+
+
+def test_training_step_in_a_graph(kla):
+    """Forward and backward through autograd, captured whole and replayed on new inputs."""
+    x = make(2, 600, 2, 32, 64, "bf16", True, True, 12)
+    d = {n: None if u is None else u.to(DEV) for n, u in x.items()}
+    ins = [d[n].requires_grad_(True) for n in ("q", "k", "v", "s0")]
+
+    def step():
+        y, sT = kla.kla_linear_attn(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"])
+        return (y.detach(), sT.detach(), *torch.autograd.grad([y, sT], ins, [d["dy"], d["ds"]]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        with torch.no_grad():
+            for u in (*ins, d["dy"]):
+                u.add_(0.125 * torch.randn_like(u))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, step())), i
 
 
 def test_refusals(kla):
