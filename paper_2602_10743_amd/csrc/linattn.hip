@@ -803,9 +803,12 @@ hipError_t launch_step(const Shape& s, const void* q, const void* k, const void*
     const unsigned n = (unsigned)((size_t)s.B * s.H);
 #define KLA_STEP(CT_) \
     linattn_step_kernel<E, DK, CT_><<<dim3(n * (unsigned)(s.dv / CT_)), dim3(256), 0, st>>>(s.H, s.dv, q_, k_, v_, g, state, y_)
-    if (s.dv == 128) KLA_STEP(128);
+    // Whole rows of dv = 128, but quarters of them while those are no more than two workgroups a CU (us a step
+    // in quarters and whole, dk = dv = 128: 16 of sequence and head 2.6 and 3.3, 64 3.0 and 3.7, 128 3.8 and 4.2,
+    // 256 5.6 and 5.2, 8192 212 and 207; of dv = 64 halves gain nothing, 2.4 and 2.3).
+    if (s.dv == 128 && n > 128) KLA_STEP(128);
     else if (s.dv == 64) KLA_STEP(64);
-    else if (s.dv == 32) KLA_STEP(32);
+    else if (s.dv >= 32) KLA_STEP(32);
     else KLA_STEP(16);
 #undef KLA_STEP
     return hipGetLastError();

@@ -245,7 +245,7 @@ def test_values_that_are_not_finite_stay_in_their_future(kla, dtype, bad, at):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("S,H,dk,dv", [(1, 1, 16, 16), (1, 16, 128, 128), (5, 3, 32, 64), (4, 2, 64, 32), (3, 2, 128, 16),
-                                       (2, 3, 16, 128)])
+                                       (2, 3, 16, 128), (9, 16, 128, 128)])
 def test_step(kla, S, H, dk, dv, dtype):
     x = make(S, 4, H, dk, dv, dtype, True, False, S + dk)
     ref, mass = expected(x), expected(x, torch.abs)
