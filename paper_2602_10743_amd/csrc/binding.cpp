@@ -8,6 +8,7 @@
 // up the interpreter lock, as ctypes does: allocations and a full launch queue can block, and under
 // KLA_CHECK=1 the library waits for the stream.
 #include <array>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
 #include <vector>
@@ -242,6 +243,20 @@ void check_int(const Opt& t, at::ScalarType type, at::IntArrayRef shape, const T
                     " tensor of shape " + shape_str(shape) + " on " + q.device().str());
 }
 
+// Outputs given by the caller: workgroups read inputs while others write, so the two must not overlap; and
+// autograd is told that their values change, so that a node that saved one refuses its backward.
+void check_apart(const Tensor& out, const char* name, std::initializer_list<const Tensor*> ins) {
+    const char* a = (const char*)out.data_ptr();
+    for (const Tensor* t : ins) {
+        const char* b = (const char*)t->data_ptr();
+        if (a < b + t->nbytes() && b < a + out.nbytes()) value_error(std::string(name) + " must not overlap an input");
+    }
+}
+
+void changed(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int32_t int32_of(int64_t n, const char* what) {
     if (n > INT32_MAX) value_error(std::string(what) + " does not fit 32 bits");
     return (int32_t)n;
@@ -319,12 +334,17 @@ Tensors lin_backward(const kla_desc& d, const Tensor& q, const Tensor& k, const 
 py::object linear_attn_forward(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
                                const Opt& len, const Opt& y_in, bool want_state) {
     const kla_desc d = check_lin(q, k, v, g, s0, len);
-    if (y_in) check_like(*y_in, {d.B, d.T, d.H, d.dv}, q, "y");
+    if (y_in) {
+        check_like(*y_in, {d.B, d.T, d.H, d.dv}, q, "y");
+        check_apart(*y_in, "y", {&q, &k, &v});
+        if (s0) check_apart(*y_in, "y", {&*s0});
+    }
     Tensors out;
     {
         py::gil_scoped_release unlocked;
         out = lin_forward(d, q, k, v, g, s0, len, y_in, want_state);
     }
+    if (y_in) changed(*y_in);
     return py::make_tuple(out[0], obj(some(out[1])));
 }
 
@@ -386,7 +406,11 @@ py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, c
     check_like(v, {S, H, dv}, q, "v");
     check_f32(g, {H}, q, "g");
     check_f32(state, {S, H, dk, dv}, q, "state");
-    if (y_in) check_like(*y_in, {S, H, dv}, q, "y");
+    if (y_in) {
+        check_like(*y_in, {S, H, dv}, q, "y");
+        check_apart(*y_in, "y", {&q, &k, &v, &state});
+    }
+    check_apart(state, "state", {&q, &k, &v});
     const int32_t s32 = int32_of(S, "S"), h32 = int32_of(H, "H"), dk32 = int32_of(dk, "dk"), dv32 = int32_of(dv, "dv");
     Tensor y;
     {
@@ -397,6 +421,8 @@ py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, c
                                 ptr(y), stream_of(q)),
            "kla_linear_attn_step");
     }
+    changed(state);
+    if (y_in) changed(*y_in);
     return py::cast(y);
 }
 

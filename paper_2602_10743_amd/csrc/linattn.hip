@@ -315,8 +315,10 @@ __device__ __forceinline__ void store4(float, const f32x4& y, rsrc_t r, uint32_t
 // e^{g n}, 1 for n = 0 whatever g is.  The exponent is formed in fp64, where g n keeps its digits, and its
 // fraction is an argument of at most 1/2 of the hardware's 2^x (1 ulp): every workgroup begins with these.
 __device__ __forceinline__ float decay_pow(float g, int n) {
-    const double x = fmin(fmax((double)g * (double)n * 1.4426950408889634, -300.0), 300.0), i = rint(x);
-    return n == 0 ? 1.f : ldexpf(__builtin_amdgcn_exp2f((float)(x - i)), (int)i);
+    double x = (double)g * (double)n * 1.4426950408889634;
+    x = x < -300.0 ? -300.0 : x > 300.0 ? 300.0 : x;   // NaN stays
+    const double i = rint(x);
+    return n == 0 ? 1.f : ldexpf(__builtin_amdgcn_exp2f((float)(x - i)), x == x ? (int)i : 0);
 }
 
 __device__ __forceinline__ float lds_val(uint16_t, const unsigned char* p) {
@@ -826,9 +828,10 @@ hipError_t step(const Shape& s, const void* q, const void* k, const void* v, con
 }
 
 // Segments per sequence and chunks in one, for passes of `groups` workgroups where no sequence is cut, to
-// make `want`, or `more` where segments would be longer than 96 chunks.  Segments cost a pass over K and V for their states and two launches more, so a sequence of
-// fewer than 16 chunks is not cut, nor where there is a workgroup for every CU (dk = dv = 128, bf16, B = 8,
-// T = 2048, H = 16, us whole and in two: forward, 256 workgroups, 100 and 135; backward, 768, 196 and 282).
+// make `want`, or `more` where segments would be longer than 96 chunks.  Segments cost a pass over K and V for
+// their states and two launches more, so a sequence of fewer than 16 chunks is not cut, nor where there is a
+// workgroup for every CU (dk = dv = 128, bf16, B = 8, T = 2048, H = 16, us whole and in two: forward, 256
+// workgroups, 100 and 135; backward, 768, 196 and 282).
 // Otherwise the forward makes two workgroups a CU and the backward, whose passes share their reads,
 // three (us in 4, 8, 16, 24 segments, B = 1, T = 16384, H = 16, forward 295, 158, 117, 119, backward 381,
 // 282, 277, 294; B = 4, T = 4096, H = 8, forward 88, 71, 73, 80, backward 147, 147, 168, 196), but none

@@ -186,6 +186,26 @@ def test_repeats_bit_for_bit_and_in_a_graph(kla):
         torch.randn(1 << 20, device=DEV).sum().item()
 
 
+def test_past_32_bits(kla):
+    """More than 2^31 elements: rows are independent, so copies of a block give copies of its results."""
+    n, rows, copies = 16384, 1000, 135
+    x, w, b, dy = make(rows, n, "bf16", True, 9)
+    out, mean, rstd = kla.kla_layer_norm_forward(x, w, b)
+    dx, dw, db = kla.kla_layer_norm_backward(x, w, mean, rstd, dy)
+    X, DY = x.repeat(copies, 1), dy.repeat(copies, 1)
+    assert X.numel() > 2 ** 31
+    OUT, MEAN, RSTD = kla.kla_layer_norm_forward(X, w, b)
+    DX, DW, DB = kla.kla_layer_norm_backward(X, w, MEAN, RSTD, DY)
+    torch.cuda.synchronize()
+    for big, small in ((OUT, out), (MEAN, mean), (RSTD, rstd), (DX, dx)):
+        assert (big.view(copies, *small.shape) == small).all()
+    # both sums are off by at most 2^-24 of the terms' size for each of the additions in a row
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    for big, small, size in ((DW, dw, (dy.double() * xh).abs().sum(0)), (DB, db, dy.double().abs().sum(0))):
+        off = (copies * rows / 256 + 64) * 2.0 ** -24 * copies * size
+        assert ((big.double() - copies * small.double()).abs() <= 2 * off).all()
+
+
 def test_refusals(kla):
     x, w, b, dy = make(4, 32, "f32", True, 8)
     with pytest.raises(ValueError, match="x must be contiguous"):

@@ -351,6 +351,100 @@ def test_training_step_in_a_graph(kla):
         assert all(torch.equal(a, b) for a, b in zip(out, step())), i
 
 
+def test_past_32_bits(kla):
+    """More than 2^31 elements, in the batch and along one sequence whose states forget all but the last 100 tokens."""
+    x = make(8, 2048, 16, 128, 128, "bf16", False, True, 5)
+    small = run(kla, x)
+    copies = 66
+    big = run(kla, {n: None if u is None else u if n == "g" else u.to(DEV).repeat(copies, *[1] * (u.dim() - 1)) for n, u in x.items()})
+    assert big["y"].numel() > 2 ** 31
+    for n in ("y", "sT", "dq", "dk", "dv"):
+        assert (big[n].view(copies, *small[n].shape) == small[n]).all(), n
+    del big
+    H, T, last = 128, 132000, 320
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    z = lambda: torch.randn(1, T, H, 128, generator=gen, device=DEV, dtype=torch.bfloat16)
+    x = dict(q=z(), k=z(), v=z(), dy=z(), g=torch.full((H,), -1.0), s0=None, ds=None, len=None)
+    assert x["q"].numel() > 2 ** 31
+    got = run(kla, x)
+    heads = [0, H - 1]
+    end = {n: x[n][:, -last:, heads].cpu() for n in ("q", "k", "v", "dy")}
+    end.update(g=x["g"][heads], s0=None, ds=None, len=None)
+    # y and dq of the last tokens, which the tokens before `last` reach by e^-128 at most, under fp32's smallest
+    tail = {n: got[n][:, -last:, heads].cpu() for n in ("y", "dq", "dk", "dv")}
+    ref, mass = expected(end), expected(end, torch.abs)
+    for n, at in (("y", 128), ("dq", 128), ("dk", 0), ("dv", 0)):
+        a, r, m = (u[:, at:] for u in (tail[n].double(), ref[n], mass[n]))
+        tol = (128 + 64 + 4 * 11) * 2.0 ** -24 * m + 2.0 ** -8 * r.abs() + 2 * 2.0 ** -16 * m + 1e-30
+        assert ((a - r).abs() <= tol).all(), n
+
+
+@pytest.mark.parametrize("T", [40, 700])
+def test_a_decay_that_is_no_number(kla, T):
+    """Its head has no value; the others keep theirs."""
+    x = make(2, T, 2, 32, 32, "f32", True, False, 15)
+    want = run(kla, x)
+    x["g"] = torch.tensor([math.nan, x["g"][1]])
+    got = run(kla, x)
+    for n in ("y", "sT", "dq", "dk", "dv", "ds0"):
+        head = (lambda u, h: u[:, :, h]) if n in ("y", "dq", "dk", "dv") else lambda u, h: u[:, h]
+        assert torch.equal(head(got[n], 1), head(want[n], 1)), n
+    assert torch.isnan(got["sT"][:, 0]).all() and torch.isnan(got["y"][:, 1:, 0]).all()
+    d = {n: None if u is None else u.to(DEV) for n, u in x.items()}
+    out = kla.kla_linear_attn_step(*(d[n][:, 0].contiguous() for n in ("q", "k", "v")), d["g"], d["s0"])
+    assert torch.isnan(out["y"][:, 0]).all() and torch.isfinite(out["y"][:, 1]).all()
+
+
+def test_outputs_apart_from_inputs(kla):
+    """An output that overlaps an input is refused, and a state that a backward saved is known to have changed."""
+    x = make(2, 8, 2, 16, 16, "f32", True, False, 1)
+    d = {n: None if u is None else u.to(DEV) for n, u in x.items()}
+    one = [d[n][:, 0].contiguous() for n in ("q", "k", "v")]
+    for n in ("q", "k", "v"):
+        with pytest.raises(ValueError, match="y must not overlap"):
+            kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], d["g"], d["s0"], y=d[n])
+    for u in one:
+        with pytest.raises(ValueError, match="y must not overlap"):
+            kla.kla_linear_attn_step(*one, d["g"], d["s0"], y=u)
+    with pytest.raises(ValueError, match="state must not overlap"):
+        kla.kla_linear_attn_step(d["s0"].view(-1)[:64].view(2, 2, 16), *one[1:], d["g"], d["s0"])
+    y, sT = kla.kla_linear_attn(d["q"].requires_grad_(True), d["k"], d["v"], d["g"], d["s0"])
+    kla.kla_linear_attn_step(*one, d["g"], d["s0"])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with torch.inference_mode():
+        kla.kla_linear_attn_step(*one, d["g"], torch.zeros_like(d["s0"]))
+
+
+def test_threads(kla):
+    """Two threads, each on a stream of its own, give what one gives."""
+    import threading
+    xs = [make(2, 600, 2, 64, 64, "bf16", True, True, 30 + i) for i in range(2)]
+    want = [run(kla, x) for x in xs]
+    got = [[], []]
+
+    def work(i):
+        d = {n: None if u is None else u.to(DEV) for n, u in xs[i].items()}
+        ins = [d[n].requires_grad_(True) for n in ("q", "k", "v", "s0")]
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                y, sT = kla.kla_linear_attn(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"])
+                grads = torch.autograd.grad([y, sT], ins, [d["dy"], d["ds"]])
+                got[i].append(dict(zip(("y", "sT", "dq", "dk", "dv", "ds0"), (y, sT, *grads))))
+            stream.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        assert len(got[i]) == 10
+        for out in got[i]:
+            assert all(torch.equal(out[n], want[i][n]) for n in out)
+
+
 def test_refusals(kla):
     x = make(2, 8, 2, 32, 16, "f32", True, False, 1)
     d = {n: None if u is None else u.to(DEV) for n, u in x.items()}

@@ -278,6 +278,24 @@ def test_repeats_bit_for_bit_and_in_a_graph(kla):
             torch.randn(1 << 20, device=DEV).sum().item()
 
 
+def test_past_32_bits(kla):
+    """More than 2^31 logits: rows are independent, so copies of a block give copies of its results."""
+    rows, V, copies = 1000, 131072, 17
+    x, target = make((rows,), V, "bf16", 9)
+
+    def call(x, target, rep):
+        out = kla.kla_token_logp_forward(x, target, want_entropy=True, top=5, save=True)
+        d = torch.linspace(-1, 1, rows, device=DEV).repeat(rep)
+        return (*out.values(), kla.kla_token_logp_backward(x, target, out["stat"], out["entropy"], d, -d))
+    small = call(x, target, 1)
+    X = x.repeat(copies, 1)
+    assert X.numel() > 2 ** 31
+    big = call(X, target.repeat(copies), copies)
+    torch.cuda.synchronize()
+    for a, b in zip(big, small):
+        assert (a.view(copies, *b.shape) == b).all()
+
+
 def test_refusals(kla):
     x, target = make((2, 4), 50, "f32", 14)
     with pytest.raises(ValueError, match="target has shape"):
