@@ -441,7 +441,7 @@ kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const fl
  * needs no saved context: it returns dq, dk [B, T, H, dk] and dv [B, T, H, dv] (dtype,
  * required) and ds0 [B, H, dk, dv] (fp32 or NULL) from dy [B, T, H, dv] and dsT
  * [B, H, dk, dv] fp32 (NULL: zero).  The step takes one token for S sequences and updates
- * state [S, H, dk, dv] in place.  H max(dk, dv) <= 2^24, B H (S H) <= 2^21 and T <= 2^30.
+ * state [S, H, dk, dv] in place.  H max(dk, dv) <= 2^24, B H (S H) <= 2^20 and T <= 2^30.
  */
 size_t kla_linear_attn_workspace(const kla_desc* desc);
 size_t kla_linear_attn_backward_workspace(const kla_desc* desc);

@@ -713,7 +713,7 @@ kla_status lin_desc(const kla_desc* d) {
     const kla_status st = check_desc(d);
     if (st != KLA_OK) return st;
     const int w = d->dk > d->dv ? d->dk : d->dv;
-    return (int64_t)d->H * w > (1 << 24) || d->T > (1 << 30) || (int64_t)d->B * d->H > (1 << 21) ? KLA_ERR_SHAPE : KLA_OK;
+    return (int64_t)d->H * w > (1 << 24) || d->T > (1 << 30) || (int64_t)d->B * d->H > (1 << 20) ? KLA_ERR_SHAPE : KLA_OK;
 }
 
 // KLA_CHECK=1: g <= 0 for every head (synchronous).

@@ -12,7 +12,8 @@
 // (o = 0): the gradient of the final state enters undecayed, and the last R is the gradient of the
 // start state.  All exponents are at least 0, so no factor exceeds 1 for g <= 0; e^{-inf * 0} is 1.
 //
-// A wave owns CW value columns of one sequence (or segment of one) and their state, in registers;
+// A wave owns CW value columns of one sequence (or segment of one) and their state, in registers, or half of
+// the state's rows, and then, the sums over the rows exchanged, the outputs of half of the chunk's tokens;
 // the waves of a workgroup share the chunk's Q, K and V in LDS, loaded a chunk ahead.  Accumulators are
 // operands as they stand: over tokens, lane group g holds {4g .. 4g+3} u {16+4g .. 16+4g+3} of a 32-deep
 // product, and the 32 rows of two tiles of the state are dealt so that g holds 8g .. 8g+7 (slot_of),
@@ -383,35 +384,41 @@ __device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_
                  : "memory");
 }
 
-// A workgroup takes DT of the D columns, a wave CW of them.  Where the rows of Q and K are long and the waves
-// that compute (NCW) few, others help with the loads.  64 columns in waves of 16 leave 168 registers and 53 KiB of
-// LDS, so three workgroups of 128-wide bf16 passes share a CU (B = 8, T = 2048, H = 16: forward 100 us and
-// backward 196, against 139 and 226 with 128 columns in waves of 32, whose scores are formed half as
-// often but which one or two waves a SIMD have to hide).  The states' pass forms no scores: all columns.
-template <typename E, int N, int D, bool NOY>
+// A workgroup takes DT of the D columns, a wave CW of them and one of RS shares of the state's rows.  Where the
+// rows of Q and K are long and the waves that compute (NCW RS) few, others help with the loads.  64 columns in
+// waves of 16 with all rows take 132 registers and 43 KiB of LDS, so three workgroups of 128-wide bf16 passes
+// share a CU (B = 8, T = 2048, H = 16: forward 100 us and backward 196, against 139 and 226 with 128 columns
+// in waves of 32, whose scores are formed half as often but which one or two waves a SIMD have to hide).  The
+// states' pass forms no scores: all columns.
+template <typename E, int N, int D, bool NOY, int RS>
 struct LinCfg {
     static constexpr int CW = NOY && D == 128 ? 32 : 16, DT = NOY || D <= 64 ? D : 64, NTILE = D / DT, NCW = DT / CW;
-    static constexpr int ROW = N * (int)sizeof(E), LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1, NW = NCW > LW ? NCW : LW;
-    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES, LDS = 2 * BUF + 2 * kLC * (int)sizeof(float) + 3 * 1024;
-    // waves per SIMD: fp32 states and operands of 128 slots need more than the registers of three
-    static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : 3;
+    static constexpr int ROW = N * (int)sizeof(E), LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1,
+                         NW = NCW * RS > LW ? NCW * RS : LW;
+    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES,
+                         LDS = 2 * BUF + 2 * kLC * (int)sizeof(float) + 3 * 1024 + (RS > 1 ? NCW * RS * (CW / 16) * 1024 : 0);
+    // waves per SIMD: of fp32 rows of 128 slots, LDS holds one workgroup a CU
+    static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : RS > 1 ? 4 : 3;
 };
 
-template <typename E, int N, int D, bool NOY>
-__global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, NOY>::OCC)) void linattn_kernel(LinArgs a) {
-    using Cfg = LinCfg<E, N, D, NOY>;
-    constexpr int CW = Cfg::CW, NW = Cfg::NW, NDT = CW / 16, NRT = N / 16, KS = (N + 31) / 32;
+template <typename E, int N, int D, bool NOY, int RS>
+__global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64), (LinCfg<E, N, D, NOY, RS>::OCC)) void linattn_kernel(LinArgs a) {
+    using Cfg = LinCfg<E, N, D, NOY, RS>;
+    constexpr int CW = Cfg::CW, NW = Cfg::NW, NDT = CW / 16;
+    // a wave's tiles of state rows, steps over them, tiles of tokens
+    constexpr int NRT = N / 16 / RS, KS = (N + 31) / 32 / RS, NIT = 2 / RS;
     constexpr int ES = (int)sizeof(E);
     using TQ = Tile<E, N>;
     constexpr int DT = Cfg::DT, NTILE = Cfg::NTILE;
     using TV = Tile<E, DT>;
     constexpr int UQ = NOY ? 0 : TQ::UNITS, UK = TQ::UNITS, UNITS = UQ + UK + TV::UNITS;
     constexpr int NL = (UNITS + NW - 1) / NW;   // a wave's loads per chunk
-    constexpr int NST = NOY ? 0 : 2 * NDT;      // and stores, of one that computes
+    constexpr int NST = NOY ? 0 : NIT * NDT;      // and stores, of one that computes
     constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
     float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
     uint4* scores = reinterpret_cast<uint4*>(pw + 2 * kLC);   // of the chunk, three tiles
+    f32x4* part = reinterpret_cast<f32x4*>(scores + 3 * 64);  // of Q R, for the wave with the other rows
 
     int vi, ji, tile;   // the passes and tiles of one sequence on one XCD: they read the same rows
     {
@@ -431,8 +438,9 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
     const int Tb = __builtin_amdgcn_readfirstlane(seq_len(a, b));
     const int u0 = seg * a.lc * kLC, nu = min(max(Tb - u0, 0), a.lc * kLC);   // this segment's tokens, in walk order
     const int nchunk = (nu + kLC - 1) / kLC;
-    const int dl0 = wave * CW, dm0 = tile * DT + dl0;   // the wave's first column, in the tile and of all
-    const bool works = NW == Cfg::NCW || wave < Cfg::NCW;
+    const int sh = RS == 1 ? 0 : wave / Cfg::NCW % 2;   // its share of the state's rows, and of the outputs' tokens
+    const int dl0 = (RS == 1 ? wave : wave % Cfg::NCW) * CW, dm0 = tile * DT + dl0;   // first column, in the tile and of all
+    const bool works = NW == Cfg::NCW * RS || wave < Cfg::NCW * RS;
 
     if (threadIdx.x < 2 * kLC) pw[threadIdx.x] = decay_pow(g, threadIdx.x);
 
@@ -464,7 +472,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
 
     // Wave load i: 64 pieces of Q, K or V; which, is known at compile time where the tiles are whole rounds
     // of the workgroup's loads.
-    constexpr bool EVEN = UQ % NW == 0 && UK % NW == 0 && UNITS % NW == 0;
+    constexpr bool EVEN = UQ % NW == 0 && UK % NW == 0, FULL = UNITS % NW == 0;
     auto part_of = [&](int i) { return EVEN ? i * NW : i * NW + wave; };
     uint32_t goff[NL];   // in a full chunk; the piece that belongs at the lane's place in the tile
 #pragma unroll
@@ -496,16 +504,16 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
                 load_lds(rq, dst + i * NW * 1024, goff[i] - hn);
             else if (part_of(i) < UQ + UK)
                 load_lds(rk, dst + i * NW * 1024, goff[i] - hn);
-            else if (part_of(i) < UNITS)
+            else if (FULL || i * NW + wave < UNITS)
                 load_lds(rv, dst + i * NW * 1024, goff[i] - hd);
         }
     };
 
-    // state R[n, d], n = slot_of(rt, 4 g4 + rr), d = dm0 + 16 dt + l16
+    // state R[n, d], n = slot_of(sh NRT + rt, 4 g4 + rr), d = dm0 + 16 dt + l16
     const size_t srow = (size_t)bh * a.ns + seg;
     f32x4 R[NRT][NDT];
     auto state_at = [&](int rt, int dt, int rr, bool flip) {
-        const int n = slot_of<N>(rt, 4 * g4 + rr), d = dm0 + 16 * dt + l16;
+        const int n = slot_of<N>(sh * NRT + rt, 4 * g4 + rr), d = dm0 + 16 * dt + l16;
         return flip ? d * N + n : n * D + d;
     };
     if (nchunk > 0) load(0);
@@ -519,21 +527,25 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
                 for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] = s0 ? s0[state_at(rt, dt, rr, job.flip & 1)] : 0.f;
     }
     __syncthreads();   // pw
-    float dia[4], off[4], rd[2], kw[8];
+    float dia[4], off[4], rd[NIT], kw[8];
 #pragma unroll
     for (int rr = 0; rr < 4; ++rr) {
         const int lag = l16 - 4 * g4 - rr;
         dia[rr] = lag >= 0 ? pw[max(lag, 0)] : 0.f;
         off[rr] = pw[16 + lag];
     }
-    rd[0] = pw[l16 + O];
-    rd[1] = pw[16 + l16 + O];
+    uint32_t yoff[NIT];
+#pragma unroll
+    for (int it = 0; it < NIT; ++it) {
+        const int i = 16 * (sh + it) + l16;
+        rd[it] = pw[i + O];
+        yoff[it] = row_off(i, sd) + (uint32_t)(4 * g4 * ES);
+    }
     auto weights = [&](int n) {   // of the state's update; values past the chunk's tokens are zero
 #pragma unroll
         for (int e = 0; e < 8; ++e) kw[e] = pw[max(n - O - (4 * g4 + (e & 3) + (e & 4) * 4), 0)];
     };
     const typename Acc<E>::Pick pick(g4, l16);
-    const uint32_t yoff[2] = {row_off(l16, sd) + (uint32_t)(4 * g4 * ES), row_off(16 + l16, sd) + (uint32_t)(4 * g4 * ES)};
     weights(kLC);
     // The state is rho R, so that its decay is one product a chunk and not one an element, until rho is under
     // 2^-8 (which leaves R all but 8 of the exponents).  Uniform: the branches on them are the wave's.
@@ -573,7 +585,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             for (int t = wave; t < 3; t += NW) {
                 f32x4 s = zero4();
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
+                for (int ks = 0; ks < KS * RS; ++ks)
                     s = mma<ST>(Op<E>::template row<N>(sK, (t == 2 ? 16 : 0) + l16, ks, g4),
                                 Op<E>::template row<N>(sQ, (t > 0 ? 16 : 0) + l16, ks, g4), s);
 #pragma unroll
@@ -592,13 +604,20 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
                 for (int dt = 0; dt < NDT; ++dt) y[dt][0] = y[dt][1] = zero4();
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const Op<E> qs[2] = {Op<E>::template row<N>(sQ, l16, ks, g4), Op<E>::template row<N>(sQ, 16 + l16, ks, g4)};
+                    const Op<E> qs[2] = {Op<E>::template row<N>(sQ, l16, sh * KS + ks, g4),
+                                         Op<E>::template row<N>(sQ, 16 + l16, sh * KS + ks, g4)};
                     Acc<E> r[NDT];
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt)
                         r[dt] = Acc<E>::template from<N == 16>(R[2 * ks][dt], N == 16 ? zero4() : R[N == 16 ? 0 : 2 * ks + 1][dt], pick);
                     mma_each<ST>(r, qs, y);
                 }
+                if constexpr (RS > 1)
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt) {
+                        part[(wave * NDT + dt) * 64 + lane] = sh ? y[dt][0] : y[dt][1];
+                        if (sh) y[dt][0] = y[dt][1];
+                    }
             }
 
             // R <- e^{g n} R + K^T (w V)
@@ -621,7 +640,7 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             for (int rt = 0; rt < NRT; rt += RT) {
                 Op<E> kt[RT];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) kt[i] = Op<E>::template slots<N>(sK, rt + i, g4, l16);
+                for (int i = 0; i < RT; ++i) kt[i] = Op<E>::template slots<N>(sK, sh * NRT + rt + i, g4, l16);
                 mma_each<RT, NDT>(kt, vs, R + rt);
             }
         }
@@ -629,27 +648,37 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY>::NW * 64), (LinCfg<E, N, D, N
             __syncthreads();   // the scores are there
             if (works) {
                 const uint4 none{0u, 0u, 0u, 0u};
-                const Acc<E> p0 = Acc<E>::of(scores[lane], none), p1 = Acc<E>::of(scores[64 + lane], scores[128 + lane]);
-                f32x4 in[NDT][2];
+                f32x4 in[NDT][NIT];
                 float sum = 0.f;   // not finite where a value is not
 #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt) {
-                    in[dt][0] = mma<4>(vf[dt], p0, zero4());
-                    in[dt][1] = mma<8>(vf[dt], p1, zero4());
+                for (int it = 0; it < NIT; ++it) {
+                    const int at = RS > 1 ? sh : it;   // one tile of earlier tokens, or two
+                    const Acc<E> p = at ? Acc<E>::of(scores[64 + lane], scores[128 + lane]) : Acc<E>::of(scores[lane], none);
 #pragma unroll
-                    for (int rr = 0; rr < 4; ++rr) sum += in[dt][0][rr] + in[dt][1][rr];
+                    for (int dt = 0; dt < NDT; ++dt) {
+                        in[dt][it] = RS > 1 || it ? mma<8>(vf[dt], p, zero4()) : mma<4>(vf[dt], p, zero4());
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) sum += in[dt][it][rr];
+                    }
                 }
                 if (__any(!(fabsf(sum) <= 3.4e38f)))
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-                        for (int it = 0; it < 2; ++it)
-                            in[dt][it] = masked_sums<E, N, DT>(sQ, sK, sV, pw, dl0 + 16 * dt, 16 * it + l16, g4);
+                        for (int it = 0; it < NIT; ++it)
+                            in[dt][it] = masked_sums<E, N, DT>(sQ, sK, sV, pw, dl0 + 16 * dt, 16 * (sh + it) + l16, g4);
+                if constexpr (RS > 1)
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt) {
+                        const f32x4 other = part[((wave ^ Cfg::NCW) * NDT + dt) * 64 + lane];
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) y[dt][0][rr] += other[rr];
+                    }
                 const rsrc_t ry = rsrc_of(py, sd, n, CW * ES);
                 const uint32_t hd = shift_of(sd, n);
                 py += step_d;
 #pragma unroll
-                for (int it = 0; it < 2; ++it) {
+                for (int it = 0; it < NIT; ++it) {
                     const uint32_t to = yoff[it] - hd;
                     const float f = rd[it] * was;
 #pragma unroll
@@ -710,10 +739,10 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int
     }
 }
 
-template <typename E, int N, int D, bool NOY>
+template <typename E, int N, int D, bool NOY, int RS = 1>
 hipError_t launch(const LinArgs& a, hipStream_t st) {
-    using Cfg = LinCfg<E, N, D, NOY>;
-    auto kern = linattn_kernel<E, N, D, NOY>;
+    using Cfg = LinCfg<E, N, D, NOY, RS>;
+    auto kern = linattn_kernel<E, N, D, NOY, RS>;
     if constexpr (Cfg::LDS > 64 * 1024) {   // must be opted into, once per kernel and device
         static std::atomic<uint64_t> done{0};
         int dev = 0;
@@ -731,10 +760,25 @@ hipError_t launch(const LinArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// One or two waves for a column group's state rows.  Two shorten the chain of a chunk's products and fill the
+// SIMDs where there are few workgroups, but both convert V.  128 rows, dk = dv = 128, T = 2048, H = 16, us with
+// one and two: bf16, forward of B = 8 (256 workgroups) 113 and 98, backward of B = 4 (384) 136 and 130, forward
+// of B = 16 (512) 141 and 160, backward of B = 8 (768) 215 and 233; fp32, whose LDS holds one workgroup a CU,
+// forward 246 and 228, backward 735 and 676.  Of 64 rows two waves win nothing (B = 16, dv = 64, forward 72 and
+// 71, backward 160 and 173).
+template <typename E, int N, int D>
+hipError_t run_rows(const LinArgs& a, hipStream_t st) {
+    if constexpr (N == 128) {
+        const size_t groups = (size_t)a.B * a.H * a.run * a.jobs * LinCfg<E, N, D, false, 1>::NTILE;
+        if (groups <= 384) return launch<E, N, D, false, 2>(a, st);
+    }
+    return launch<E, N, D, false, N == 128 && sizeof(E) == 4 ? 2 : 1>(a, st);
+}
+
 template <typename E>
 hipError_t run(const LinArgs& a, int N, int D, bool noy, hipStream_t st) {
 #define KLA_LIN(N_, D_) \
-    if (N == N_ && D == D_) return noy ? launch<E, N_, D_, true>(a, st) : launch<E, N_, D_, false>(a, st);
+    if (N == N_ && D == D_) return noy ? launch<E, N_, D_, true>(a, st) : run_rows<E, N_, D_>(a, st);
 #define KLA_LIN_ROW(N_) KLA_LIN(N_, 16) KLA_LIN(N_, 32) KLA_LIN(N_, 64) KLA_LIN(N_, 128)
     KLA_LIN_ROW(16) KLA_LIN_ROW(32) KLA_LIN_ROW(64) KLA_LIN_ROW(128)
 #undef KLA_LIN_ROW

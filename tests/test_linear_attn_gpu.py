@@ -120,7 +120,7 @@ def test_reference_against_differences():
         assert abs((up - down) / (2 * h) - (got[grad] * way).sum()) < 1e-6
 
 
-WIDTHS = [(16, 16), (16, 128), (32, 32), (32, 64), (64, 16), (64, 128), (128, 32), (128, 128)]
+WIDTHS = [(16, 16), (16, 128), (32, 32), (32, 64), (64, 16), (64, 128), (128, 16), (128, 32), (128, 64), (128, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -134,6 +134,14 @@ def test_widths(kla, dk, dv, dtype):
 @pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 97])
 def test_lengths(kla, T, dtype):
     x = make(2, T, 2, 32, 32, dtype, T % 2 == 0, False, T)
+    check(run(kla, x), x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T", [(2, 1), (2, 15), (2, 17), (2, 32), (2, 97), (70, 1), (70, 40)])
+def test_wide_rows_in_few_and_many_sequences(kla, B, T, dtype):
+    """The rows of a state 128 wide are one wave's or two's, by the number of workgroups."""
+    x = make(B, T, 3, 128, 128, dtype, True, True, B + T)
     check(run(kla, x), x)
 
 
@@ -222,11 +230,11 @@ def test_large_and_small_values(kla, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("at", [1, 45, 98])
-@pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_values_that_are_not_finite_stay_in_their_future(kla, dtype, bad, at):
+@pytest.mark.parametrize("bad,width", [(math.nan, 32), (math.inf, 32), (math.nan, 128), (math.inf, 128)])
+def test_values_that_are_not_finite_stay_in_their_future(kla, dtype, bad, width, at):
     """A bad value at one token leaves the outputs of earlier ones as they are, and in the backward the
     gradients of later ones."""
-    clean = make(1, 100, 2, 32, 32, dtype, True, False, 9)
+    clean = make(1, 100, 2, width, width, dtype, True, False, 9)
     want = run(kla, clean)
     for name in ("q", "k", "v", "dy"):
         x = {n: None if u is None else u.clone() for n, u in clean.items()}
@@ -353,9 +361,9 @@ def test_training_step_in_a_graph(kla):
 
 def test_past_32_bits(kla):
     """More than 2^31 elements, in the batch and along one sequence whose states forget all but the last 100 tokens."""
-    x = make(8, 2048, 16, 128, 128, "bf16", False, True, 5)
+    x = make(16, 2048, 16, 128, 128, "bf16", False, True, 5)
     small = run(kla, x)
-    copies = 66
+    copies = 33
     big = run(kla, {n: None if u is None else u if n == "g" else u.to(DEV).repeat(copies, *[1] * (u.dim() - 1)) for n, u in x.items()})
     assert big["y"].numel() > 2 ** 31
     for n in ("y", "sT", "dq", "dk", "dv"):

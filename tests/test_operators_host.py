@@ -45,7 +45,7 @@ def test_linear_attn(lib):
     fwd = lambda d, a, n=0: lib.kla_linear_attn_forward(d, *a, n, None)
     assert fwd(desc(dk=24), ok) == 2 and fwd(desc(B=0), ok) == 2 and fwd(desc(T=-1), ok) == 2
     assert fwd(desc(H=1 << 24, dk=32), ok) == 2           # row offsets of a chunk past 32 bits
-    assert fwd(desc(B=1 << 20, H=4), ok) == 2             # a launch's threads past 32 bits
+    assert fwd(desc(B=(1 << 20) + 1, H=1), ok) == 2       # a launch's threads past 32 bits
     assert fwd(desc(dtype=3), ok) == 3 and fwd(None, ok) == 1
     for i in (0, 1, 2, 3, 6):
         assert fwd(desc(), put(ok, i, None)) == 1, i
