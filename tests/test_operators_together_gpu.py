@@ -96,3 +96,34 @@ def test_training_step_and_serving():
     want = torch.sort(logits, dim=-1, descending=True, stable=True).indices[:, :5]
     assert torch.equal(got["top_index"], want)
     assert torch.allclose(got["top_logp"], torch.log_softmax(logits.double(), -1).gather(1, want).float(), atol=1e-5)
+
+
+def test_captured_backward_beside_an_eager_graph():
+    """Refused while a graph of the same leaves lives that the default stream made; right once it is gone."""
+    import paper_2602_10743_amd as kla
+    z = lambda *s: torch.randn(*s, device=DEV)
+    g = torch.tensor([-0.1, -0.01], device=DEV)
+    q, k, v, x, w, b, logits = (z(*s).requires_grad_(True) for s in ((2, 40, 2, 32), (2, 40, 2, 32), (2, 40, 2, 32), (50, 64),
+                                                                    (64,), (64,), (50, 100)))
+    target = torch.randint(0, 100, (50,), device=DEV)
+    for call, ins in ((lambda: kla.kla_linear_attn(q, k, v, g)[0], (q, k, v)), (lambda: kla.kla_layer_norm(x, w, b), (x, w, b)),
+                      (lambda: kla.kla_token_logp(logits, target), (logits,))):
+        alive = call()
+        up = torch.randn_like(alive)
+        want = torch.autograd.grad(alive, ins, up, retain_graph=True)
+        torch.cuda.synchronize()
+        with pytest.raises(RuntimeError, match="drop its outputs first"):
+            with torch.cuda.graph(torch.cuda.CUDAGraph()):
+                torch.autograd.grad(call(), ins, up)
+        torch.cuda.synchronize()
+        del alive
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = torch.autograd.grad(call(), ins, up)
+        for _ in range(3):
+            for u in got:
+                u.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(map(torch.equal, got, want))
+            call()
