@@ -401,10 +401,11 @@ struct LinCfg {
     static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : RS > 1 ? 4 : 3;
 };
 
-template <typename E, int N, int D, bool NOY, int RS>
-__global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64), (LinCfg<E, N, D, NOY, RS>::OCC)) void linattn_kernel(LinArgs a) {
+// Workgroup `block` of `jobs` passes from job[j0] on; NW: its waves.
+template <typename E, int N, int D, bool NOY, int RS, int NW>
+__device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0, int jobs) {
     using Cfg = LinCfg<E, N, D, NOY, RS>;
-    constexpr int CW = Cfg::CW, NW = Cfg::NW, NDT = CW / 16;
+    constexpr int CW = Cfg::CW, NDT = CW / 16;
     // a wave's tiles of state rows, steps over them, tiles of tokens
     constexpr int NRT = N / 16 / RS, KS = (N + 31) / 32 / RS, NIT = 2 / RS;
     constexpr int ES = (int)sizeof(E);
@@ -422,10 +423,10 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64), (LinCfg<E, N, 
 
     int vi, ji, tile;   // the passes and tiles of one sequence on one XCD: they read the same rows
     {
-        const int i = blockIdx.x, nv = a.B * a.H * a.run, each = a.jobs * NTILE;
+        const int i = block, nv = a.B * a.H * a.run, each = jobs * NTILE;
         const int slot = nv % 8 == 0 ? i / 8 : i;
         vi = nv % 8 == 0 ? slot / each * 8 + i % 8 : slot / each;
-        ji = slot % each / NTILE;
+        ji = j0 + slot % each / NTILE;
         tile = slot % NTILE;
     }
     const LinJob job = a.job[ji];
@@ -712,6 +713,32 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64), (LinCfg<E, N, 
     }
 }
 
+template <typename E, int N, int D, bool NOY, int RS>
+__global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64),
+                             (LinCfg<E, N, D, NOY, RS>::OCC)) void linattn_kernel(LinArgs a) {
+    linattn_pass<E, N, D, NOY, RS, LinCfg<E, N, D, NOY, RS>::NW>(a, blockIdx.x, 0, a.jobs);
+}
+
+// A backward with dk != dv: two passes with N = dv, D = dk and one the other way round in one launch, R0 and R1
+// waves for their state rows.  Side by side they fill what each leaves idle (us in two launches and in one, dk/dv:
+// bf16, B = 8, T = 2048, H = 16, 64/128 155 and 130, 128/64 176 and 159; B = 16, T = 512, 16/64 40 and 24; B = 3,
+// T = 777, H = 5, 64/128 37 and 32; fp32, B = 8, T = 1024, H = 16, 32/64 122 and 91, 64/128 190 and 190).
+template <typename E, int N, int D, int R0, int R1>
+struct PairCfg {
+    using A = LinCfg<E, N, D, false, R0>;
+    using B = LinCfg<E, D, N, false, R1>;
+    static constexpr int NW = A::NW > B::NW ? A::NW : B::NW, LDS = A::LDS > B::LDS ? A::LDS : B::LDS,
+                         OCC = A::OCC < B::OCC ? A::OCC : B::OCC;
+};
+template <typename E, int N, int D, int R0, int R1>
+__global__ __launch_bounds__((PairCfg<E, N, D, R0, R1>::NW * 64),
+                             (PairCfg<E, N, D, R0, R1>::OCC)) void linattn_pair_kernel(LinArgs a) {
+    using Cfg = PairCfg<E, N, D, R0, R1>;
+    const int two = a.B * a.H * a.run * 2 * Cfg::A::NTILE;
+    if ((int)blockIdx.x < two) linattn_pass<E, N, D, false, R0, Cfg::NW>(a, blockIdx.x, 0, 2);
+    else linattn_pass<E, D, N, false, R1, Cfg::NW>(a, blockIdx.x - two, 2, 1);
+}
+
 // Start states of the segments from their own end states, in place: a workgroup takes 256 elements of
 // one sequence's state through its segments.  job.k: the states before the first segments.
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int D) {
@@ -739,25 +766,36 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinArgs a, int N, int
     }
 }
 
-template <typename E, int N, int D, bool NOY, int RS = 1>
-hipError_t launch(const LinArgs& a, hipStream_t st) {
-    using Cfg = LinCfg<E, N, D, NOY, RS>;
-    auto kern = linattn_kernel<E, N, D, NOY, RS>;
-    if constexpr (Cfg::LDS > 64 * 1024) {   // must be opted into, once per kernel and device
+template <auto KERN, int LDS>
+hipError_t launch_kernel(const LinArgs& a, size_t grid, int threads, hipStream_t st) {
+    if constexpr (LDS > 64 * 1024) {   // must be opted into, once per kernel and device
         static std::atomic<uint64_t> done{0};
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
         const uint64_t bit = 1ull << (dev & 63);
         if (!(done.load() & bit)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS);
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERN), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
             if (e != hipSuccess) return e;
             done.fetch_or(bit);
         }
     }
-    const size_t grid = (size_t)a.B * a.H * a.run * a.jobs * Cfg::NTILE;
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(Cfg::NW * 64), Cfg::LDS, st, a);
+    hipLaunchKernelGGL(KERN, dim3((unsigned)grid), dim3(threads), LDS, st, a);
     return hipGetLastError();
+}
+
+template <typename E, int N, int D, bool NOY, int RS = 1>
+hipError_t launch(const LinArgs& a, hipStream_t st) {
+    using Cfg = LinCfg<E, N, D, NOY, RS>;
+    return launch_kernel<linattn_kernel<E, N, D, NOY, RS>, Cfg::LDS>(a, (size_t)a.B * a.H * a.run * a.jobs * Cfg::NTILE,
+                                                                     Cfg::NW * 64, st);
+}
+
+template <typename E, int N, int D, int R0, int R1>
+hipError_t launch_pair(const LinArgs& a, hipStream_t st) {
+    using Cfg = PairCfg<E, N, D, R0, R1>;
+    return launch_kernel<linattn_pair_kernel<E, N, D, R0, R1>, Cfg::LDS>(
+        a, (size_t)a.B * a.H * a.run * (2 * Cfg::A::NTILE + Cfg::B::NTILE), Cfg::NW * 64, st);
 }
 
 // One or two waves for a column group's state rows.  Two shorten the chain of a chunk's products and fill the
@@ -768,11 +806,10 @@ hipError_t launch(const LinArgs& a, hipStream_t st) {
 // 71, backward 160 and 173).
 template <typename E, int N, int D>
 hipError_t run_rows(const LinArgs& a, hipStream_t st) {
-    if constexpr (N == 128) {
-        const size_t groups = (size_t)a.B * a.H * a.run * a.jobs * LinCfg<E, N, D, false, 1>::NTILE;
-        if (groups <= 384) return launch<E, N, D, false, 2>(a, st);
-    }
-    return launch<E, N, D, false, N == 128 && sizeof(E) == 4 ? 2 : 1>(a, st);
+    constexpr int RS = N == 128 ? 2 : 1;
+    if constexpr (sizeof(E) == 2 && RS > 1)
+        if ((size_t)a.B * a.H * a.run * a.jobs * LinCfg<E, N, D, false, 1>::NTILE > 384) return launch<E, N, D, false, 1>(a, st);
+    return launch<E, N, D, false, RS>(a, st);
 }
 
 template <typename E>
@@ -782,6 +819,25 @@ hipError_t run(const LinArgs& a, int N, int D, bool noy, hipStream_t st) {
 #define KLA_LIN_ROW(N_) KLA_LIN(N_, 16) KLA_LIN(N_, 32) KLA_LIN(N_, 64) KLA_LIN(N_, 128)
     KLA_LIN_ROW(16) KLA_LIN_ROW(32) KLA_LIN_ROW(64) KLA_LIN_ROW(128)
 #undef KLA_LIN_ROW
+#undef KLA_LIN
+    return hipErrorInvalidValue;
+}
+
+template <typename E, int N, int D>
+hipError_t pair_rows(const LinArgs& a, hipStream_t st) {   // by the same rule as run_rows
+    constexpr int R0 = N == 128 ? 2 : 1, R1 = D == 128 ? 2 : 1;
+    using Cfg = PairCfg<E, N, D, R0, R1>;
+    if constexpr (sizeof(E) == 2 && R0 + R1 > 2)
+        if ((size_t)a.B * a.H * a.run * (2 * Cfg::A::NTILE + Cfg::B::NTILE) > 384) return launch_pair<E, N, D, 1, 1>(a, st);
+    return launch_pair<E, N, D, R0, R1>(a, st);
+}
+
+template <typename E>
+hipError_t run_pair(const LinArgs& a, int N, int D, hipStream_t st) {
+#define KLA_LIN(N_, D_) \
+    if (N == N_ && D == D_) return pair_rows<E, N_, D_>(a, st);
+    KLA_LIN(16, 32) KLA_LIN(16, 64) KLA_LIN(16, 128) KLA_LIN(32, 16) KLA_LIN(32, 64) KLA_LIN(32, 128)
+    KLA_LIN(64, 16) KLA_LIN(64, 32) KLA_LIN(64, 128) KLA_LIN(128, 16) KLA_LIN(128, 32) KLA_LIN(128, 64)
 #undef KLA_LIN
     return hipErrorInvalidValue;
 }
@@ -973,12 +1029,9 @@ hipError_t launch_linattn_bwd(const Shape& s, const void* q, const void* k, cons
     a.job[0] = LinJob{dy, v, k, first, dq, nullptr, 0, 1};
     a.job[1] = LinJob{v, dy, q, last, dk, nullptr, 1, 1};
     a.job[2] = LinJob{k, q, dy, last, dv, ds0, 1, 0};
-    a.jobs = s.dk == s.dv ? 3 : 2;
-    const hipError_t e = run(s, a, s.dv, s.dk, false, st);
-    if (e != hipSuccess || a.jobs == 3) return e;
-    a.job[0] = a.job[2];
-    a.jobs = 1;
-    return run(s, a, s.dk, s.dv, false, st);
+    a.jobs = 3;
+    if (s.dk == s.dv) return run(s, a, s.dk, s.dv, false, st);
+    return s.bf16 ? run_pair<uint16_t>(a, s.dv, s.dk, st) : run_pair<float>(a, s.dv, s.dk, st);
 }
 
 hipError_t launch_linattn_step(const Shape& s, const void* q, const void* k, const void* v, const float* g, float* state,

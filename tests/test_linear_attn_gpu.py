@@ -146,6 +146,15 @@ def test_wide_rows_in_few_and_many_sequences(kla, B, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H", [(2, 3), (8, 3), (70, 3)])
+@pytest.mark.parametrize("dk,dv", [(a, b) for a in (16, 32, 64, 128) for b in (16, 32, 64, 128) if a != b])
+def test_two_widths(kla, dk, dv, B, H, dtype):
+    """The backward runs passes of both shapes side by side."""
+    x = make(B, 45, H, dk, dv, dtype, True, True, dk + dv + B)
+    check(run(kla, x), x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("state", [False, True])
 def test_ragged_batch(kla, state, dtype):
     x = make(7, 75, 3, 64, 32, dtype, state, True, 11)
