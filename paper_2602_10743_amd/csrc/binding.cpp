@@ -296,11 +296,14 @@ Tensor dense(const Tensor& t) {
     const Tensor c = t.contiguous();
     return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 ? c.clone() : c;
 }
-// The nodes' backward passes are not differentiable themselves.  And where one is captured, no node that takes
-// its gradients may belong to the default stream, as a leaf's does that an eager graph made which still lives:
-// autograd would have that stream, which cannot be captured, wait for the capture, and so end it and the process.
-void check_backward(const Tensor& t) {
+// The nodes' backward passes are not differentiable themselves.
+void once() {
     TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), "second derivatives (create_graph=True) are not available");
+}
+// Where a backward is captured, no node that takes its gradients may belong to the default stream, as a leaf's
+// does that an eager graph made which still lives: autograd would have that stream, which cannot be captured, wait
+// for the capture, and so end it and the process.
+void check_capture(const Tensor& t) {
     const auto stream = c10::hip::getCurrentHIPStream(t.device().index());
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     if (!stream.stream() || hipStreamIsCapturing(stream.stream(), &status) != hipSuccess || status == hipStreamCaptureStatusNone)
@@ -387,9 +390,10 @@ struct LinearAttn : torch::autograd::Function<LinearAttn> {
         return lin_forward(d, q, k, v, g, s0, len, c10::nullopt, true);
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors x = ctx->get_saved_variables();
         const Tensor &q = x[0], &v = x[2];
-        check_backward(q);
+        check_capture(q);
         const kla_desc d{(int32_t)q.size(0), (int32_t)q.size(1), (int32_t)q.size(2), (int32_t)q.size(3), (int32_t)v.size(3),
                          q.scalar_type() == at::kFloat ? KLA_F32 : KLA_BF16};
         const Tensor dy = up[0].defined() ? dense(up[0]) : at::zeros_like(v);
@@ -526,8 +530,9 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         return out[0];
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors s = ctx->get_saved_variables();
-        check_backward(s[0]);
+        check_capture(s[0]);
         const Tensors out = norm_backward(rows_of(s[0], "x"), s[0], s[1], s[2], s[3], dense(up[0]),
                                           ctx->saved_data["bias"].toBool());
         return {out[0], out[1], out[2], Tensor()};
@@ -638,8 +643,9 @@ struct TokenLogp : torch::autograd::Function<TokenLogp> {
         return want_entropy ? Tensors{out[0], out[1]} : Tensors{out[0]};
     }
     static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
         const Tensors s = ctx->get_saved_variables();
-        check_backward(s[0]);
+        check_capture(s[0]);
         const Tensor dentropy = up.size() > 1 ? dense(up[1]) : Tensor();
         return {logp_backward(logits_of(s[0], s[1]), s[0], s[1], s[2], some(s[3]), some(dense(up[0])), some(dentropy)), Tensor(),
                 Tensor()};
