@@ -436,7 +436,8 @@ kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const fl
  *        gradients of the rows past them are written as zeros.
  *
  * The arithmetic is fp32 for either dtype: bf16 products are exact, their fp32 factors
- * carried to 16 bits or more, and the state keeps its 24 bits.  A value that is not finite
+ * (scores, states, decayed values) enter with all of their 24 bits, and outputs are
+ * rounded once.  A value that is not finite
  * reaches its own token and later ones only (in the backward, earlier ones).  The backward
  * needs no saved context: it returns dq, dk [B, T, H, dk] and dv [B, T, H, dv] (dtype,
  * required) and ds0 [B, H, dk, dv] (fp32 or NULL) from dy [B, T, H, dv] and dsT

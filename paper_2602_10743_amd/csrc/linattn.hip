@@ -21,9 +21,10 @@
 // (Q K^T) V and K^T V.  Rows are stored in 16-byte pieces, piece p of row r at p ^ f(r), which
 // spreads both the reads along rows and those across rows over the LDS banks.
 //
-// bf16: v_mfma_f32_16x16x32_bf16.  q, k, v are exact operands; fp32 factors are split into bf16
-// parts: the masked scores and the state (whose products are rounded to bf16 at the end) into two,
-// 16 bits, the decayed values that are added to the fp32 state into three, its 24 bits.
+// bf16: v_mfma_f32_16x16x32_bf16.  q, k, v are exact operands; fp32 factors (the masked scores, the
+// state, the decayed values) are split into three bf16 parts, all of their 24 bits, so that outputs are
+// fp32 sums rounded once.  (Two parts of scores and state, 16 bits, take 11% off a training step, but round
+// one output in 500 the other way, and what cancels against a large state keeps their error.)
 // fp32: v_mfma_f32_16x16x4_f32.
 #include <atomic>
 
@@ -130,15 +131,17 @@ struct Op<float> {
     }
 };
 
-// Accumulators (rows 4 g4 + rr of two 16-row tiles) as operands.  bf16: two parts, 16 bits.  What the first
-// leaves is formed by the matrix cores, tile - pick hi with pick[u] minus the unit that takes tile u's rows out
-// of the operand (exact: one product a sum); on the vector units, which bound this kernel, the same takes
-// four instructions for each pair of elements.
+// Accumulators (rows 4 g4 + rr of two 16-row tiles) as operands.  bf16: three parts, each the upper half of what
+// the ones before leave, which is exact: 24 bits.  What a part leaves is formed by the matrix cores, tile - pick
+// part with pick[u] minus the unit that takes tile u's rows out of the operand (one product a sum); on the vector
+// units the same takes four instructions for each pair of elements (backward of B = 8, T = 2048, H = 16, 128 wide:
+// 241 us, with both on the vector units 244, of B = 4 145 and 152).
 template <typename E>
 struct Acc;
 template <>
 struct Acc<uint16_t> {
-    bf16x8 h, l;
+    static constexpr int BYTES = 24;   // of a lane of one tile
+    bf16x8 p[3];
     struct Pick {
         bf16x8 of[2];
         __device__ Pick(int g4, int l16) {
@@ -155,32 +158,46 @@ struct Acc<uint16_t> {
         }
     };
     __device__ Acc() {}
+    template <bool HALF>
+    __device__ static bf16x8 upper(const f32x4& a, const f32x4& b) {
+        auto two = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+        return __builtin_bit_cast(bf16x8, uint4{two(a[0], a[1]), two(a[2], a[3]), HALF ? 0u : two(b[0], b[1]),
+                                                HALF ? 0u : two(b[2], b[3])});
+    }
     template <bool HALF = false>   // HALF: b is zero
-    __device__ static Acc from(const f32x4& a, const f32x4& b, const Pick& pick) {
+    __device__ static Acc from(f32x4 a, f32x4 b, const Pick& pick) {
         Acc o;
-        const uint4 hi{cvt_pk_bf16(a[0], a[1]), cvt_pk_bf16(a[2], a[3]), HALF ? 0u : cvt_pk_bf16(b[0], b[1]),
-                       HALF ? 0u : cvt_pk_bf16(b[2], b[3])};
-        o.h = __builtin_bit_cast(bf16x8, hi);
-        const f32x4 la = mfma_bf16(pick.of[0], o.h, a), lb = HALF ? zero4() : mfma_bf16(pick.of[1], o.h, b);
-        o.l = __builtin_bit_cast(bf16x8, uint4{cvt_pk_bf16(la[0], la[1]), cvt_pk_bf16(la[2], la[3]),
-                                               HALF ? 0u : cvt_pk_bf16(lb[0], lb[1]), HALF ? 0u : cvt_pk_bf16(lb[2], lb[3])});
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+            o.p[s] = upper<HALF>(a, b);
+            if (s == 2) break;
+            a = mfma_bf16(pick.of[0], o.p[s], a);
+            if (!HALF) b = mfma_bf16(pick.of[1], o.p[s], b);
+        }
         return o;
     }
-    // One tile's parts as 16 bytes of a lane, and the operands of (tile, nothing) or two tiles from them.
-    __device__ static uint4 packed(const f32x4& a, const Pick& pick) {
+    // One tile in LDS, at: the lane's place, and the operands of (tile, nothing) or two tiles from there.
+    __device__ static void put(const f32x4& a, const Pick& pick, uint2* at) {
         const Acc o = from<true>(a, zero4(), pick);
-        const uint4 h = __builtin_bit_cast(uint4, o.h), l = __builtin_bit_cast(uint4, o.l);
-        return uint4{h.x, h.y, l.x, l.y};
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+            const uint4 u = __builtin_bit_cast(uint4, o.p[s]);
+            at[64 * s] = uint2{u.x, u.y};
+        }
     }
-    __device__ static Acc of(const uint4& a, const uint4& b) {
+    __device__ static Acc get(const uint2* a, const uint2* b) {
         Acc o;
-        o.h = __builtin_bit_cast(bf16x8, uint4{a.x, a.y, b.x, b.y});
-        o.l = __builtin_bit_cast(bf16x8, uint4{a.z, a.w, b.z, b.w});
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+            const uint2 x = a[64 * s], y = b ? b[64 * s] : uint2{0u, 0u};
+            o.p[s] = __builtin_bit_cast(bf16x8, uint4{x.x, x.y, y.x, y.y});
+        }
         return o;
     }
 };
 template <>
 struct Acc<float> {
+    static constexpr int BYTES = 16;
     float x[8];
     struct Pick {
         __device__ Pick(int, int) {}
@@ -196,9 +213,15 @@ struct Acc<float> {
         }
         return o;
     }
-    __device__ static uint4 packed(const f32x4& a, const Pick&) { return __builtin_bit_cast(uint4, a); }
-    __device__ static Acc of(const uint4& a, const uint4& b) {
-        return from(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, b), Pick(0, 0));
+    __device__ static void put(const f32x4& a, const Pick&, uint2* at) {
+        const uint4 u = __builtin_bit_cast(uint4, a);
+        at[0] = uint2{u.x, u.y};
+        at[64] = uint2{u.z, u.w};
+    }
+    __device__ static Acc get(const uint2* a, const uint2* b) {
+        const uint2 none{0u, 0u}, x = a[0], y = a[64], z = b ? b[0] : none, w = b ? b[64] : none;
+        return from(__builtin_bit_cast(f32x4, uint4{x.x, x.y, y.x, y.y}), __builtin_bit_cast(f32x4, uint4{z.x, z.y, w.x, w.y}),
+                    Pick(0, 0));
     }
 };
 
@@ -248,19 +271,19 @@ __device__ __forceinline__ f32x4 mma(const Op<uint16_t>& a, const Op<uint16_t>& 
 }
 template <int STEPS = 8>
 __device__ __forceinline__ f32x4 mma(const Op<uint16_t>& a, const Acc<uint16_t>& b, f32x4 c) {
-    return mfma2b(a.x, b.h, b.l, c);
+#pragma unroll
+    for (int s = 2; s >= 0; --s) c = mfma_bf16(a.x, b.p[s], c);
+    return c;
 }
 // c[i][j] += a[i] b[j], part after part, so that no product waits for the one before it
 template <int STEPS, int NI>
 __device__ __forceinline__ void mma_each(const Acc<uint16_t> (&a)[NI], const Op<uint16_t> (&b)[2], f32x4 (&c)[NI][2]) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int s = 2; s >= 0; --s)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) c[i][j] = mfma_bf16(a[i].l, b[j].x, c[i][j]);
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) c[i][j] = mfma_bf16(a[i].h, b[j].x, c[i][j]);
+            for (int j = 0; j < 2; ++j) c[i][j] = mfma_bf16(a[i].p[s], b[j].x, c[i][j]);
 }
 template <int NI, int NJ>
 __device__ __forceinline__ void mma_each(const Op<uint16_t> (&a)[NI], const Scaled<uint16_t> (&b)[NJ], f32x4 (*c)[NJ]) {
@@ -395,8 +418,8 @@ struct LinCfg {
     static constexpr int CW = NOY && D == 128 ? 32 : 16, DT = NOY || D <= 64 ? D : 64, NTILE = D / DT, NCW = DT / CW;
     static constexpr int ROW = N * (int)sizeof(E), LW = ROW >= 256 ? 4 : ROW >= 128 ? 2 : 1,
                          NW = NCW * RS > LW ? NCW * RS : LW;
-    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES,
-                         LDS = 2 * BUF + 2 * kLC * (int)sizeof(float) + 3 * 1024 + (RS > 1 ? NCW * RS * (CW / 16) * 1024 : 0);
+    static constexpr int BUF = 2 * Tile<E, N>::BYTES + Tile<E, DT>::BYTES, SCORE = 64 * Acc<E>::BYTES,
+                         LDS = 2 * BUF + 2 * kLC * (int)sizeof(float) + 3 * SCORE + (RS > 1 ? NCW * RS * (CW / 16) * 1024 : 0);
     // waves per SIMD: of fp32 rows of 128 slots, LDS holds one workgroup a CU
     static constexpr int OCC = sizeof(E) == 4 && N == 128 ? 2 : RS > 1 ? 4 : 3;
 };
@@ -418,8 +441,9 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
     constexpr int BUF = Cfg::BUF;
     extern __shared__ __align__(16) unsigned char smem[];
     float* pw = reinterpret_cast<float*>(smem + 2 * BUF);   // e^{g n}
-    uint4* scores = reinterpret_cast<uint4*>(pw + 2 * kLC);   // of the chunk, three tiles
-    f32x4* part = reinterpret_cast<f32x4*>(scores + 3 * 64);  // of Q R, for the wave with the other rows
+    constexpr int SCORE = Cfg::SCORE / 8;
+    uint2* scores = reinterpret_cast<uint2*>(pw + 2 * kLC);   // of the chunk, three tiles
+    f32x4* part = reinterpret_cast<f32x4*>(scores + 3 * SCORE);  // of Q R, for the wave with the other rows
 
     int vi, ji, tile;   // the passes and tiles of one sequence on one XCD: they read the same rows
     {
@@ -591,7 +615,7 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
                                 Op<E>::template row<N>(sQ, (t > 0 ? 16 : 0) + l16, ks, g4), s);
 #pragma unroll
                 for (int rr = 0; rr < 4; ++rr) s[rr] *= t == 1 ? off[rr] : dia[rr];
-                scores[t * 64 + lane] = Acc<E>::packed(s, pick);
+                Acc<E>::put(s, pick, scores + t * SCORE + lane);
             }
         }
         Op<E> vf[NDT];
@@ -648,13 +672,12 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
         if constexpr (!NOY) {
             __syncthreads();   // the scores are there
             if (works) {
-                const uint4 none{0u, 0u, 0u, 0u};
                 f32x4 in[NDT][NIT];
                 float sum = 0.f;   // not finite where a value is not
 #pragma unroll
                 for (int it = 0; it < NIT; ++it) {
                     const int at = RS > 1 ? sh : it;   // one tile of earlier tokens, or two
-                    const Acc<E> p = at ? Acc<E>::of(scores[64 + lane], scores[128 + lane]) : Acc<E>::of(scores[lane], none);
+                    const Acc<E> p = at ? Acc<E>::get(scores + SCORE + lane, scores + 2 * SCORE + lane) : Acc<E>::get(scores + lane, nullptr);
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt) {
                         in[dt][it] = RS > 1 || it ? mma<8>(vf[dt], p, zero4()) : mma<4>(vf[dt], p, zero4());

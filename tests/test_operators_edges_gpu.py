@@ -1,0 +1,83 @@
+"""Edges of linear attention, layer norm and the token log probabilities: sums that cancel, values at the ends of
+fp32's range, infinities, operands off 16 bytes and outputs that lie over inputs, against the formulas in fp64.
+
+A rounding is off by half a step: bf16 2^-8, fp32 2^-24 of the value.  A product of the matrix cores adds to its
+sum with at most 2^-23 of the larger of the two."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from test_linear_attn_gpu import DEV, TYPES, expected, kla, make, run  # noqa: E402, F401
+
+pytestmark = pytest.mark.gpu
+
+
+def zeros(B, T, H, dk, dv, dtype, g):
+    """Inputs of linear attention that are all zero."""
+    x = dict(q=(dk,), k=(dk,), v=(dv,), dy=(dv,))
+    x = {n: torch.zeros(B, T, H, *w, dtype=TYPES[dtype]) for n, w in x.items()}
+    x.update(s0=torch.zeros(B, H, dk, dv), ds=torch.zeros(B, H, dk, dv), g=torch.full((H,), g), len=None)
+    return x
+
+
+def pair(shape, gen, dtype):
+    """Vectors of two values that are opposite, at places 2 n and 2 n + 1, and zeros."""
+    a = torch.zeros(*shape, dtype=TYPES[dtype])
+    n = 2 * torch.randint(0, shape[-1] // 2, shape[:-1], generator=gen)[..., None]
+    c = (1 + torch.rand(*shape[:-1], 1, generator=gen)).to(a.dtype)
+    return a.scatter_(-1, n, c).scatter_(-1, n + 1, -c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [16, 32, 128])
+@pytest.mark.parametrize("g", [0.0, -0.01])
+def test_large_states_that_cancel(kla, g, width, dtype):
+    """y, dq from a start state and dk, dv from a final state's gradient whose neighbouring rows and columns are the
+    same but for 2^-13, multiplied by opposite values.
+
+    Each output is a difference of two products with the state.  Its parts enter one after another, at most
+    three times two products, each adding with 2^-23 of half the mass: 3 x 2^-23 of the mass, the decay's
+    roundings 2^-22 of it; the factors' roundings scale the difference, which is small."""
+    gen = torch.Generator().manual_seed(width)
+    B, T, H = 3, 40, 2
+    for what in ("start", "final"):
+        x = zeros(B, T, H, width, width, dtype, g)
+        one = torch.randn(B, H, width // 2, width // 2, generator=gen).repeat_interleave(2, -1).repeat_interleave(2, -2)
+        near = one * (1 + 2.0 ** -13 * (2 * torch.rand(one.shape, generator=gen) - 1))
+        if what == "start":
+            x["s0"], names = near, ("y", "dq")
+            x["q"], x["dy"] = (pair((B, T, H, width), gen, dtype) for _ in range(2))
+        else:
+            x["ds"], names = near, ("dk", "dv")
+            x["k"], x["v"] = (pair((B, T, H, width), gen, dtype) for _ in range(2))
+        got, ref, mass = run(kla, x), expected(x), expected(x, torch.abs)
+        for n in names:
+            tol = 5 * 2.0 ** -23 * mass[n] + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * ref[n].abs()
+            assert ref[n].abs().max() > 2.0 ** -14 * mass[n].max() > 0
+            worst = ((got[n].double().cpu() - ref[n]).abs() / tol).nan_to_num(0.0).max().item()
+            print(f"{n} {worst:.3f} of the tolerance", flush=True)
+            assert worst <= 1.0, f"{n}: {worst:.2f} times the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_that_cancel(kla, dtype):
+    """Two tokens whose keys are the same but for 2^-13 in one slot and whose values are opposite.
+
+    The second's y is the difference of its two scores times a value.  A score is a sum of 16 products, off by
+    16 x 2^-24 of itself; the three parts of each score add with 2^-23 of it: (16 + 6) x 2^-24 of the mass."""
+    gen = torch.Generator().manual_seed(7)
+    B, T, H, w = 64, 2, 8, 16
+    x = zeros(B, T, H, w, w, dtype, 0.0)
+    t = TYPES[dtype]
+    x["q"][:, 1] = (0.5 + torch.rand(B, H, w, generator=gen)).to(t)
+    x["k"][:] = (0.5 + torch.rand(B, 1, H, w, generator=gen)).to(t)
+    x["k"][..., 15] = 0
+    x["k"][:, 1, :, 15] = (2.0 ** -10 * torch.rand(B, H, generator=gen)).to(t)
+    c = (1 + torch.rand(B, H, w, generator=gen)).to(t)
+    x["v"][:, 0], x["v"][:, 1] = c, -c
+    got, ref, mass = run(kla, x)["y"], expected(x)["y"], expected(x, torch.abs)["y"]
+    tol = 22 * 2.0 ** -24 * mass + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * ref.abs()
+    worst = ((got.double().cpu() - ref).abs() / tol).nan_to_num(0.0)[:, 1].max().item()
+    print(f"y {worst:.3f} of the tolerance", flush=True)
+    assert worst <= 1.0, f"{worst:.2f} times the tolerance"
