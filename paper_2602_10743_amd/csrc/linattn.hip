@@ -10,7 +10,9 @@
 //   R <- e^{g n} R + K^T diag(e^{g (n-j-o)}) V            n: the chunk's tokens
 // R is the state before the chunk (o = 1), or, walking backwards, that state already decayed once
 // (o = 0): the gradient of the final state enters undecayed, and the last R is the gradient of the
-// start state.  All exponents are at least 0, so no factor exceeds 1 for g <= 0; e^{-inf * 0} is 1.
+// start state.  All exponents are at least 0, so no factor exceeds 1 for g <= 0; e^{-inf * 0} is 1.  What is
+// formed on the way are products q . k and q . R of undecayed values: where those leave fp32's range, so may
+// the outputs that decay away from them, and nothing else does.
 //
 // A wave owns CW value columns of one sequence (or segment of one) and their state, in registers, or half of
 // the state's rows, and then, the sums over the rows exchanged, the outputs of half of the chunk's tokens;
@@ -572,10 +574,12 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
     };
     const typename Acc<E>::Pick pick(g4, l16);
     weights(kLC);
-    // The state is rho R, so that its decay is one product a chunk and not one an element, until rho is under
-    // 2^-8 (which leaves R all but 8 of the exponents).  Uniform: the branches on them are the wave's.
+    // The state is rho R, so that its decay is one product a chunk and not one an element.  rho falls from kRho
+    // to 1 and is then set back: R is the state or up to kRho times smaller, so it is finite where the state is;
+    // what it loses are bits of states within 2^8 of fp32's smallest.  Uniform: the branches on them are the wave's.
     auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
-    float gn = uniform(pw[kLC]), rho = 1.f;
+    constexpr float kRho = 0x1p8f;
+    float gn = uniform(pw[kLC]), rho = nchunk > 0 ? kRho : 1.f;
     auto scale = [&](float f) {
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt)
@@ -584,6 +588,7 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
 #pragma unroll
                 for (int rr = 0; rr < 4; ++rr) R[rt][dt][rr] *= f;
     };
+    if (job.start) scale(1.f / rho);
     // the start state has arrived: without this the loop would wait at the state's first use for every
     // access in flight, in each round
     wait_vm_all();
@@ -648,13 +653,11 @@ __device__ __forceinline__ void linattn_pass(const LinArgs& a, int block, int j0
             // R <- e^{g n} R + K^T (w V)
             float w[8];
             rho *= gn;
-            float inv = 1.f;
-            if (rho >= 0x1p-8f) {
-                inv = 1.f / rho;
-            } else {
-                scale(rho);
-                rho = 1.f;
+            if (!(rho >= 1.f)) {
+                scale(rho * (1.f / kRho));
+                rho = kRho;
             }
+            const float inv = 1.f / rho;
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = kw[e] * inv;
             Scaled<E> vs[NDT];

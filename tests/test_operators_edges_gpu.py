@@ -8,7 +8,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_linear_attn_gpu import DEV, TYPES, expected, kla, make, run  # noqa: E402, F401
+from test_linear_attn_gpu import DEV, TYPES, check, expected, kla, make, run  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,40 @@ def test_scores_that_cancel(kla, dtype):
     worst = ((got.double().cpu() - ref).abs() / tol).nan_to_num(0.0)[:, 1].max().item()
     print(f"y {worst:.3f} of the tolerance", flush=True)
     assert worst <= 1.0, f"{worst:.2f} times the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("g", [0.0, -0.01, -0.04, -0.17, -0.6, -6.0])
+@pytest.mark.parametrize("B,T,w", [(1, 320, 16), (1, 1100, 16), (2, 100, 128)])
+def test_states_near_the_top_of_the_range(kla, B, T, w, g, dtype):
+    """States and their gradients up to 1e38, from large values, keys and gradients and from a large start, at decays
+    of which a chunk's takes next to nothing and everything.  The factors that read them are small, so that every
+    sum over absolute values is within fp32's range."""
+    for big, beside in (("v", "k"), ("k", "v"), ("dy", "q")):
+        x = make(B, T, 1, w, w, dtype, True, False, 17, g)
+        for n in ("q", "k", "v", "dy"):
+            x[n] = x[n] * (1.0 if n in (big, beside) else 2.0 ** -10)
+        end, start, other = ("ds0", "ds", "s0") if big == "dy" else ("sT", "s0", "ds")
+        x[start], x[other] = x[start] * (1e38 / 5), x[other] * 1e-3
+        # the tokens' share of the state as large as the start's, where that leaves them in the range
+        one = expected({**x, start: 0 * x[start]}, torch.abs)[end].max().item()
+        x[big] = x[big] * 2.0 ** math.floor(math.log2(min(1e38 / one, 1e38 / x[big].abs().max().item())))
+        mass = expected(x, torch.abs)
+        assert all(u.max() < 3.3e38 for u in mass.values()), {n: u.max().item() for n, u in mass.items()}
+        assert max(mass[end].max(), x[big].abs().max()) > 2e37
+        check(run(kla, x), x, f"g {g} large {big}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("g", [0.0, -0.01, -0.6])
+def test_states_near_the_bottom_of_the_range(kla, g, dtype):
+    """States of 1e-34 and less, which are held to 2^-116 each: 16 of them in an output, with factors under 8."""
+    for scale in (1e-30, 1e-34, 1e-37):
+        x = make(1, 100, 2, 16, 16, dtype, True, False, 19, g)
+        for n in ("q", "k", "v", "dy"):
+            x[n] = x[n].clamp(-4, 4) * (1 if n in ("q", "k") else scale)
+        x["s0"], x["ds"] = x["s0"] * scale, x["ds"] * scale
+        got, ref, mass = run(kla, x), expected(x), expected(x, torch.abs)
+        for n in ("y", "sT", "dv", "ds0"):   # dq and dk are products of two such numbers
+            tol = 132 * 2.0 ** -24 * mass[n] + 2.0 ** -8 * ref[n].abs() + 16 * 8 * 2.0 ** -116
+            assert ((got[n].double().cpu() - ref[n]).abs() <= tol).all(), (n, scale)
