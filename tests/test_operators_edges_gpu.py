@@ -118,3 +118,26 @@ def test_states_near_the_bottom_of_the_range(kla, g, dtype):
         for n in ("y", "sT", "dv", "ds0"):   # dq and dk are products of two such numbers
             tol = 132 * 2.0 ** -24 * mass[n] + 2.0 ** -8 * ref[n].abs() + 16 * 8 * 2.0 ** -116
             assert ((got[n].double().cpu() - ref[n]).abs() <= tol).all(), (n, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinity_stays_in_its_column(kla, dtype):
+    """Of a value and of a start state: the columns beside it are as without it, its own is not finite from there on,
+    and infinite in fp32."""
+    clean = make(1, 100, 2, 32, 64, dtype, True, False, 23)
+    want = run(kla, clean)
+    for name, at, first in (("v", (0, 41, 1, 5), 41), ("s0", (0, 1, 3, 5), 0)):
+        x = {n: None if u is None else u.clone() for n, u in clean.items()}
+        x[name][at] = math.inf
+        got = run(kla, x)
+        rest = [d for d in range(64) if d != 5]
+        assert torch.equal(got["y"][0, :, 0], want["y"][0, :, 0]) and torch.equal(got["sT"][0, 0], want["sT"][0, 0])
+        # the chunk of an infinite value is added up in another order: rounding of one sum
+        assert torch.allclose(got["y"][0, :, 1, rest], want["y"][0, :, 1, rest], rtol=2.0 ** -7 if dtype == "bf16" else 1e-4,
+                              atol=1e-4)
+        assert torch.equal(got["sT"][0, 1][:, rest], want["sT"][0, 1][:, rest])
+        own = got["y"][0, :, 1, 5]
+        assert torch.allclose(own[:first], want["y"][0, :first, 1, 5], rtol=2.0 ** -7, atol=1e-4)
+        assert not torch.isfinite(own[first:]).any()
+        if name == "s0" and dtype == "f32":
+            assert torch.equal(own.cpu(), math.inf * x["q"][0, :, 1, 3].sign())
