@@ -7,7 +7,9 @@ torch is used for) and passes raw device pointers and the current HIP stream to
 the library, where every step of the filter runs.  The filter layer's forward,
 backward and decode step, linear attention, layer norm and the token log
 probabilities do this in C++ (``_kla_torch.so``, csrc/binding.cpp), the other entry
-points through ctypes.
+points through ctypes.  The library takes pointers on 16 bytes; linear attention, layer
+norm and the token log probabilities copy an input that is off them, such as one layer's
+row of stacked weights.
 
 There is no fallback: if the HIP library is missing or the tensors are not on
 a GPU, every entry point raises.

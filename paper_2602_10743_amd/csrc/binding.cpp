@@ -290,12 +290,13 @@ using Tensors = torch::autograd::variable_list;
 using Ctx = torch::autograd::AutogradContext;
 Opt some(const Tensor& t) { return t.defined() ? Opt(t) : Opt(); }
 Tensor or_undefined(const Opt& t) { return t ? *t : Tensor(); }
-// A tensor as the library takes it: dense, and on 16 bytes, which a slice of a larger one need not be.
-Tensor dense(const Tensor& t) {
-    if (!t.defined()) return t;
-    const Tensor c = t.contiguous();
-    return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 ? c.clone() : c;
+// An input as the library takes it, on 16 bytes: a slice of a larger one, such as one layer's row of stacked
+// weights, need not be and is copied.
+Tensor aligned(const Tensor& t) {
+    return t.defined() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 ? t.clone() : t;
 }
+Opt aligned(const Opt& t) { return t ? Opt(aligned(*t)) : Opt(); }
+Tensor dense(const Tensor& t) { return t.defined() ? t.contiguous() : t; }
 // The nodes' backward passes are not differentiable themselves.
 void once() {
     TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), "second derivatives (create_graph=True) are not available");
@@ -320,9 +321,11 @@ void check_capture(const Tensor& t) {
 }
 
 // The raw calls take checked tensors and need no interpreter lock.
-Tensors lin_forward(const kla_desc& d, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
-                    const Opt& len, const Opt& y_in, bool want_state) {
-    const c10::hip::HIPGuard on(q.device().index());
+Tensors lin_forward(const kla_desc& d, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Tensor& g_in,
+                    const Opt& s0_in, const Opt& len_in, const Opt& y_in, bool want_state) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in), v = aligned(v_in), g = aligned(g_in);
+    const Opt s0 = aligned(s0_in), len = aligned(len_in);
     const Tensor y = y_in ? *y_in : at::empty({d.B, d.T, d.H, d.dv}, q.options());
     Opt sT, ws;
     if (want_state) sT = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
@@ -334,9 +337,11 @@ Tensors lin_forward(const kla_desc& d, const Tensor& q, const Tensor& k, const T
     return {y, or_undefined(sT)};
 }
 
-Tensors lin_backward(const kla_desc& d, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
-                     const Opt& len, const Tensor& dy, const Opt& dsT, bool want_init) {
-    const c10::hip::HIPGuard on(q.device().index());
+Tensors lin_backward(const kla_desc& d, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Tensor& g_in,
+                     const Opt& s0_in, const Opt& len_in, const Tensor& dy_in, const Opt& dsT_in, bool want_init) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in), v = aligned(v_in), g = aligned(g_in), dy = aligned(dy_in);
+    const Opt s0 = aligned(s0_in), len = aligned(len_in), dsT = aligned(dsT_in);
     const Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
     Opt ds0, ws;
     if (want_init) ds0 = at::empty({d.B, d.H, d.dk, d.dv}, q.options().dtype(at::kFloat));
@@ -436,7 +441,8 @@ py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, c
         py::gil_scoped_release unlocked;
         const c10::hip::HIPGuard on(q.device().index());
         y = y_in ? *y_in : at::empty({S, H, dv}, q.options());
-        ok(kla_linear_attn_step(s32, h32, dk32, dv32, dt, ptr(q), ptr(k), ptr(v), (const float*)ptr(g), (float*)ptr(state),
+        const Tensor qa = aligned(q), ka = aligned(k), va = aligned(v), ga = aligned(g);
+        ok(kla_linear_attn_step(s32, h32, dk32, dv32, dt, ptr(qa), ptr(ka), ptr(va), (const float*)ptr(ga), (float*)ptr(state),
                                 ptr(y), stream_of(q)),
            "kla_linear_attn_step");
     }
@@ -469,8 +475,10 @@ Rows check_rows(const Tensor& x, const char* name) {
     return r;
 }
 
-Tensors norm_forward(const Rows& r, const Tensor& x, const Tensor& w, const Opt& bias, double eps) {
-    const c10::hip::HIPGuard on(x.device().index());
+Tensors norm_forward(const Rows& r, const Tensor& x_in, const Tensor& w_in, const Opt& bias_in, double eps) {
+    const c10::hip::HIPGuard on(x_in.device().index());
+    const Tensor x = aligned(x_in), w = aligned(w_in);
+    const Opt bias = aligned(bias_in);
     const Tensor out = at::empty_like(x), mean = at::empty(r.lead, x.options().dtype(at::kFloat)), rstd = at::empty_like(mean);
     ok(kla_layer_norm_forward(r.rows, r.n, r.dtype, ptr(x), (const float*)ptr(w), fptr(bias), (float)eps, ptr(out),
                               (float*)ptr(mean), (float*)ptr(rstd), stream_of(x)),
@@ -478,9 +486,10 @@ Tensors norm_forward(const Rows& r, const Tensor& x, const Tensor& w, const Opt&
     return {out, mean, rstd};
 }
 
-Tensors norm_backward(const Rows& r, const Tensor& x, const Tensor& w, const Tensor& mean, const Tensor& rstd,
-                      const Tensor& dout, bool want_bias) {
-    const c10::hip::HIPGuard on(x.device().index());
+Tensors norm_backward(const Rows& r, const Tensor& x_in, const Tensor& w_in, const Tensor& mean_in, const Tensor& rstd_in,
+                      const Tensor& dout_in, bool want_bias) {
+    const c10::hip::HIPGuard on(x_in.device().index());
+    const Tensor x = aligned(x_in), w = aligned(w_in), mean = aligned(mean_in), rstd = aligned(rstd_in), dout = aligned(dout_in);
     const Tensor dx = at::empty_like(x), dw = at::empty_like(w);
     Opt db;
     if (want_bias) db = at::empty_like(w);
@@ -523,7 +532,7 @@ py::object layer_norm_backward(const Tensor& x, const Tensor& w, const Tensor& m
 
 struct LayerNorm : torch::autograd::Function<LayerNorm> {
     static Tensor forward(Ctx* ctx, const Tensor& x_in, const Tensor& w, const Opt& bias, double eps) {
-        const Tensor x = dense(x_in);
+        const Tensor x = aligned(dense(x_in));
         const Tensors out = norm_forward(rows_of(x, "x"), x, w, bias, eps);
         ctx->save_for_backward({x, w, out[1], out[2]});
         ctx->saved_data["bias"] = bias && bias->requires_grad();
@@ -578,8 +587,10 @@ std::vector<int64_t> with(std::vector<int64_t> lead, int64_t n) {
 }
 
 // logp, entropy, stat, top_logp, top_index.  No rows, or no draws of them: nothing to do.
-Tensors logp_forward(const Logits& l, const Tensor& x, const Tensor& target, bool want_entropy, int32_t top, bool want_stat) {
-    const c10::hip::HIPGuard on(x.device().index());
+Tensors logp_forward(const Logits& l, const Tensor& x_in, const Tensor& target_in, bool want_entropy, int32_t top,
+                     bool want_stat) {
+    const c10::hip::HIPGuard on(x_in.device().index());
+    const Tensor x = aligned(x_in), target = aligned(target_in);
     const auto f32 = x.options().dtype(at::kFloat);
     const Tensor logp = at::empty(l.lead, f32);
     Opt entropy, stat, top_logp, top_index, ws;
@@ -598,9 +609,11 @@ Tensors logp_forward(const Logits& l, const Tensor& x, const Tensor& target, boo
     return {logp, or_undefined(entropy), or_undefined(stat), or_undefined(top_logp), or_undefined(top_index)};
 }
 
-Tensor logp_backward(const Logits& l, const Tensor& x, const Tensor& target, const Tensor& stat, const Opt& entropy,
-                     const Opt& dlogp, const Opt& dentropy) {
-    const c10::hip::HIPGuard on(x.device().index());
+Tensor logp_backward(const Logits& l, const Tensor& x_in, const Tensor& target_in, const Tensor& stat_in,
+                     const Opt& entropy_in, const Opt& dlogp_in, const Opt& dentropy_in) {
+    const c10::hip::HIPGuard on(x_in.device().index());
+    const Tensor x = aligned(x_in), target = aligned(target_in), stat = aligned(stat_in);
+    const Opt entropy = aligned(entropy_in), dlogp = aligned(dlogp_in), dentropy = aligned(dentropy_in);
     const Tensor dx = at::empty_like(x);
     if (x.numel() > 0)
         ok(kla_token_logp_backward(l.S, l.n, l.V, l.dtype, ptr(x), (const int64_t*)ptr(target), (const float*)ptr(stat),
@@ -636,7 +649,7 @@ Tensor token_logp_backward(const Tensor& x, const Tensor& target, const Tensor& 
 
 struct TokenLogp : torch::autograd::Function<TokenLogp> {
     static Tensors forward(Ctx* ctx, const Tensor& x_in, const Tensor& target_in, bool want_entropy) {
-        const Tensor x = dense(x_in), target = dense(target_in);
+        const Tensor x = aligned(dense(x_in)), target = aligned(dense(target_in));
         const Tensors out = logp_forward(logits_of(x, target), x, target, want_entropy, 0, true);
         ctx->save_for_backward({x, target, out[2], out[1]});
         ctx->set_materialize_grads(false);

@@ -141,3 +141,73 @@ def test_an_infinity_stays_in_its_column(kla, dtype):
         assert not torch.isfinite(own[first:]).any()
         if name == "s0" and dtype == "f32":
             assert torch.equal(own.cpu(), math.inf * x["q"][0, :, 1, 3].sign())
+
+
+def off16(u):
+    """The same values in a tensor that is dense but does not start on 16 bytes, as a row of stacked ones."""
+    o = torch.empty(u.numel() + 1, dtype=u.dtype, device=u.device)[1:].view_as(u).copy_(u)
+    assert o.is_contiguous() and o.data_ptr() % 16
+    return o
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_attention_of_operands_off_16_bytes(kla, dtype):
+    x = {n: None if u is None else u.to(DEV) for n, u in make(3, 70, 5, 32, 64, dtype, True, True, 25).items()}
+    calls = (lambda d: kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"]),
+             lambda d: kla.kla_linear_attn_backward(d["q"], d["k"], d["v"], d["g"], d["s0"], d["len"], d["dy"], d["ds"]),
+             lambda d: kla.kla_linear_attn_step(*(d[n] for n in ("q1", "k1", "v1")), d["g"], x["s0"].clone()))
+
+    def train(d):
+        ins = [d[n].detach().requires_grad_(True) for n in ("q", "k", "v", "s0")]
+        y, sT = kla.kla_linear_attn(*ins[:3], d["g"], ins[3], d["len"])
+        return dict(enumerate([y, sT, *torch.autograd.grad([y, sT], ins, [d["dy"], d["ds"]])]))
+    x.update({n + "1": x[n][:, 0].contiguous() for n in ("q", "k", "v")})
+    for call in (*calls, train):
+        want = call(x)
+        for n in x:
+            got = call({**x, n: off16(x[n])})
+            assert all(torch.equal(want[m], got[m]) for m in want), n
+    stacked = torch.stack([2 * x["g"], x["g"]])   # [layers, 5]
+    got = train({**x, "g": stacked[1]})
+    assert all(torch.equal(a, got[m]) for m, a in train(x).items())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [64, 1001])
+def test_layer_norm_of_operands_off_16_bytes(kla, n, dtype):
+    g = torch.Generator(device=DEV).manual_seed(n)
+    z = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    x = dict(x=z(7, n).to(TYPES[dtype]), w=1 + z(n), b=z(n), dy=z(7, n).to(TYPES[dtype]))
+    x["mean"], x["rstd"] = kla.kla_layer_norm_forward(x["x"], x["w"], x["b"])[1:]
+    calls = (lambda d: kla.kla_layer_norm_forward(d["x"], d["w"], d["b"]),
+             lambda d: kla.kla_layer_norm_backward(d["x"], d["w"], d["mean"], d["rstd"], d["dy"]))
+
+    def train(d):
+        ins = [d[m].detach().requires_grad_(True) for m in ("x", "w", "b")]
+        y = kla.kla_layer_norm(*ins)
+        return (y, *torch.autograd.grad(y, ins, d["dy"]))
+    for call in (*calls, train):
+        want = call(x)
+        for m in x:
+            assert all(map(torch.equal, want, call({**x, m: off16(x[m])}))), m
+    layers = {m: torch.stack([2 * x[m], x[m], 0 * x[m]]) for m in ("w", "b")}   # the second layer's row
+    assert all(map(torch.equal, train(x), train({**x, "w": layers["w"][1], "b": layers["b"][1]})))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_token_logp_of_operands_off_16_bytes(kla, dtype):
+    g = torch.Generator(device=DEV).manual_seed(3)
+    z = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    x = dict(x=z(5, 333).to(TYPES[dtype]), t=torch.randint(0, 333, (5,), generator=g, device=DEV), dl=z(5), de=z(5))
+    fwd = lambda d: kla.kla_token_logp_forward(d["x"], d["t"], want_entropy=True, top=4, save=True)
+    x.update({m: fwd(x)[m] for m in ("stat", "entropy")})
+
+    def train(d):
+        u = d["x"].detach().requires_grad_(True)
+        out = kla.kla_token_logp(u, d["t"], want_entropy=True)
+        return (*out, *torch.autograd.grad(out, u, [d["dl"], d["de"]]))
+    for call in (lambda d: tuple(fwd(d).values()), train,
+                 lambda d: (kla.kla_token_logp_backward(d["x"], d["t"], d["stat"], d["entropy"], d["dl"], d["de"]),)):
+        want = call(x)
+        for m in x:
+            assert all(map(torch.equal, want, call({**x, m: off16(x[m])}))), m
