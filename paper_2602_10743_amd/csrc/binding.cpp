@@ -359,8 +359,9 @@ py::object linear_attn_forward(const Tensor& q, const Tensor& k, const Tensor& v
     const kla_desc d = check_lin(q, k, v, g, s0, len);
     if (y_in) {
         check_like(*y_in, {d.B, d.T, d.H, d.dv}, q, "y");
-        check_apart(*y_in, "y", {&q, &k, &v});
+        check_apart(*y_in, "y", {&q, &k, &v, &g});
         if (s0) check_apart(*y_in, "y", {&*s0});
+        if (len) check_apart(*y_in, "y", {&*len});
     }
     Tensors out;
     {
@@ -432,9 +433,9 @@ py::object linear_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, c
     check_f32(state, {S, H, dk, dv}, q, "state");
     if (y_in) {
         check_like(*y_in, {S, H, dv}, q, "y");
-        check_apart(*y_in, "y", {&q, &k, &v, &state});
+        check_apart(*y_in, "y", {&q, &k, &v, &g, &state});
     }
-    check_apart(state, "state", {&q, &k, &v});
+    check_apart(state, "state", {&q, &k, &v, &g});
     const int32_t s32 = int32_of(S, "S"), h32 = int32_of(H, "H"), dk32 = int32_of(dk, "dk"), dv32 = int32_of(dv, "dv");
     Tensor y;
     {

@@ -211,3 +211,22 @@ def test_token_logp_of_operands_off_16_bytes(kla, dtype):
         want = call(x)
         for m in x:
             assert all(map(torch.equal, want, call({**x, m: off16(x[m])}))), m
+
+
+def test_outputs_apart_from_decays_and_lengths(kla):
+    """Other workgroups read them while an output that lies over them would be written."""
+    x = make(2, 8, 4, 16, 16, "f32", True, True, 1)
+    d = {n: None if u is None else u.to(DEV) for n, u in x.items()}
+    y = torch.empty_like(d["v"])
+    g = y.view(-1)[-4:].copy_(d["g"])
+    with pytest.raises(ValueError, match="y must not overlap"):
+        kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], g, d["s0"], y=y)
+    n = y.view(-1)[:2].view(torch.int32).copy_(d["len"])
+    with pytest.raises(ValueError, match="y must not overlap"):
+        kla.kla_linear_attn_forward(d["q"], d["k"], d["v"], d["g"], d["s0"], n, y=y)
+    one = [d[n][:, 0].contiguous() for n in ("q", "k", "v")]
+    y = torch.empty_like(one[2])
+    with pytest.raises(ValueError, match="y must not overlap"):
+        kla.kla_linear_attn_step(*one, y.view(-1)[4:8].copy_(d["g"]), d["s0"], y=y)
+    with pytest.raises(ValueError, match="state must not overlap"):
+        kla.kla_linear_attn_step(*one, d["s0"].view(-1)[8:12].fill_(-1.0), d["s0"])
