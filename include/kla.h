@@ -468,7 +468,7 @@ kla_status kla_linear_attn_step(int32_t S, int32_t H, int32_t dk, int32_t dv, in
  *
  *   x, out, dout, dx [rows, n] dtype, n in 1 .. 16384; w [n] fp32; bias [n] fp32 or NULL;
  *   mean, rstd [rows] fp32: written for the backward (each may be NULL in the forward).
- * Sums are fp32, the squares about the mean.  dw [n] (required) and dbias [n] (or NULL),
+ * Sums are fp32, the squares about the mean, and the mean is corrected by the mean of what it leaves.  dw [n] (required) and dbias [n] (or NULL),
  * fp32, are overwritten with the sums over the rows, in a fixed order through the workspace.
  */
 size_t kla_layer_norm_workspace(int32_t n);

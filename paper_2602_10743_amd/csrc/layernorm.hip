@@ -6,10 +6,10 @@
 //
 // Bound by HBM: x is read and out written once, x and dout read and dx written once.  A group of TPR
 // lanes holds a row in registers (EPT elements a lane, in vectors of VEC), so the sum of squares is
-// taken about the mean in a second pass over registers, and the sums are fp32.  A lane's columns are
-// the same in every row: w and bias are loaded once, and the backward adds its rows' dw and dbias up in
-// registers, joins a workgroup's groups in LDS and leaves one part per workgroup, which a second
-// kernel adds in a fixed order: results are bitwise reproducible.
+// taken about the mean in a second pass over registers, which also corrects the mean, and the sums are
+// fp32.  A lane's columns are the same in every row: w and bias are loaded once, and the backward adds
+// its rows' dw and dbias up in registers, joins a workgroup's groups in LDS and leaves one part per
+// workgroup, which a second kernel adds in a fixed order: results are bitwise reproducible.
 #include "kla_buf.hpp"
 #include "kla_device.hpp"
 #include "kla_internal.hpp"
@@ -90,36 +90,34 @@ __device__ __forceinline__ void load_w(const float* w, int c, int n, float* f) {
     }
 }
 
-// Two sums over the TPR lanes of a row, in every lane.  buf: LDS for groups of several waves, two
+// Sums of M values over the TPR lanes of a row, in every lane.  buf: LDS for groups of several waves, two
 // slots of 2 x TPR / 64 floats taken in turn, so that one barrier per call is enough.
-template <int TPR>
-__device__ __forceinline__ void group_sum2(float& a, float& b, float* buf, int& turn) {
+template <int TPR, int M>
+__device__ __forceinline__ void group_sum(float (&a)[M], float* buf, int& turn) {
     if constexpr (TPR < 64) {
 #pragma unroll
-        for (int m = 1; m < TPR; m *= 2) {
-            a += __shfl_xor(a, m);
-            b += __shfl_xor(b, m);
-        }
+        for (int m = 1; m < TPR; m *= 2)
+#pragma unroll
+            for (int i = 0; i < M; ++i) a[i] += __shfl_xor(a[i], m);
     } else {
-        a = wave_sum(a);
-        b = wave_sum(b);
+#pragma unroll
+        for (int i = 0; i < M; ++i) a[i] = wave_sum(a[i]);
         if constexpr (TPR > 64) {
             constexpr int NW = TPR / 64;
             const int group = threadIdx.x / TPR, wave = (threadIdx.x % TPR) / 64;
             const int groups = blockDim.x / TPR;
             float* s = buf + (turn * groups + group) * 2 * NW;
             turn ^= 1;
-            if ((threadIdx.x & 63) == 0) {
-                s[2 * wave] = a;
-                s[2 * wave + 1] = b;
-            }
-            __syncthreads();
-            a = b = 0.f;
+            if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                a += s[2 * w];
-                b += s[2 * w + 1];
-            }
+                for (int i = 0; i < M; ++i) s[M * wave + i] = a[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < M; ++i) a[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int i = 0; i < M; ++i) a[i] += s[M * w + i];
         }
     }
 }
@@ -152,7 +150,7 @@ __global__ __launch_bounds__(kFwdThreads<TPR>) void layernorm_fwd_kernel(size_t 
     for (size_t r0 = (size_t)blockIdx.x * RPB; r0 < rows; r0 += (size_t)gridDim.x * RPB) {
         const size_t r = r0 + threadIdx.x / TPR;
         const bool live = r < rows;
-        float v[EPT], s = 0.f, unused = 0.f;
+        float v[EPT], s[1] = {0.f}, t[2] = {0.f, 0.f};   // t: of squares and of what the mean leaves
 #pragma unroll
         for (int i = 0; i < HB; ++i) {
             const int c = (i * TPR + tl) * VEC;
@@ -164,29 +162,34 @@ __global__ __launch_bounds__(kFwdThreads<TPR>) void layernorm_fwd_kernel(size_t 
             }
         }
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) s += v[e];
-        group_sum2<TPR>(s, unused, buf, turn);
-        const float mu = s * inv;
-        float q = 0.f;
+        for (int e = 0; e < EPT; ++e) s[0] += v[e];
+        group_sum<TPR>(s, buf, turn);
+        // The sum's roundings are up to 2^-20 of |x|, which rstd may raise 300 times: the mean of what it leaves
+        // corrects it, at the barrier that the squares need.  x - mu is exact near a mu that is rounded: kept from
+        // being contracted with the product.
+        float mu = s[0] * inv;
+        asm("" : "+v"(mu));
 #pragma unroll
         for (int i = 0; i < HB; ++i)
             if ((i * TPR + tl) * VEC < n)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     v[i * VEC + e] -= mu;
-                    q += v[i * VEC + e] * v[i * VEC + e];
+                    t[0] += v[i * VEC + e] * v[i * VEC + e];
+                    t[1] += v[i * VEC + e];
                 }
-        group_sum2<TPR>(q, unused, buf, turn);
-        const float rs = 1.f / sqrtf(q * inv + eps);
+        group_sum<TPR>(t, buf, turn);
+        const float c = t[1] * inv, var = t[0] * inv - c * c, rs = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
+        mu += c;
         if (!live) continue;
 #pragma unroll
         for (int i = 0; i < HB; ++i) {
-            const int c = (i * TPR + tl) * VEC;
-            if (c < n) {
+            const int at = (i * TPR + tl) * VEC;
+            if (at < n) {
                 float o[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) o[e] = v[i * VEC + e] * rs * wr[i * VEC + e] + br[i * VEC + e];
-                store_vec<E, VEC>(out + r * n + c, o);
+                for (int e = 0; e < VEC; ++e) o[e] = fmaf(v[i * VEC + e], rs, -c * rs) * wr[i * VEC + e] + br[i * VEC + e];
+                store_vec<E, VEC>(out + r * n + at, o);
             }
         }
         if (tl == 0) {
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(kBwdThreads) void layernorm_bwd_kernel(size_t rows,
             }
         }
         const float mu = live ? mean[r] : 0.f, rs = live ? rstd[r] : 0.f;
-        float c1 = 0.f, c2 = 0.f;
+        float t[2] = {0.f, 0.f};   // sums of d and of d xh
 #pragma unroll
         for (int i = 0; i < HB; ++i)
             if ((i * TPR + tl) * VEC < n)
@@ -245,12 +248,11 @@ __global__ __launch_bounds__(kBwdThreads) void layernorm_bwd_kernel(size_t rows,
                     sw[j] += d[j] * v[j];
                     sb[j] += d[j];
                     d[j] *= wr[j];
-                    c1 += d[j];
-                    c2 += d[j] * v[j];
+                    t[0] += d[j];
+                    t[1] += d[j] * v[j];
                 }
-        group_sum2<TPR>(c1, c2, buf, turn);
-        c1 *= inv;
-        c2 *= inv;
+        group_sum<TPR>(t, buf, turn);
+        const float c1 = t[0] * inv, c2 = t[1] * inv;
         if (!live) continue;
 #pragma unroll
         for (int i = 0; i < HB; ++i) {

@@ -230,3 +230,49 @@ def test_outputs_apart_from_decays_and_lengths(kla):
         kla.kla_linear_attn_step(*one, y.view(-1)[4:8].copy_(d["g"]), d["s0"], y=y)
     with pytest.raises(ValueError, match="state must not overlap"):
         kla.kla_linear_attn_step(*one, d["s0"].view(-1)[8:12].fill_(-1.0), d["s0"])
+
+
+@pytest.mark.parametrize("n", [7, 100, 1001, 2048, 5000, 16384])
+def test_layer_norm_of_constant_rows(kla, n):
+    """No spread: the output is the bias, however large the value is against sqrt(eps).
+
+    The mean's sum is off by D <= 48 x 2^-24 |x| and what it leaves, the same in every element, is exact and adds up
+    exactly; its mean is off by 2^-22 D, which rstd = eps^-1/2 raises 316 times: 48 x 2^-46 |x| 316."""
+    x = torch.tensor([1000.1, -77.77, 3.0e4 + 0.125, 0.3, 0.0], device=DEV)[:, None].repeat(1, n)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    w, b, dy = (torch.randn(s, generator=g, device=DEV) for s in ((n,), (n,), (5, n)))
+    out, mean, rstd = kla.kla_layer_norm_forward(x, w, b)
+    dx, dw, db = kla.kla_layer_norm_backward(x, w, mean, rstd, dy)
+    off = 48 * 2.0 ** -46 * 317 * x.abs()
+    assert ((out - b).abs() <= off * w.abs() + 2.0 ** -23 * b.abs()).all()
+    assert torch.equal(mean, x[:, 0])
+    assert ((rstd * 1e-5 ** 0.5 - 1).abs() <= 2.0 ** -22 + off[:, 0] ** 2).all()
+    assert (dw.abs() <= (off * dy.abs()).sum(0)).all()
+    d = (dy * w).double()
+    want = 1e-5 ** -0.5 * (d - d.mean(-1, keepdim=True))
+    # sums of 48 roundings, and the roundings of rstd, of the difference and of the product
+    assert ((dx - want).abs() <= 64 * 2.0 ** -24 * 1e-5 ** -0.5 * (d.abs() + d.abs().mean(-1, keepdim=True))).all()
+
+
+@pytest.mark.parametrize("n", [100, 1001, 4096])
+@pytest.mark.parametrize("shift,spread", [(1000.0, 0.02), (-5e4, 3.0), (3.0, 1e-4)])
+def test_layer_norm_far_from_zero(kla, n, shift, spread):
+    """Rows whose offset is large against their spread.
+
+    x - mu is exact for a mu near x; the sum that gives mu is off by D <= 48 x 2^-24 |shift|, which the second mean
+    takes out but for 64 x 2^-24 of the mean of |x - mu|, at most that of |x - mean| and D."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    x = shift + spread * torch.randn(20, n, generator=g, device=DEV)
+    w, b = (torch.randn(n, generator=g, device=DEV) for _ in range(2))
+    out, mean, rstd = kla.kla_layer_norm_forward(x, w, b)
+    X = x.double()
+    m = X.mean(-1, keepdim=True)
+    var = (X - m).square().mean(-1, keepdim=True)
+    r = 1 / torch.sqrt(var + 1e-5)
+    D = 48 * 2.0 ** -24 * X.abs().amax(-1, keepdim=True)
+    left = 64 * 2.0 ** -24 * ((X - m).abs() + (X - m).abs().mean(-1, keepdim=True) + D)
+    rel = 64 * 2.0 ** -24 * (1 + (D * r).square())   # of the mean square, which has the mean's square taken off
+    want = (X - m) * r * w + b
+    assert ((out - want).abs() <= (left * r + rel * (X - m).abs() * r) * w.abs() + 2.0 ** -23 * (want.abs() + b.abs())).all()
+    assert ((mean - m[:, 0]).abs() <= left[:, 0] + 2.0 ** -24 * m[:, 0].abs()).all()
+    assert ((rstd / r[:, 0] - 1).abs() <= rel[:, 0]).all()
