@@ -35,6 +35,7 @@ constexpr int kRoom = 1024;     // collected elements
 constexpr int kMaxParts = 64;   // of a row
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eLo = (float)(1.4426950408889634 - (double)kLog2e);
 
 template <typename E>
 constexpr int kVec = 16 / (int)sizeof(E);
@@ -95,7 +96,17 @@ struct Sums {
     float m, s, u;
 };
 
-__device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }   // e^d
+// e^d of d <= 0 as 2^x of a rounded x: off by 2^-24 |x| of itself and the instruction's 2^-23.  For the sums, where
+// |d| e^d is under 1/2 of the largest term, and for outputs of 8 bits.
+__device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// The same with what x loses, for the fp32 gradients of unlikely tokens (d = -80: 2e-7 instead of 3e-6).  0 from
+// d = -150 on, and for NaN.
+__device__ __forceinline__ float exp_of(float d) {
+    d = fmaxf(d, -150.f);
+    const float x = d * kLog2e, lo = fmaf(d, kLog2eLo, fmaf(d, kLog2e, -x)), e = __builtin_amdgcn_exp2f(x);
+    return fmaf(e, lo * 0.693147181f, e);
+}
 
 __device__ __forceinline__ void rise(Sums& t, float m) {   // m >= t.m
     const float d = fmaxf(t.m - m, kLowest), r = exp2_of(d);
@@ -419,7 +430,7 @@ __global__ __launch_bounds__(kThreads) void logp_bwd_kernel(LogpArgs a, const fl
     const float base = dl + (de != 0.f ? de * (a.entropy[r] - ls) : 0.f);
     const size_t hot = tg >= 0 && tg < a.V ? sp.a + (size_t)tg : ~(size_t)0;
     auto grad = [&](float v, size_t at) {
-        const float d = v - m, p = exp2_of(d) * inv;
+        const float d = v - m, p = (N == 4 ? exp_of(d) : exp2_of(d)) * inv;   // NaN logits are in s
         float y = p == 0.f ? 0.f : -p * (base + de * d);
         if (at == hot) y += dl;
         return s == 0.f ? 0.f : y;

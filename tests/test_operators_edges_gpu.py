@@ -276,3 +276,23 @@ def test_layer_norm_far_from_zero(kla, n, shift, spread):
     assert ((out - want).abs() <= (left * r + rel * (X - m).abs() * r) * w.abs() + 2.0 ** -23 * (want.abs() + b.abs())).all()
     assert ((mean - m[:, 0]).abs() <= left[:, 0] + 2.0 ** -24 * m[:, 0].abs()).all()
     assert ((rstd / r[:, 0] - 1).abs() <= rel[:, 0]).all()
+
+
+def test_gradients_of_unlikely_tokens(kla):
+    """fp32 logits under a first one of 0, far enough for their sum to be 1: the gradient of token v is -e^{x_v}.
+
+    2^x is off by 2^-23 and the product that adds what x lost by 2^-24; the product with 1 / s = 1 is exact."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = -(25 + 60 * torch.rand(6, 1000, generator=g, device=DEV))
+    x[:, 0] = 0
+    x[1] = torch.where(x[1] < 0, x[1].round(), x[1])
+    target = torch.zeros(6, dtype=torch.int64, device=DEV)
+    out = kla.kla_token_logp_forward(x, target, save=True)
+    assert torch.equal(out["stat"], torch.tensor([0.0, 1.0], device=DEV).expand(6, 2))
+    dx = kla.kla_token_logp_backward(x, target, out["stat"], None, torch.ones(6, device=DEV))
+    want = -torch.exp(x.double())[:, 1:]
+    off = ((dx[:, 1:].double() - want) / want).abs().max().item()
+    assert off <= 2.0 ** -22, off
+    x[2, 5] = -math.inf
+    dx = kla.kla_token_logp_backward(x, target, out["stat"], None, torch.ones(6, device=DEV))
+    assert dx[2, 5] == 0 and torch.isfinite(dx).all()
