@@ -396,16 +396,17 @@ __device__ __forceinline__ int seq_len(const LinArgs& a, int b) {
 
 // 16 bytes a lane from r at voff into LDS at dst + 16 lane; lanes past the buffer's end write zeros.  Not the
 // compiler's builtin, behind which every transposing read of LDS waits for all loads in flight, the prefetch
-// among them: who reads the tile waits with wait_vm_le.  Nothing is loaded into registers, and nothing else
-// in this file uses m0.  The wait states are those between a vector instruction that writes a scalar register
-// (readfirstlane) and a memory access that reads it, which the compiler does not count inside.
+// among them: who reads the tile waits with wait_vm_le.  Nothing is loaded into registers, and m0, the place in
+// LDS, is an operand that the compiler sets.  The wait states are those between an instruction that writes a
+// scalar register (readfirstlane, the move to m0) and a memory access that reads it, which the compiler does not
+// count inside.
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t words_t;
 __device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_t voff) {
     words_t u;   // uniform: in scalar registers
 #pragma unroll
     for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_readfirstlane(r[i]);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
-                 "s"(__builtin_amdgcn_readfirstlane(dst))
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
+                 "{m0}"(__builtin_amdgcn_readfirstlane(dst))
                  : "memory");
 }
 
