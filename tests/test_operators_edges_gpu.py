@@ -296,3 +296,39 @@ def test_gradients_of_unlikely_tokens(kla):
     x[2, 5] = -math.inf
     dx = kla.kla_token_logp_backward(x, target, out["stat"], None, torch.ones(6, device=DEV))
     assert dx[2, 5] == 0 and torch.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_segments_of_a_long_sequence(kla, dtype):
+    """More than 96 chunks a segment where there were two workgroups a CU: the other number of segments, in both
+    directions, with a padded sequence's tokens ending inside one."""
+    x = make(1, 49170, 32, 16, 16, dtype, True, True, 31)
+    x["len"] = torch.tensor([49170 - 500], dtype=torch.int32)
+    check(run(kla, x), x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("at", [1, 95, 96, 550, 1098])
+def test_values_that_are_not_finite_in_a_cut_sequence(kla, dtype, bad, at):
+    """In the first segment, at a border, in the middle and in the last: earlier outputs (in the backward, later
+    gradients), the other sequence and the other head stay as they are."""
+    clean = make(2, 1100, 2, 32, 32, dtype, True, True, 33)
+    clean["len"] = torch.tensor([1100, 700], dtype=torch.int32)
+    want = run(kla, clean)
+    for name in ("q", "k", "v", "dy"):
+        x = {n: None if u is None else u.clone() for n, u in clean.items()}
+        x[name][0, at, 1] = bad
+        got = run(kla, x)
+        for n in ("y", "dq", "dk", "dv"):
+            assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, :, 0], want[n][0, :, 0]), (name, n)
+            late = n in ("dk", "dv")
+            a, b = (u[n][0, at + 1:, 1] if late else u[n][0, :at, 1] for u in (got, want))
+            assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7 if dtype == "bf16" else 1e-4, atol=1e-4), (name, n)
+        for n in ("sT", "ds0"):
+            assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 0], want[n][0, 0]), (name, n)
+        if name in ("k", "v"):
+            assert not torch.isfinite(got["y"][0, at:, 1]).all() and not torch.isfinite(got["sT"][0, 1]).all()
+        else:
+            assert not torch.isfinite(got["ds0"][0, 1]).all()
+            assert torch.equal(got["sT"], want["sT"])
