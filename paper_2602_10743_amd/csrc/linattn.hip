@@ -412,10 +412,10 @@ __device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_
 
 // A workgroup takes DT of the D columns, a wave CW of them and one of RS shares of the state's rows.  Where the
 // rows of Q and K are long and the waves that compute (NCW RS) few, others help with the loads.  64 columns in
-// waves of 16 with all rows take 132 registers and 43 KiB of LDS, so three workgroups of 128-wide bf16 passes
-// share a CU (B = 8, T = 2048, H = 16: forward 100 us and backward 196, against 139 and 226 with 128 columns
-// in waves of 32, whose scores are formed half as often but which one or two waves a SIMD have to hide).  The
-// states' pass forms no scores: all columns.
+// waves of 16 with all rows take 133 registers and 45 KiB of LDS, so three workgroups of 128-wide bf16 passes
+// share a CU (B = 8, T = 2048, H = 16: forward 108 us and backward 243, against 225 and 316 with 128 columns
+// in waves of 32, whose scores are formed half as often but which one wave a SIMD has to hide).  The states' pass
+// forms no scores: all columns.
 template <typename E, int N, int D, bool NOY, int RS>
 struct LinCfg {
     static constexpr int CW = NOY && D == 128 ? 32 : 16, DT = NOY || D <= 64 ? D : 64, NTILE = D / DT, NCW = DT / CW;
@@ -748,8 +748,8 @@ __global__ __launch_bounds__((LinCfg<E, N, D, NOY, RS>::NW * 64),
 
 // A backward with dk != dv: two passes with N = dv, D = dk and one the other way round in one launch, R0 and R1
 // waves for their state rows.  Side by side they fill what each leaves idle (us in two launches and in one, dk/dv:
-// bf16, B = 8, T = 2048, H = 16, 64/128 155 and 130, 128/64 176 and 159; B = 16, T = 512, 16/64 40 and 24; B = 3,
-// T = 777, H = 5, 64/128 37 and 32; fp32, B = 8, T = 1024, H = 16, 32/64 122 and 91, 64/128 190 and 190).
+// bf16, B = 8, T = 2048, H = 16, 64/128 195 and 156, 128/64 197 and 176; B = 16, T = 512, 16/64 46 and 27; B = 3,
+// T = 777, H = 5, 64/128 40 and 34; fp32, B = 8, T = 1024, H = 16, 32/64 125 and 94, 64/128 200 and 189).
 template <typename E, int N, int D, int R0, int R1>
 struct PairCfg {
     using A = LinCfg<E, N, D, false, R0>;
@@ -826,16 +826,21 @@ hipError_t launch_pair(const LinArgs& a, hipStream_t st) {
 }
 
 // One or two waves for a column group's state rows.  Two shorten the chain of a chunk's products and fill the
-// SIMDs where there are few workgroups, but both convert V.  128 rows, dk = dv = 128, T = 2048, H = 16, us with
-// one and two: bf16, forward of B = 8 (256 workgroups) 113 and 98, backward of B = 4 (384) 136 and 130, forward
-// of B = 16 (512) 141 and 160, backward of B = 8 (768) 215 and 233; fp32, whose LDS holds one workgroup a CU,
-// forward 246 and 228, backward 735 and 676.  Of 64 rows two waves win nothing (B = 16, dv = 64, forward 72 and
-// 71, backward 160 and 173).
+// SIMDs where there are fewer than two workgroups a CU, but both convert V.  128 rows, us with one and two
+// (workgroups): bf16, 128/128, H = 16, T = 2048, forward 118 and 108 (256), T = 1024, forward 97 and 98 (512), 122 and
+// 136 (640), backward 84 and 80 (384), 90 and 89 (480), 107 and 119 (576); backward of both shapes, H = 8,
+// T = 1024, 128/64 77 and 69 (480), 92 and 98 (640), 64/128 81 and 79 (480), 100 and 114 (640); fp32, whose LDS holds
+// one workgroup a CU, 128/128, T = 1024, forward 127 and 117, backward 369 and 339 (B = 8), 735 and 674 (B = 16).
+// With 32 columns or fewer two win beyond that too (backward of 128/16, 640: 77 and 67, 1920: 198 and 192).  Of 64
+// rows two take the forward of an uncut sequence from 81 to 75 (128 workgroups), where segments take it to 41, and
+// the backward from 175 to 201 (768).
+constexpr size_t kTwoWaves = 512;   // two workgroups a CU: fewer take two waves
 template <typename E, int N, int D>
 hipError_t run_rows(const LinArgs& a, hipStream_t st) {
     constexpr int RS = N == 128 ? 2 : 1;
     if constexpr (sizeof(E) == 2 && RS > 1)
-        if ((size_t)a.B * a.H * a.run * a.jobs * LinCfg<E, N, D, false, 1>::NTILE > 384) return launch<E, N, D, false, 1>(a, st);
+        if ((size_t)a.B * a.H * a.run * a.jobs * LinCfg<E, N, D, false, 1>::NTILE >= kTwoWaves)
+            return launch<E, N, D, false, 1>(a, st);
     return launch<E, N, D, false, RS>(a, st);
 }
 
@@ -855,7 +860,8 @@ hipError_t pair_rows(const LinArgs& a, hipStream_t st) {   // by the same rule a
     constexpr int R0 = N == 128 ? 2 : 1, R1 = D == 128 ? 2 : 1;
     using Cfg = PairCfg<E, N, D, R0, R1>;
     if constexpr (sizeof(E) == 2 && R0 + R1 > 2)
-        if ((size_t)a.B * a.H * a.run * (2 * Cfg::A::NTILE + Cfg::B::NTILE) > 384) return launch_pair<E, N, D, 1, 1>(a, st);
+        if ((size_t)a.B * a.H * a.run * (2 * Cfg::A::NTILE + Cfg::B::NTILE) >= kTwoWaves)
+            return launch_pair<E, N, D, 1, 1>(a, st);
     return launch_pair<E, N, D, R0, R1>(a, st);
 }
 
@@ -958,12 +964,12 @@ hipError_t step(const Shape& s, const void* q, const void* k, const void* v, con
 // make `want`, or `more` where segments would be longer than 96 chunks.  Segments cost a pass over K and V for
 // their states and two launches more, so a sequence of fewer than 16 chunks is not cut, nor where there is a
 // workgroup for every CU (dk = dv = 128, bf16, B = 8, T = 2048, H = 16, us whole and in two: forward, 256
-// workgroups, 100 and 135; backward, 768, 196 and 282).
+// workgroups, 110 and 145; backward, 768, 250 and 322).
 // Otherwise the forward makes two workgroups a CU and the backward, whose passes share their reads,
-// three (us in 4, 8, 16, 24 segments, B = 1, T = 16384, H = 16, forward 295, 158, 117, 119, backward 381,
-// 282, 277, 294; B = 4, T = 4096, H = 8, forward 88, 71, 73, 80, backward 147, 147, 168, 196), but none
-// shorter than two chunks; where they are long, one and three workgroups a CU more (T = 65536 in 8, 16, 24,
-// 32: forward 582, 447, 427, 457, backward 1170, 1054, 1071, 1083).
+// three (us in 4, 8, 16, 24 segments, B = 1, T = 16384, H = 16, forward 317, 175, 137, 137, backward 428,
+// 330, 327, 349; in 2, 4, 8, 16, B = 4, T = 4096, H = 8, forward 165, 96, 78, 81, backward 220, 171, 175, 198), but
+// none shorter than two chunks; where they are long, one and three workgroups a CU more (T = 65536 in 8, 16, 24,
+// 32: forward 629, 513, 501, 505, backward 1267, 1225, 1266, 1233).
 void segments(const Shape& s, long groups, long want, long more, int& ns, int& lc) {
     const int nc = (s.T + kLC - 1) / kLC;
     ns = 1;

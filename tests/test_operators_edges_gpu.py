@@ -332,3 +332,11 @@ def test_values_that_are_not_finite_in_a_cut_sequence(kla, dtype, bad, at):
         else:
             assert not torch.isfinite(got["ds0"][0, 1]).all()
             assert torch.equal(got["sT"], want["sT"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dv", [16, 32, 64, 128])
+def test_wide_rows_in_many_sequences(kla, dv, dtype):
+    """More than two workgroups a CU in the forward too: one wave for the rows of a state 128 wide in bf16."""
+    x = make(180, 35, 3, 128, dv, dtype, True, True, dv)
+    check(run(kla, x), x)
