@@ -4,7 +4,8 @@
 //
 // A training step of a few sequences is bound by the host: through ctypes and torch.empty the
 // forward took 21 us and the backward 33 us of it, more than their kernels.  Functions return the
-// output tensors, or the status code when the library refuses the call.  Past the checks they give
+// output tensors; where the library refuses the call, those of the layer return its status code and
+// those of the operators around it raise KLAError.  Past the checks they give
 // up the interpreter lock, as ctypes does: allocations and a full launch queue can block, and under
 // KLA_CHECK=1 the library waits for the stream.
 #include <array>

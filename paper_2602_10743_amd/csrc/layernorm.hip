@@ -333,7 +333,8 @@ constexpr unsigned kParts = 256;   // workgroups of the backward, one per CU
 
 // Calls f<VEC, EPT, TPR> for a row of n elements: the widest vectors that rows of n keep aligned, and the
 // fewest lanes that hold a row in 16 registers each (16384 x 2048 bf16, forward: 24 us with 16 elements on
-// 128 lanes, 24 with 8 on 256, 27 with 32 on 64; backward, whose lanes hold five such rows: 52, 56, 52).
+// 128 lanes, 24 with 8 on 256, 27 with 32 on 64; backward, whose lanes hold five such rows: 46, 46, and 168 in
+// more registers than its 1024 threads have).
 template <typename E, typename F>
 hipError_t by_shape(int n, F&& f) {
 #define KLA_LN_SHAPES(V_)                                                               \
