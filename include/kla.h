@@ -437,16 +437,16 @@ kla_status kla_mc_nll_backward(int32_t S, int64_t n, const float* logp, const fl
  *
  * The arithmetic is fp32 for either dtype: bf16 products are exact, their fp32 factors
  * (scores, states, decayed values) enter with all of their 24 bits, and outputs are
- * rounded once.  A state is finite where the recurrence's is; one under 2^-92 is held to
- * 2^-116.  Within 32 tokens q_t . k_s and q_t . S are formed before they decay: these have
- * to stay within fp32's range.  A value that is not finite reaches its own token and later
- * ones only (in the backward, earlier ones); an infinite v[d] or S[., d] leaves the columns
- * beside d as they are, and with bf16 inputs may come out of its own as NaN, as inf - inf
- * does.  The backward needs no saved context: it
- * returns dq, dk [B, T, H, dk] and dv [B, T, H, dv] (dtype, required) and ds0 [B, H, dk, dv]
- * (fp32 or NULL) from dy [B, T, H, dv] and dsT [B, H, dk, dv] fp32 (NULL: zero).  The step
- * takes one token for S sequences and updates state [S, H, dk, dv] in place.
- * H max(dk, dv) <= 2^24, B H (S H) <= 2^20 and T <= 2^30.
+ * rounded once.  A state is finite where the recurrence's is; states and values (v; in the
+ * backward q, k and dy too) under 2^-92 are held to 2^-116.  Within 32 tokens q_t . k_s and
+ * q_t . S are formed before they decay: these have to stay within fp32's range.  A value
+ * that is not finite reaches its own token and later ones only (in the backward, earlier
+ * ones); an infinite v[d] or S[., d] leaves the columns beside d as they are, and with
+ * bf16 inputs may come out of its own as NaN, as inf - inf does.  The backward needs no
+ * saved context: it returns dq, dk [B, T, H, dk] and dv [B, T, H, dv] (dtype, required)
+ * and ds0 [B, H, dk, dv] (fp32 or NULL) from dy [B, T, H, dv] and dsT [B, H, dk, dv] fp32
+ * (NULL: zero).  The step takes one token for S sequences and updates state [S, H, dk, dv]
+ * in place.  H max(dk, dv) <= 2^24, B H (S H) <= 2^20 and T <= 2^30.
  */
 size_t kla_linear_attn_workspace(const kla_desc* desc);
 size_t kla_linear_attn_backward_workspace(const kla_desc* desc);

@@ -340,3 +340,16 @@ def test_wide_rows_in_many_sequences(kla, dv, dtype):
     """More than two workgroups a CU in the forward too: one wave for the rows of a state 128 wide in bf16."""
     x = make(180, 35, 3, 128, dv, dtype, True, True, dv)
     check(run(kla, x), x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_small_values_of_large_keys(kla, dtype):
+    """Values of 1e-33 and less, held to 2^-116 each, of keys of 1e6: the state and y keep that times the keys."""
+    for scale in (1e-26, 1e-33, 1e-36):
+        x = make(1, 100, 2, 16, 16, dtype, True, False, 35, -0.02)
+        x["k"], x["v"], x["dy"], x["s0"], x["ds"] = x["k"] * 1e6, x["v"] * scale, 0 * x["dy"], 0 * x["s0"], 0 * x["ds"]
+        got, ref, mass = run(kla, x), expected(x), expected(x, torch.abs)
+        per = expected({**x, "v": torch.ones_like(x["v"])}, torch.abs)   # of values that are one
+        for n in ("y", "sT"):
+            tol = 132 * 2.0 ** -24 * mass[n] + 2.0 ** -8 * ref[n].abs() + 2.0 ** -116 * per[n] + 2.0 ** -116
+            assert ((got[n].double().cpu() - ref[n]).abs() <= tol).all(), (n, scale)
