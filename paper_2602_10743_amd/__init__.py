@@ -815,8 +815,9 @@ def kla_linear_attn_step(q, k, v, g, state, *, y=None) -> dict:
 
 
 def kla_linear_attn(q, k, v, g, s0=None, lengths=None):
-    """Differentiable linear attention with a decay for each head: returns (y, sT).  The decays are
-    constants: a g that requires a gradient is refused."""
+    """Differentiable linear attention with a decay for each head: returns (y, sT).  q, k and v may have any
+    strides, as parts of a fused projection do.  The decays are constants: a g that requires a gradient is
+    refused."""
     return _native().linear_attn(q, k, v, g, s0, lengths)
 
 

@@ -225,16 +225,17 @@ py::object decode_step(const Tensor& q, const Tensor& k, const Tensor& v, const 
 
 // ---- the operators around the layer: each call runs on its tensors' device, whichever is current
 
-void check_gpu(const Tensor& t, const char* name) {
+// strided: any strides will do, the caller makes the tensor dense
+void check_gpu(const Tensor& t, const char* name, bool strided = false) {
     if (!t.is_cuda()) value_error(std::string(name) + " must live on a GPU; there is no CPU path");
-    if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+    if (!strided && !t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
 }
 
-void check_like(const Tensor& t, at::IntArrayRef shape, const Tensor& q, const char* name) {
+void check_like(const Tensor& t, at::IntArrayRef shape, const Tensor& q, const char* name, bool strided = false) {
     if (t.sizes() != shape) value_error(std::string(name) + " has shape " + shape_str(t.sizes()) + ", expected " + shape_str(shape));
     if (t.scalar_type() != q.scalar_type() || t.device() != q.device())
         value_error(std::string(name) + " must share the inputs' dtype and device");
-    if (!t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+    if (!strided && !t.is_contiguous()) value_error(std::string(name) + " must be contiguous");
 }
 
 void check_int(const Opt& t, at::ScalarType type, at::IntArrayRef shape, const Tensor& q, const char* name) {
@@ -263,13 +264,14 @@ int32_t int32_of(int64_t n, const char* what) {
     return (int32_t)n;
 }
 
-kla_desc check_lin(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s, const Opt& len) {
-    check_gpu(q, "q");
+kla_desc check_lin(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s, const Opt& len,
+                   bool strided = false) {
+    check_gpu(q, "q", strided);
     const int dt = dtype_of(q);
     if (q.dim() != 4 || v.dim() != 4) value_error("q must be [B, T, H, dk] and v [B, T, H, dv]");
     const int64_t B = q.size(0), T = q.size(1), H = q.size(2), dk = q.size(3), dv = v.size(3);
-    check_like(k, {B, T, H, dk}, q, "k");
-    check_like(v, {B, T, H, dv}, q, "v");
+    check_like(k, {B, T, H, dk}, q, "k", strided);
+    check_like(v, {B, T, H, dv}, q, "v", strided);
     check_f32(g, {H}, q, "g");
     check_f32(s, {B, H, dk, dv}, q, "s0");
     check_int(len, at::kInt, {B}, q, "lengths");
@@ -389,8 +391,9 @@ py::object linear_attn_backward(const Tensor& q, const Tensor& k, const Tensor& 
 
 // y, sT with their gradients.  Nodes in C++: through Python's they took most of a small training step.
 struct LinearAttn : torch::autograd::Function<LinearAttn> {
-    static Tensors forward(Ctx* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0,
+    static Tensors forward(Ctx* ctx, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Tensor& g, const Opt& s0,
                            const Opt& len, const kla_desc& d) {
+        const Tensor q = dense(q_in), k = dense(k_in), v = dense(v_in);   // parts of a fused projection
         ctx->save_for_backward({q, k, v, g, or_undefined(s0), or_undefined(len)});
         ctx->set_materialize_grads(false);   // an unused output's gradient stays undefined: nothing to fill or read
         ctx->saved_data["init"] = s0 && s0->requires_grad();
@@ -411,7 +414,7 @@ struct LinearAttn : torch::autograd::Function<LinearAttn> {
 };
 
 py::object linear_attn(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& g, const Opt& s0, const Opt& len) {
-    const kla_desc d = check_lin(q, k, v, g, s0, len);
+    const kla_desc d = check_lin(q, k, v, g, s0, len, true);
     if (g.requires_grad()) value_error("g holds constants: the decays take no gradient");
     Tensors out;
     {

@@ -353,3 +353,23 @@ def test_small_values_of_large_keys(kla, dtype):
         for n in ("y", "sT"):
             tol = 132 * 2.0 ** -24 * mass[n] + 2.0 ** -8 * ref[n].abs() + 2.0 ** -116 * per[n] + 2.0 ** -116
             assert ((got[n].double().cpu() - ref[n]).abs() <= tol).all(), (n, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_of_a_fused_projection(kla, dtype):
+    """q, k and v as views of one tensor, or with heads before tokens: the same values and gradients as dense ones."""
+    x = {n: None if u is None else u.to(DEV) for n, u in make(2, 60, 3, 32, 64, dtype, True, True, 37).items()}
+
+    def train(make_qkv, leaves):
+        leaves = [u.detach().requires_grad_(True) for u in leaves]
+        y, sT = kla.kla_linear_attn(*make_qkv(*leaves), x["g"], x["s0"], x["len"])
+        return y, sT, torch.autograd.grad([y, sT], leaves, [x["dy"], x["ds"]])
+    y, sT, (dq, dk, dv) = train(lambda *u: u, [x["q"], x["k"], x["v"]])
+    fused = torch.cat([x[n].flatten(2) for n in ("q", "k", "v")], -1)   # [B, T, H (2 dk + dv)]
+    y1, sT1, (df,) = train(lambda f: [u.unflatten(2, (3, -1)) for u in f.split([96, 96, 192], -1)], [fused])
+    assert torch.equal(y, y1) and torch.equal(sT, sT1)
+    assert torch.equal(df, torch.cat([u.flatten(2) for u in (dq, dk, dv)], -1))
+    turned = [x[n].transpose(1, 2).contiguous() for n in ("q", "k", "v")]
+    y2, sT2, grads = train(lambda *u: [w.transpose(1, 2) for w in u], turned)
+    assert torch.equal(y, y2) and torch.equal(sT, sT2)
+    assert all(torch.equal(a.transpose(1, 2), b) for a, b in zip((dq, dk, dv), grads))
