@@ -504,6 +504,100 @@ kla_status kla_token_logp_backward(int32_t S, int64_t n, int32_t V, int32_t dtyp
                                    const int64_t* target, const float* stat, const float* entropy, const float* dlogp,
                                    const float* dentropy, void* dlogits, hipStream_t stream);
 
+/*
+ * Norms of queries and keys for each head and the position rotation, in one pass: what
+ * an attention layer between filter layers has in front of it.  Per token and head,
+ *
+ *   u = x / sqrt(mean(x^2) + eps) * w          over the head's n elements
+ *   (u_a, u_b) -> (u_a cos phi - u_b sin phi, u_b cos phi + u_a sin phi),   phi = position * freq[i]
+ *
+ * for the pairs i < pairs: elements i and i + pairs, or with `interleaved` 2i and 2i + 1; the
+ * elements from 2 pairs on are not rotated.
+ *
+ *   q, q_out [B, T, H, n]   k, k_out [B, T, Hk, n]   dtype;  n in {16, 32, 64, 128}
+ *   wq, wk    [n] fp32, shared by the heads; either may be NULL (ones)
+ *   freq      [pairs] fp64; pairs a multiple of 8, at most n / 2; NULL for pairs = 0 (the norm alone)
+ *   positions [B, T] int32, or NULL: token t of each sequence is at position t
+ *
+ * Angles are formed and reduced in fp64, all else in fp32; sums of squares have to stay within
+ * fp32's range.  The backward needs no saved context: from dq_out and dk_out it returns dq, dk
+ * (dtype) and dwq, dwk [n] fp32 (either may be NULL), summed over tokens and heads in a fixed
+ * order through the workspace.  H and Hk >= 1, (H + Hk) n <= 2^24.
+ */
+typedef struct kla_rope_desc {
+    int32_t B, T, H, Hk;
+    int32_t n, pairs;
+    int32_t interleaved; /* 0 or 1 */
+    int32_t dtype;
+    float eps; /* >= 0 */
+} kla_rope_desc;
+
+size_t kla_qk_norm_rope_workspace(const kla_rope_desc* desc);
+kla_status kla_qk_norm_rope_forward(const kla_rope_desc* desc, const void* q, const void* k, const float* wq,
+                                    const float* wk, const double* freq, const int32_t* positions, void* q_out,
+                                    void* k_out, hipStream_t stream);
+kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, const void* k, const float* wq,
+                                     const float* wk, const double* freq, const int32_t* positions,
+                                     const void* dq_out, const void* dk_out, void* dq, void* dk, float* dwq, float* dwk,
+                                     void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Softmax attention with a sliding window and first tokens that stay visible, the attention
+ * layer of a hybrid stack: like the filter's belief, what it keeps of a sequence is bounded.
+ *
+ *   y_i = sum_j P_ij v_j,   P_i = softmax of scale q_i . k_j over the visible j
+ *
+ * The key of token j is visible to the query at position p iff j <= p and (j > p - window or
+ * j < sinks); window >= Tk is plain causal attention.  Query head h reads key head h Hk / H.
+ *
+ *   q, y [B, T, H, d]   k, v [B, Tk, Hk, d]   dtype;  d in {16, 32, 64, 128}, H a multiple of Hk
+ *   Tk >= T: the queries are the last T of Tk tokens (query i is at position Tk - T + i)
+ *   len  [B] int32 or NULL: sequence b has len[b] tokens (taken into 0 .. Tk).  Tokens past them
+ *        are not read; y and the gradients of the rows past them are written as zeros.
+ *   saved  kla_window_attn_saved_bytes(desc) or NULL: the forward's context for the backward (each
+ *        row's largest score and sum of exponentials, and for bf16 rows that see few tokens what the
+ *        rounding of y left)
+ *   cache_k, cache_v [B, sinks + window, Hk, d] dtype or both NULL: the cache for the step, as it
+ *        is after the last token; slots that hold no token are written as zeros
+ *
+ * The step takes one token for S sequences, q, y [S, H, d] and k, v [S, Hk, d], at positions
+ * pos [S] int32 (the number of tokens before it): it writes k and v into the caches' slot of
+ * that position, p < sinks ? p : sinks + (p - sinks) mod window, and attends to every slot that
+ * holds a token.  Slots that hold none are not read.  A sequence with pos < 0 takes no token: its
+ * caches stay as they are and y is zero.
+ *
+ * Scores, softmax and sums are fp32.  With bf16 inputs P and its gradient enter their products
+ * rounded to bf16; with fp32 inputs everything stays fp32.  A row whose visible scores are all
+ * -inf has y = 0 and no gradient.  What is masked has no influence, finite or not.  The backward
+ * takes y and saved of the forward and returns dq, dk, dv (dtype, all required).  scale > 0 and
+ * finite, window >= 1, sinks in 0 .. 64, sinks + window <= 2^30, H d <= 2^22, Tk <= 2^28, and
+ * fewer than 2^23 workgroups: B H (T / 128) and B Hk (Tk / 128 + T / 512).
+ */
+typedef struct kla_window_desc {
+    int32_t B, T, Tk;
+    int32_t H, Hk, d;
+    int32_t window, sinks;
+    int32_t dtype;
+    float scale;
+} kla_window_desc;
+
+size_t kla_window_attn_saved_bytes(const kla_window_desc* desc);
+size_t kla_window_attn_workspace(const kla_window_desc* desc);
+size_t kla_window_attn_backward_workspace(const kla_window_desc* desc);
+kla_status kla_window_attn_forward(const kla_window_desc* desc, const void* q, const void* k, const void* v,
+                                   const int32_t* len, void* y, void* saved, void* cache_k, void* cache_v,
+                                   void* ws, size_t ws_bytes, hipStream_t stream);
+kla_status kla_window_attn_backward(const kla_window_desc* desc, const void* q, const void* k, const void* v,
+                                    const int32_t* len, const void* y, const void* saved, const void* dy, void* dq,
+                                    void* dk, void* dv, void* ws, size_t ws_bytes, hipStream_t stream);
+
+size_t kla_window_attn_step_workspace(int32_t S, int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks,
+                                      int32_t dtype);
+kla_status kla_window_attn_step(int32_t S, int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks,
+                                int32_t dtype, float scale, const void* q, const void* k, const void* v,
+                                const int32_t* pos, void* cache_k, void* cache_v, void* y, void* ws, size_t ws_bytes,
+                                hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char* kla_status_string(kla_status status);
 

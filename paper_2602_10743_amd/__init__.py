@@ -34,6 +34,8 @@ __all__ = ["kla_forward", "kla_backward", "kla_backward_noalloc", "kla_decode_st
            "kla_linear_attn_forward", "kla_linear_attn_backward", "kla_linear_attn_step", "kla_linear_attn",
            "kla_layer_norm_forward", "kla_layer_norm_backward", "kla_layer_norm",
            "kla_token_logp_forward", "kla_token_logp_backward", "kla_token_logp",
+           "kla_qk_norm_rope_forward", "kla_qk_norm_rope_backward", "kla_qk_norm_rope",
+           "kla_window_attn_forward", "kla_window_attn_backward", "kla_window_attn_step", "kla_window_attn",
            "KLAError", "KLAFilter", "kla_filter", "KLAFilterOU", "kla_filter_ou", "library_path"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -858,3 +860,63 @@ def kla_token_logp(logits, target, *, want_entropy: bool = False):
     """Differentiable log probabilities of the tokens target, or (logp, entropy) with want_entropy; the
     logp of S draws [S, n] is what kla_mc_nll takes."""
     return _native().token_logp(logits, target, bool(want_entropy))
+
+
+# ------------------------------------------------------------------ norms of queries and keys with the rotation
+def kla_qk_norm_rope_forward(q, k, wq=None, wk=None, freq=None, positions=None, eps: float = 1e-6, *,
+                             interleaved: bool = False):
+    """x / sqrt(mean(x^2) + eps) * w for each head of q [B, T, H, n] and k [B, T, Hk, n] (fp32 or bf16; or [S, H, n]
+    and [S, Hk, n], one token of S sequences), wq, wk [n] fp32 or None (ones), then the rotation of pairs of elements
+    by position * freq: freq [pairs] fp64 (pairs a multiple of 8, at most n / 2) or None (no rotation), positions
+    [B, T] (or [S]) int32 or None (token t is at position t).  Pair i is elements i and i + pairs, or with interleaved
+    2i and 2i + 1.  Returns (q_out, k_out)."""
+    return _native().qk_norm_rope_forward(q, k, wq, wk, freq, positions, float(eps), bool(interleaved))
+
+
+def kla_qk_norm_rope_backward(q, k, wq, wk, freq, positions, dq_out, dk_out, eps: float = 1e-6, *,
+                              interleaved: bool = False) -> dict:
+    """Gradients of kla_qk_norm_rope_forward: dq, dk in the input dtype and dwq, dwk [n] fp32 (None without the
+    weight)."""
+    out = _native().qk_norm_rope_backward(q, k, wq, wk, freq, positions, dq_out, dk_out, float(eps), bool(interleaved))
+    return dict(zip(("dq", "dk", "dwq", "dwk"), out))
+
+
+def kla_qk_norm_rope(q, k, wq=None, wk=None, freq=None, positions=None, eps: float = 1e-6, *, interleaved: bool = False):
+    """Differentiable norms of queries and keys with the rotation: returns (q_out, k_out).  q and k may have any
+    strides, as parts of a fused projection do.  The frequencies are constants: a freq that requires a gradient is
+    refused."""
+    return _native().qk_norm_rope(q, k, wq, wk, freq, positions, float(eps), bool(interleaved))
+
+
+# ------------------------------------------------------------------ attention with a sliding window
+def kla_window_attn_forward(q, k, v, window: int, sinks: int = 0, lengths=None, *, scale: Optional[float] = None,
+                            save: bool = False, want_cache: bool = False, y=None) -> dict:
+    """Softmax attention of q [B, T, H, d] to the visible tokens of k, v [B, Tk, Hk, d] (fp32 or bf16): token j is
+    visible to the query at position p iff j <= p and (j > p - window or j < sinks).  The queries are the last T of
+    Tk >= T tokens, query head h reads key head h Hk / H; scale is 1 / sqrt(d) unless given; lengths [B] int32 or
+    None: sequence b has lengths[b] of the Tk tokens, y is zero past them.  Returns y and, as asked, saved for
+    kla_window_attn_backward and the caches [B, sinks + window, Hk, d] with which kla_window_attn_step goes on."""
+    out = _native().window_attn_forward(q, k, v, int(window), int(sinks), lengths, scale, y, bool(save), bool(want_cache))
+    return dict(zip(("y", "saved", "cache_k", "cache_v"), out))
+
+
+def kla_window_attn_backward(q, k, v, window: int, sinks: int, lengths, y, saved, dy, *,
+                             scale: Optional[float] = None) -> dict:
+    """dq, dk, dv of kla_window_attn_forward from its y and saved (save=True) and the gradient of y."""
+    out = _native().window_attn_backward(q, k, v, int(window), int(sinks), lengths, y, saved, dy, scale)
+    return dict(zip(("dq", "dk", "dv"), out))
+
+
+def kla_window_attn_step(q, k, v, cache_k, cache_v, positions, sinks: int = 0, *, scale: Optional[float] = None,
+                         y=None) -> dict:
+    """One token for S sequences: q [S, H, d]; k, v [S, Hk, d]; the caches [S, sinks + window, Hk, d] take k and v in
+    place, at the slot of positions [S] int32 (the number of tokens before this one; a negative one: no token, y is
+    zero), and every slot that holds a token is attended to."""
+    y = _native().window_attn_step(q, k, v, cache_k, cache_v, positions, int(sinks), scale, y)
+    return {"y": y, "cache_k": cache_k, "cache_v": cache_v}
+
+
+def kla_window_attn(q, k, v, window: int, sinks: int = 0, lengths=None, *, scale: Optional[float] = None):
+    """Differentiable attention with a sliding window and sinks, as kla_window_attn_forward; returns y.  q, k and v
+    may have any strides, as parts of a fused projection do."""
+    return _native().window_attn(q, k, v, int(window), int(sinks), lengths, scale)

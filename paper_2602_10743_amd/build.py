@@ -28,7 +28,8 @@ FLAGS = [
 ]
 SOURCES = ["kla_api.cpp", "recurrent.hip", "validate.hip", "ou.hip", "pc.hip", "block.hip", "chunk_fwd.hip",
            "chunk_seg.hip", "chunk_bwd_dv.hip", "chunk_bwd_dk.hip", "chunk64.hip", "chunk64_par.hip",
-           "noalloc.hip", "mc.hip", "linattn.hip", "layernorm.hip", "logp.hip"]
+           "noalloc.hip", "mc.hip", "linattn.hip", "layernorm.hip", "logp.hip",
+           "qkrope.hip", "window.hip"]
 
 
 def _hipcc() -> str:

@@ -9,6 +9,7 @@
 // up the interpreter lock, as ctypes does: allocations and a full launch queue can block, and under
 // KLA_CHECK=1 the library waits for the stream.
 #include <array>
+#include <cmath>
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
@@ -683,6 +684,301 @@ py::object token_logp(const Tensor& x, const Tensor& target, bool want_entropy) 
     return py::make_tuple(out[0], out[1]);
 }
 
+// ---- norms of queries and keys with the rotation
+
+// q [*lead, T, H, n] (lead: at most one dimension), or [S, H, n] for one token of S sequences
+kla_rope_desc check_rope(const Tensor& q, const Tensor& k, const Opt& wq, const Opt& wk, const Opt& freq, const Opt& pos,
+                         double eps, bool interleaved, bool strided = false) {
+    check_gpu(q, "q", strided);
+    const int dt = dtype_of(q);
+    const int64_t m = q.dim();
+    if ((m != 3 && m != 4) || k.dim() != m) value_error("q must be [B, T, H, n] or [S, H, n], and k likewise");
+    const int64_t B = q.size(0), T = m == 4 ? q.size(1) : 1, H = q.size(-2), Hk = k.size(-2), n = q.size(-1);
+    std::vector<int64_t> lead(q.sizes().begin(), q.sizes().end() - 2), ks = lead;
+    ks.push_back(Hk);
+    ks.push_back(n);
+    check_like(k, ks, q, "k", strided);
+    check_f32(wq, {n}, q, "wq");
+    check_f32(wk, {n}, q, "wk");
+    check_int(pos, at::kInt, lead, q, "positions");
+    int64_t pairs = 0;
+    if (freq) {
+        pairs = freq->dim() == 1 ? freq->size(0) : -1;
+        if (pairs < 0 || freq->scalar_type() != at::kDouble || freq->device() != q.device() || !freq->is_contiguous())
+            value_error("freq must be a contiguous float64 tensor [pairs] on " + q.device().str());
+    }
+    if (m == 3 && pairs > 0 && !pos) value_error("one token of S sequences needs their positions");
+    return kla_rope_desc{int32_of(B, "B"),         int32_of(T, "T"), int32_of(H, "H"), int32_of(Hk, "Hk"), int32_of(n, "n"),
+                         int32_of(pairs, "pairs"), interleaved,      dt,               (float)eps};
+}
+
+// No sequences: nothing to do, and the weights' gradients are zero.
+Tensors rope_forward(const kla_rope_desc& d, const Tensor& q_in, const Tensor& k_in, const Opt& wq_in, const Opt& wk_in,
+                     const Opt& freq_in, const Opt& pos_in) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in);
+    const Opt wq = aligned(wq_in), wk = aligned(wk_in), freq = aligned(freq_in), pos = aligned(pos_in);
+    const Tensor oq = at::empty_like(q), ok_ = at::empty_like(k);
+    if (d.B > 0)
+        ok(kla_qk_norm_rope_forward(&d, ptr(q), ptr(k), fptr(wq), fptr(wk), (const double*)ptr(freq), (const int32_t*)ptr(pos),
+                                    ptr(oq), ptr(ok_), stream_of(q)),
+           "kla_qk_norm_rope_forward");
+    return {oq, ok_};
+}
+
+Tensors rope_backward(kla_rope_desc d, const Tensor& q_in, const Tensor& k_in, const Opt& wq_in, const Opt& wk_in,
+                      const Opt& freq_in, const Opt& pos_in, const Tensor& dq_in, const Tensor& dk_in) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in), doq = aligned(dq_in), dok = aligned(dk_in);
+    const Opt wq = aligned(wq_in), wk = aligned(wk_in), freq = aligned(freq_in), pos = aligned(pos_in);
+    const Tensor dq = at::empty_like(q), dk = at::empty_like(k);
+    Opt dwq, dwk;
+    if (wq) dwq = at::empty_like(*wq);
+    if (wk) dwk = at::empty_like(*wk);
+    if (d.B == 0) d.B = 1, d.T = 0;
+    const size_t nw = kla_qk_norm_rope_workspace(&d);
+    const Tensor ws = bytes(nw, q);
+    ok(kla_qk_norm_rope_backward(&d, ptr(q), ptr(k), fptr(wq), fptr(wk), (const double*)ptr(freq), (const int32_t*)ptr(pos),
+                                 ptr(doq), ptr(dok), ptr(dq), ptr(dk), fptr(dwq), fptr(dwk), ptr(ws), nw, stream_of(q)),
+       "kla_qk_norm_rope_backward");
+    return {dq, dk, or_undefined(dwq), or_undefined(dwk)};
+}
+
+// (q_out, k_out)
+py::object qk_norm_rope_forward(const Tensor& q, const Tensor& k, const Opt& wq, const Opt& wk, const Opt& freq, const Opt& pos,
+                                double eps, bool interleaved) {
+    const kla_rope_desc d = check_rope(q, k, wq, wk, freq, pos, eps, interleaved);
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = rope_forward(d, q, k, wq, wk, freq, pos);
+    }
+    return py::make_tuple(out[0], out[1]);
+}
+
+// (dq, dk, dwq, dwk)
+py::object qk_norm_rope_backward(const Tensor& q, const Tensor& k, const Opt& wq, const Opt& wk, const Opt& freq,
+                                 const Opt& pos, const Tensor& dq_out, const Tensor& dk_out, double eps, bool interleaved) {
+    const kla_rope_desc d = check_rope(q, k, wq, wk, freq, pos, eps, interleaved);
+    check_like(dq_out, q.sizes(), q, "dq_out");
+    check_like(dk_out, k.sizes(), q, "dk_out");
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = rope_backward(d, q, k, wq, wk, freq, pos, dq_out, dk_out);
+    }
+    return py::make_tuple(out[0], out[1], obj(some(out[2])), obj(some(out[3])));
+}
+
+struct QkNormRope : torch::autograd::Function<QkNormRope> {
+    static Tensors forward(Ctx* ctx, const Tensor& q_in, const Tensor& k_in, const Opt& wq, const Opt& wk, const Opt& freq,
+                           const Opt& pos, const kla_rope_desc& d) {
+        const Tensor q = dense(q_in), k = dense(k_in);
+        ctx->save_for_backward({q, k, or_undefined(wq), or_undefined(wk), or_undefined(freq), or_undefined(pos)});
+        ctx->set_materialize_grads(false);
+        ctx->saved_data["eps"] = (double)d.eps;
+        ctx->saved_data["interleaved"] = d.interleaved != 0;
+        return rope_forward(d, q, k, wq, wk, freq, pos);
+    }
+    static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
+        const Tensors s = ctx->get_saved_variables();
+        check_capture(s[0]);
+        const kla_rope_desc d = check_rope(s[0], s[1], some(s[2]), some(s[3]), some(s[4]), some(s[5]),
+                                           ctx->saved_data["eps"].toDouble(), ctx->saved_data["interleaved"].toBool());
+        const Tensor doq = up[0].defined() ? dense(up[0]) : at::zeros_like(s[0]);
+        const Tensor dok = up[1].defined() ? dense(up[1]) : at::zeros_like(s[1]);
+        const Tensors out = rope_backward(d, s[0], s[1], some(s[2]), some(s[3]), some(s[4]), some(s[5]), doq, dok);
+        return {out[0], out[1], out[2], out[3], Tensor(), Tensor(), Tensor()};
+    }
+};
+
+py::object qk_norm_rope(const Tensor& q, const Tensor& k, const Opt& wq, const Opt& wk, const Opt& freq, const Opt& pos,
+                        double eps, bool interleaved) {
+    const kla_rope_desc d = check_rope(q, k, wq, wk, freq, pos, eps, interleaved, true);
+    if (freq && freq->requires_grad()) value_error("freq holds constants: the frequencies take no gradient");
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = QkNormRope::apply(q, k, wq, wk, freq, pos, d);
+    }
+    return py::make_tuple(out[0], out[1]);
+}
+
+// ---- sliding-window attention
+
+float scale_of(const c10::optional<double>& scale, int64_t d) {
+    return scale ? (float)*scale : (float)(1.0 / std::sqrt((double)(d > 0 ? d : 1)));
+}
+
+kla_window_desc check_window(const Tensor& q, const Tensor& k, const Tensor& v, int64_t window, int64_t sinks, const Opt& len,
+                             const c10::optional<double>& scale, bool strided = false) {
+    check_gpu(q, "q", strided);
+    const int dt = dtype_of(q);
+    if (q.dim() != 4 || k.dim() != 4) value_error("q must be [B, T, H, d] and k [B, Tk, Hk, d]");
+    const int64_t B = q.size(0), T = q.size(1), H = q.size(2), d = q.size(3), Tk = k.size(1), Hk = k.size(2);
+    check_like(k, {B, Tk, Hk, d}, q, "k", strided);
+    check_like(v, {B, Tk, Hk, d}, q, "v", strided);
+    check_int(len, at::kInt, {B}, q, "lengths");
+    if (Tk < T) value_error("k must have at least as many tokens as q");
+    if (window < 1) value_error("window must be at least 1");
+    return kla_window_desc{int32_of(B, "B"),
+                           int32_of(T, "T"),
+                           int32_of(Tk, "Tk"),
+                           int32_of(H, "H"),
+                           int32_of(Hk, "Hk"),
+                           int32_of(d, "d"),
+                           int32_of(window, "window"),
+                           int32_of(sinks, "sinks"),
+                           dt,
+                           scale_of(scale, d)};
+}
+
+// y, saved, cache_k, cache_v
+Tensors win_forward(const kla_window_desc& d, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Opt& len_in,
+                    const Opt& y_in, bool save, bool want_cache) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in), v = aligned(v_in);
+    const Opt len = aligned(len_in);
+    const Tensor y = y_in ? *y_in : at::empty_like(q);
+    Opt saved, ck, cv, ws;
+    if (save) saved = bytes(kla_window_attn_saved_bytes(&d), q);
+    if (want_cache) {
+        ck = at::empty({d.B, (int64_t)d.sinks + d.window, d.Hk, d.d}, q.options());
+        cv = at::empty_like(*ck);
+    }
+    const size_t nw = kla_window_attn_workspace(&d);
+    if (nw) ws = bytes(nw, q);
+    ok(kla_window_attn_forward(&d, ptr(q), ptr(k), ptr(v), (const int32_t*)ptr(len), ptr(y), ptr(saved), ptr(ck), ptr(cv),
+                               ptr(ws), nw, stream_of(q)),
+       "kla_window_attn_forward");
+    return {y, or_undefined(saved), or_undefined(ck), or_undefined(cv)};
+}
+
+Tensors win_backward(const kla_window_desc& d, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Opt& len_in,
+                     const Tensor& y_in, const Tensor& saved_in, const Tensor& dy_in) {
+    const c10::hip::HIPGuard on(q_in.device().index());
+    const Tensor q = aligned(q_in), k = aligned(k_in), v = aligned(v_in), y = aligned(y_in), saved = aligned(saved_in),
+                 dy = aligned(dy_in);
+    const Opt len = aligned(len_in);
+    const Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
+    Opt ws;
+    const size_t nw = kla_window_attn_backward_workspace(&d);
+    if (nw) ws = bytes(nw, q);
+    ok(kla_window_attn_backward(&d, ptr(q), ptr(k), ptr(v), (const int32_t*)ptr(len), ptr(y), ptr(saved), ptr(dy),
+                                ptr(dq), ptr(dk), ptr(dv), ptr(ws), nw, stream_of(q)),
+       "kla_window_attn_backward");
+    return {dq, dk, dv};
+}
+
+// (y, saved, cache_k, cache_v)
+py::object window_attn_forward(const Tensor& q, const Tensor& k, const Tensor& v, int64_t window, int64_t sinks, const Opt& len,
+                               const c10::optional<double>& scale, const Opt& y_in, bool save, bool want_cache) {
+    const kla_window_desc d = check_window(q, k, v, window, sinks, len, scale);
+    if (y_in) {
+        check_like(*y_in, q.sizes(), q, "y");
+        check_apart(*y_in, "y", {&q, &k, &v});
+        if (len) check_apart(*y_in, "y", {&*len});
+    }
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = win_forward(d, q, k, v, len, y_in, save, want_cache);
+    }
+    if (y_in) changed(*y_in);
+    return py::make_tuple(out[0], obj(some(out[1])), obj(some(out[2])), obj(some(out[3])));
+}
+
+// (dq, dk, dv)
+py::object window_attn_backward(const Tensor& q, const Tensor& k, const Tensor& v, int64_t window, int64_t sinks,
+                                const Opt& len, const Tensor& y, const Tensor& saved, const Tensor& dy,
+                                const c10::optional<double>& scale) {
+    const kla_window_desc d = check_window(q, k, v, window, sinks, len, scale);
+    check_like(y, q.sizes(), q, "y");
+    check_like(dy, q.sizes(), q, "dy");
+    if (saved.scalar_type() != at::kByte || saved.device() != q.device() || !saved.is_contiguous() ||
+        (size_t)saved.numel() < kla_window_attn_saved_bytes(&d))
+        value_error("saved must be what the forward of these sizes returned");
+    Tensors out;
+    {
+        py::gil_scoped_release unlocked;
+        out = win_backward(d, q, k, v, len, y, saved, dy);
+    }
+    return py::make_tuple(out[0], out[1], out[2]);
+}
+
+struct WindowAttn : torch::autograd::Function<WindowAttn> {
+    static Tensor forward(Ctx* ctx, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Opt& len,
+                          const kla_window_desc& d) {
+        const Tensor q = dense(q_in), k = dense(k_in), v = dense(v_in);   // parts of a fused projection
+        const Tensors out = win_forward(d, q, k, v, len, c10::nullopt, true, false);
+        ctx->save_for_backward({q, k, v, or_undefined(len), out[0], out[1]});
+        ctx->saved_data["window"] = (int64_t)d.window;
+        ctx->saved_data["sinks"] = (int64_t)d.sinks;
+        ctx->saved_data["scale"] = (double)d.scale;
+        return out[0];
+    }
+    static Tensors backward(Ctx* ctx, Tensors up) {
+        once();
+        const Tensors s = ctx->get_saved_variables();
+        check_capture(s[0]);
+        const kla_window_desc d = check_window(s[0], s[1], s[2], ctx->saved_data["window"].toInt(), ctx->saved_data["sinks"].toInt(),
+                                               some(s[3]), ctx->saved_data["scale"].toDouble());
+        const Tensors out = win_backward(d, s[0], s[1], s[2], some(s[3]), s[4], s[5], dense(up[0]));
+        return {out[0], out[1], out[2], Tensor(), Tensor()};
+    }
+};
+
+Tensor window_attn(const Tensor& q, const Tensor& k, const Tensor& v, int64_t window, int64_t sinks, const Opt& len,
+                   const c10::optional<double>& scale) {
+    const kla_window_desc d = check_window(q, k, v, window, sinks, len, scale, true);
+    py::gil_scoped_release unlocked;
+    return WindowAttn::apply(q, k, v, len, d);
+}
+
+// y; the caches updated in place
+Tensor window_attn_step(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& ck, const Tensor& cv, const Tensor& pos,
+                        int64_t sinks, const c10::optional<double>& scale, const Opt& y_in) {
+    check_gpu(q, "q");
+    const int dt = dtype_of(q);
+    if (q.dim() != 3 || k.dim() != 3 || ck.dim() != 4)
+        value_error("q must be [S, H, d], k [S, Hk, d] and cache_k [S, sinks + window, Hk, d]");
+    const int64_t S = q.size(0), H = q.size(1), d = q.size(2), Hk = k.size(1), slots = ck.size(1);
+    check_like(k, {S, Hk, d}, q, "k");
+    check_like(v, {S, Hk, d}, q, "v");
+    check_like(ck, {S, slots, Hk, d}, q, "cache_k");
+    check_like(cv, {S, slots, Hk, d}, q, "cache_v");
+    check_int(pos, at::kInt, {S}, q, "positions");
+    if (sinks < 0 || slots <= sinks) value_error("the caches must have more slots than sinks");
+    for (const Tensor* c : {&ck, &cv})
+        if (reinterpret_cast<uintptr_t>(c->data_ptr()) % 16) value_error("the caches must lie on 16 bytes");
+    check_apart(ck, "cache_k", {&q, &k, &v, &pos, &cv});
+    check_apart(cv, "cache_v", {&q, &k, &v, &pos});
+    if (y_in) {
+        check_like(*y_in, {S, H, d}, q, "y");
+        check_apart(*y_in, "y", {&q, &k, &v, &pos, &ck, &cv});
+    }
+    const int32_t s32 = int32_of(S, "S"), h32 = int32_of(H, "H"), k32 = int32_of(Hk, "Hk"), d32 = int32_of(d, "d"),
+                  w32 = int32_of(slots - sinks, "window"), f32 = int32_of(sinks, "sinks");
+    Tensor y;
+    {
+        py::gil_scoped_release unlocked;
+        const c10::hip::HIPGuard on(q.device().index());
+        y = y_in ? *y_in : at::empty_like(q);
+        const Tensor qa = aligned(q), ka = aligned(k), va = aligned(v), pa = aligned(pos);
+        const size_t nw = kla_window_attn_step_workspace(s32, h32, k32, d32, w32, f32, dt);
+        Opt ws;
+        if (nw) ws = bytes(nw, q);
+        ok(kla_window_attn_step(s32, h32, k32, d32, w32, f32, dt, scale_of(scale, d), ptr(qa), ptr(ka), ptr(va),
+                                (const int32_t*)ptr(pa), ptr(ck), ptr(cv), ptr(y), ptr(ws), nw, stream_of(q)),
+           "kla_window_attn_step");
+    }
+    changed(ck);
+    changed(cv);
+    if (y_in) changed(*y_in);
+    return y;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_kla_torch, m) {
@@ -704,6 +1000,13 @@ PYBIND11_MODULE(_kla_torch, m) {
     m.def("layer_norm_backward", &layer_norm_backward);
     m.def("token_logp_forward", &token_logp_forward);
     m.def("token_logp_backward", &token_logp_backward);
+    m.def("qk_norm_rope", &qk_norm_rope);
+    m.def("qk_norm_rope_forward", &qk_norm_rope_forward);
+    m.def("qk_norm_rope_backward", &qk_norm_rope_backward);
+    m.def("window_attn", &window_attn);
+    m.def("window_attn_forward", &window_attn_forward);
+    m.def("window_attn_backward", &window_attn_backward);
+    m.def("window_attn_step", &window_attn_step);
     m.def("forward", &forward);
     m.def("backward", &backward);
     m.def("decode_step", &decode_step);

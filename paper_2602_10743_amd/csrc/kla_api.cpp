@@ -874,6 +874,149 @@ kla_status kla_token_logp_backward(int32_t S, int64_t n, int32_t V, int32_t dtyp
                : KLA_ERR_HIP;
 }
 
+// ---------------------------------------------------------------- norms of queries and keys with the rotation
+
+namespace {
+kla_status rope_desc(const kla_rope_desc* d, kla::RopeShape* s) {
+    if (!d) return KLA_ERR_NULL;
+    if (d->dtype != KLA_F32 && d->dtype != KLA_BF16) return KLA_ERR_DTYPE;
+    if (d->B < 1 || d->T < 0 || d->H < 1 || d->Hk < 1 || !width_ok(d->n)) return KLA_ERR_SHAPE;
+    if (d->pairs < 0 || d->pairs % 8 || d->pairs > d->n / 2 || (d->interleaved & ~1) || !(d->eps >= 0.f)) return KLA_ERR_SHAPE;
+    if (((int64_t)d->H + d->Hk) * d->n > 1 << 24) return KLA_ERR_SHAPE;   // offsets inside a token's rows are 32-bit
+    *s = {d->B, d->T, d->H, d->Hk, d->n, d->pairs, d->interleaved != 0, d->dtype == KLA_BF16, d->eps};
+    return KLA_OK;
+}
+}  // namespace
+
+size_t kla_qk_norm_rope_workspace(const kla_rope_desc* desc) {
+    kla::RopeShape s;
+    return rope_desc(desc, &s) == KLA_OK ? kla::rope_parts_bytes(s.n) : 0;
+}
+
+kla_status kla_qk_norm_rope_forward(const kla_rope_desc* desc, const void* q, const void* k, const float* wq,
+                                    const float* wk, const double* freq, const int32_t* positions, void* q_out,
+                                    void* k_out, hipStream_t stream) {
+    kla::RopeShape s;
+    const kla_status st = rope_desc(desc, &s);
+    if (st != KLA_OK) return st;
+    if ((s.pairs > 0 && !freq) || (s.T > 0 && (!q || !k || !q_out || !k_out))) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, (const void*)wq, (const void*)wk, (const void*)freq, (const void*)positions, q_out, k_out))
+        return KLA_ERR_ALIGN;
+    return kla::launch_rope_fwd(s, q, k, wq, wk, freq, positions, q_out, k_out, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
+kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, const void* k, const float* wq,
+                                     const float* wk, const double* freq, const int32_t* positions,
+                                     const void* dq_out, const void* dk_out, void* dq, void* dk, float* dwq, float* dwk,
+                                     void* ws, size_t ws_bytes, hipStream_t stream) {
+    kla::RopeShape s;
+    const kla_status st = rope_desc(desc, &s);
+    if (st != KLA_OK) return st;
+    if ((s.pairs > 0 && !freq) || (s.T > 0 && (!q || !k || !dq_out || !dk_out || !dq || !dk))) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, (const void*)wq, (const void*)wk, (const void*)freq, (const void*)positions, dq_out, dk_out, dq,
+                     dk, (void*)dwq, (void*)dwk, ws))
+        return KLA_ERR_ALIGN;
+    if (!ws || ws_bytes < kla::rope_parts_bytes(s.n)) return KLA_ERR_WORKSPACE;
+    return kla::launch_rope_bwd(s, q, k, wq, wk, freq, positions, dq_out, dk_out, dq, dk, dwq, dwk, static_cast<float*>(ws),
+                                stream) == hipSuccess
+               ? KLA_OK
+               : KLA_ERR_HIP;
+}
+
+// ---------------------------------------------------------------- sliding-window attention
+
+namespace {
+kla_status window_sizes(int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks, int32_t dtype) {
+    if (dtype != KLA_F32 && dtype != KLA_BF16) return KLA_ERR_DTYPE;
+    if (H < 1 || Hk < 1 || H % Hk || !width_ok(d) || window < 1 || sinks < 0 || sinks > 64) return KLA_ERR_SHAPE;
+    // offsets inside a tile of 64 rows are 32-bit, and so are slots
+    return window > (1 << 30) - sinks || (int64_t)H * d > 1 << 22 ? KLA_ERR_SHAPE : KLA_OK;
+}
+
+bool scale_ok(float scale) { return scale > 0.f && scale <= 3.4028235e38f; }
+
+kla_status window_desc(const kla_window_desc* d, kla::WinShape* s) {
+    if (!d) return KLA_ERR_NULL;
+    const kla_status st = window_sizes(d->H, d->Hk, d->d, d->window, d->sinks, d->dtype);
+    if (st != KLA_OK) return st;
+    if (d->B < 1 || d->T < 0 || d->Tk < d->T || d->Tk > 1 << 28 || !scale_ok(d->scale)) return KLA_ERR_SHAPE;
+    *s = {d->B, d->T, d->Tk, d->H, d->Hk, d->d, d->window, d->sinks, d->dtype == KLA_BF16, d->scale};
+    return kla::window_blocks(*s) >= 1 << 23 ? KLA_ERR_SHAPE : KLA_OK;   // a launch's threads are 32-bit
+}
+
+// sequences and heads of a step: a launch's threads are 32-bit
+kla_status step_desc(int32_t S, int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks, int32_t dtype,
+                     kla::StepShape* s) {
+    const kla_status st = window_sizes(H, Hk, d, window, sinks, dtype);
+    if (st != KLA_OK) return st;
+    if (S < 1 || (int64_t)S * H > 1 << 20) return KLA_ERR_SHAPE;
+    *s = {S, H, Hk, d, window, sinks, dtype == KLA_BF16, 1.f};
+    return KLA_OK;
+}
+}  // namespace
+
+size_t kla_window_attn_saved_bytes(const kla_window_desc* desc) {
+    kla::WinShape s;
+    return window_desc(desc, &s) == KLA_OK ? round_up(kla::window_saved(s)) : 0;
+}
+
+size_t kla_window_attn_workspace(const kla_window_desc* desc) {
+    kla::WinShape s;
+    return window_desc(desc, &s) == KLA_OK ? round_up(kla::window_workspace(s, false)) : 0;
+}
+
+size_t kla_window_attn_backward_workspace(const kla_window_desc* desc) {
+    kla::WinShape s;
+    return window_desc(desc, &s) == KLA_OK ? round_up(kla::window_workspace(s, true)) : 0;
+}
+
+kla_status kla_window_attn_forward(const kla_window_desc* desc, const void* q, const void* k, const void* v,
+                                   const int32_t* len, void* y, void* saved, void* cache_k, void* cache_v, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+    kla::WinShape s;
+    const kla_status st = window_desc(desc, &s);
+    if (st != KLA_OK) return st;
+    if ((s.Tk > 0 && (!k || !v)) || (s.T > 0 && (!q || !y)) || !cache_k != !cache_v) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)len, y, saved, cache_k, cache_v, ws)) return KLA_ERR_ALIGN;
+    const size_t need = kla_window_attn_workspace(desc);
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    return kla::launch_window_fwd(s, q, k, v, len, y, saved, cache_k, cache_v, ws, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
+kla_status kla_window_attn_backward(const kla_window_desc* desc, const void* q, const void* k, const void* v,
+                                    const int32_t* len, const void* y, const void* saved, const void* dy, void* dq, void* dk,
+                                    void* dv, void* ws, size_t ws_bytes, hipStream_t stream) {
+    kla::WinShape s;
+    const kla_status st = window_desc(desc, &s);
+    if (st != KLA_OK) return st;
+    if ((s.Tk > 0 && (!k || !v || !dk || !dv)) || (s.T > 0 && (!q || !y || !saved || !dy || !dq))) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)len, y, saved, dy, dq, dk, dv, ws)) return KLA_ERR_ALIGN;
+    const size_t need = kla_window_attn_backward_workspace(desc);
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    return kla::launch_window_bwd(s, q, k, v, len, y, saved, dy, dq, dk, dv, ws, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
+size_t kla_window_attn_step_workspace(int32_t S, int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks,
+                                      int32_t dtype) {
+    kla::StepShape s;
+    return step_desc(S, H, Hk, d, window, sinks, dtype, &s) == KLA_OK ? round_up(kla::window_step_workspace(s)) : 0;
+}
+
+kla_status kla_window_attn_step(int32_t S, int32_t H, int32_t Hk, int32_t d, int32_t window, int32_t sinks, int32_t dtype,
+                                float scale, const void* q, const void* k, const void* v, const int32_t* pos, void* cache_k,
+                                void* cache_v, void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
+    kla::StepShape s;
+    const kla_status st = step_desc(S, H, Hk, d, window, sinks, dtype, &s);
+    if (st != KLA_OK) return st;
+    if (!scale_ok(scale)) return KLA_ERR_SHAPE;
+    s.scale = scale;
+    if (!q || !k || !v || !pos || !cache_k || !cache_v || !y) return KLA_ERR_NULL;
+    if (!all_aligned(q, k, v, (const void*)pos, cache_k, cache_v, y, ws)) return KLA_ERR_ALIGN;
+    const size_t need = round_up(kla::window_step_workspace(s));
+    if (need > 0 && (!ws || ws_bytes < need)) return KLA_ERR_WORKSPACE;
+    return kla::launch_window_step(s, q, k, v, pos, cache_k, cache_v, y, ws, stream) == hipSuccess ? KLA_OK : KLA_ERR_HIP;
+}
+
 const char* kla_status_string(kla_status s) {
     switch (s) {
         case KLA_OK: return "KLA_OK";

@@ -191,6 +191,41 @@ hipError_t launch_logp_bwd(int S, size_t n, int V, bool bf16, const void* logits
                            const float* stat, const float* entropy, const float* dlogp, const float* dentropy,
                            void* dlogits, hipStream_t st);
 
+// Norms of queries and keys for each head with the position rotation (qkrope.hip).
+struct RopeShape {
+    int B, T, H, Hk, n, pairs;
+    bool interleaved, bf16;
+    float eps;
+};
+size_t rope_parts_bytes(int n);
+hipError_t launch_rope_fwd(const RopeShape& s, const void* q, const void* k, const float* wq, const float* wk,
+                           const double* freq, const int* pos, void* oq, void* ok, hipStream_t st);
+hipError_t launch_rope_bwd(const RopeShape& s, const void* q, const void* k, const float* wq, const float* wk,
+                           const double* freq, const int* pos, const void* doq, const void* dok, void* dq, void* dk,
+                           float* dwq, float* dwk, float* part, hipStream_t st);
+
+// Attention with a sliding window and first tokens that stay visible (window.hip).
+struct WinShape {
+    int B, T, Tk, H, Hk, d, window, sinks;
+    bool bf16;
+    float scale;
+};
+struct StepShape {
+    int S, H, Hk, d, window, sinks;
+    bool bf16;
+    float scale;
+};
+int64_t window_blocks(const WinShape& s);   // workgroups of the largest launch
+size_t window_saved(const WinShape& s);
+size_t window_workspace(const WinShape& s, bool backward);
+hipError_t launch_window_fwd(const WinShape& s, const void* q, const void* k, const void* v, const int* len, void* y,
+                             void* saved, void* ck, void* cv, void* ws, hipStream_t st);
+hipError_t launch_window_bwd(const WinShape& s, const void* q, const void* k, const void* v, const int* len, const void* y,
+                             const void* saved, const void* dy, void* dq, void* dk, void* dv, void* ws, hipStream_t st);
+size_t window_step_workspace(const StepShape& s);
+hipError_t launch_window_step(const StepShape& s, const void* q, const void* k, const void* v, const int* pos, void* ck,
+                              void* cv, void* y, void* ws, hipStream_t st);
+
 // OU gates: gradients of the parameters from the per-part gate-gradient sums (fp32
 // parts, or fp64 when part_f64)
 hipError_t launch_ou_param_grads(int H, int dk, int nparts, const void* part, bool part_f64, const float* a,

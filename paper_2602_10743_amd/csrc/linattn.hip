@@ -394,22 +394,6 @@ __device__ __forceinline__ int seq_len(const LinArgs& a, int b) {
     return a.len ? min(max(a.len[b], 0), a.T) : a.T;
 }
 
-// 16 bytes a lane from r at voff into LDS at dst + 16 lane; lanes past the buffer's end write zeros.  Not the
-// compiler's builtin, behind which every transposing read of LDS waits for all loads in flight, the prefetch
-// among them: who reads the tile waits with wait_vm_le.  Nothing is loaded into registers, and m0, the place in
-// LDS, is an operand that the compiler sets.  The wait states are those between an instruction that writes a
-// scalar register (readfirstlane, the move to m0) and a memory access that reads it, which the compiler does not
-// count inside.
-typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t words_t;
-__device__ __forceinline__ void load_lds(const words_t& r, uint32_t dst, uint32_t voff) {
-    words_t u;   // uniform: in scalar registers
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_readfirstlane(r[i]);
-    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(u),
-                 "{m0}"(__builtin_amdgcn_readfirstlane(dst))
-                 : "memory");
-}
-
 // A workgroup takes DT of the D columns, a wave CW of them and one of RS shares of the state's rows.  Where the
 // rows of Q and K are long and the waves that compute (NCW RS) few, others help with the loads.  64 columns in
 // waves of 16 with all rows take 133 registers and 45 KiB of LDS, so three workgroups of 128-wide bf16 passes

@@ -1,0 +1,1156 @@
+// Softmax attention with a sliding window and first tokens that stay visible, on matrix instructions.
+//
+//   y_i = sum_j P_ij v_j,   P_i = softmax over the visible j of scale q_i . k_j
+//
+// j is visible to the query at position p iff j <= p and (j > p - W or j < sinks).  H query heads share Hk heads
+// of keys and values.  Queries are the last T of Tk tokens; a sequence ends at len.
+//
+// Forward and dq: a wave owns 32 queries of a head, the workgroup's four 128.  Tiles of 64 tokens' keys and
+// values go through LDS, loaded a tile ahead.  Scores are formed transposed, S^T = K Q^T (tokens x queries), so
+// that a query is a lane's column: its running maximum and sum are one value a lane and one exchange between the
+// wave's halves, and S^T, rounded to the operands' type, is the operand of O^T += V^T P^T as it stands.
+//   m, l: largest score and sum of exponentials about it; O is rescaled only where a maximum grew.
+//   dS = P (dy . v - D),  D = dy . y,  dq = scale dS K
+// dk, dv: a wave owns 32 tokens and walks the queries that see them, of all heads that share them, with
+// S = Q K^T (queries x tokens) in the same way: dV^T += dy^T P, dK^T += Q^T dS.  No sum has more than one
+// writer, so results do not depend on the order of workgroups.  First tokens are seen by all later queries:
+// the queries behind the window of the first 128 tokens are cut into segments, whose sums over those tokens are
+// joined.
+//
+// v_mfma_f32_32x32x16_bf16 (lane l, half h = l / 32): A row l % 32 and B column l % 32, contraction 8 h .. 8 h + 7;
+// C column l % 32, register r at row 8 (r / 4) + 4 h + r % 4.  Over the contraction of a C used as B, half h
+// therefore has rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 of 16, and A is read with the same.  fp32:
+// v_mfma_f32_32x32x2_f32, one contraction index a half.
+//
+// bf16: q, k, v, dy are exact operands; P and dS are rounded to bf16 (as much as the rounding of the outputs, and
+// with signs that average out), while scores, maxima, sums and accumulators stay in fp32.  In rows that see few
+// tokens (fewer than kFew) little averages out, and D, which is common to a row's dS, is as large as dy . v: there P and
+// dS enter in two parts, and y is saved with 8 more bits for D.  fp32 inputs keep fp32 operands throughout.
+//
+// Not finite values: what is masked is left out by selection, but a product with a zero weight is not.  Tiles
+// that hold masked places form their product apart, and where that is not finite form it again element by
+// element without the masked places.
+#include <type_traits>
+
+#include "kla_buf.hpp"
+#include "kla_internal.hpp"
+#include "kla_mfma.hpp"
+
+namespace kla {
+namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+
+constexpr int kTile = 64;    // tokens (queries in the dk, dv pass) a tile
+constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgroup
+constexpr int kFew = 256;    // visible tokens below which a row sees few
+constexpr int kSeg = 512;    // queries a segment of the first tokens' sums
+constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which no weight is otherwise
+
+// Rows of D elements in LDS, in 16-byte pieces: piece c of row r lies at c ^ key(r), so that 8 rows read at one
+// piece, and 4 rows read across at two pieces, touch different banks.  16 columns are padded with zeros to 32.
+template <typename E, int D>
+struct Rows {
+    static constexpr int DP = D < 32 ? 32 : D, NC = DP * (int)sizeof(E) / 16, NR = D * (int)sizeof(E) / 16;
+    static constexpr int BYTES = kTile * NC * 16;
+    __device__ static int key(int r) {
+        return NC >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : (r & 2) | ((r >> 2) & 1);
+    }
+    __device__ static int piece(int r, int c) { return r * NC * 16 + ((c ^ key(r)) << 4); }
+    __device__ static int at(int r, int col) {
+        constexpr int PER = 16 / (int)sizeof(E);
+        return piece(r, col / PER) + (col % PER) * (int)sizeof(E);
+    }
+};
+
+// C tiles over the columns of a row, 32 each
+template <typename E, int D>
+using Acc = f32x16[Rows<E, D>::DP / 32];
+
+// What rounding to bf16 left of four values, in 1/254 of each one's last place: with it D = dy . y has 16 bits of
+// y.  D is common to a row's dS = P (dy . v - D); where a row sees few tokens it is as large as dy . v, and y's
+// rounding alone would be as much as that of dS.
+__device__ __forceinline__ uint32_t rest_of(const float (&x)[4], const uint2& y) {
+    const uint32_t b[4] = {y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u};
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float per = __uint_as_float(0x7f000000u - (b[e] & 0x7f800000u));   // 1 / its power of two
+        const float q = fminf(fmaxf((x[e] - __uint_as_float(b[e])) * per * (254.f * 128.f), -127.f), 127.f);
+        w |= ((uint32_t)(int)rintf(q) & 0xffu) << (8 * e);
+    }
+    return w;
+}
+__device__ __forceinline__ float rest_add(float y, uint32_t w, int e) {
+    const float unit = __uint_as_float(__float_as_uint(y) & 0x7f800000u);
+    return fmaf((float)(int8_t)(w >> (8 * e)), unit * (1.f / (254.f * 128.f)), y);
+}
+
+// One row of a lane (A's or B's 32 rows): half h has every second piece.
+template <typename E, int D>
+struct Row;
+template <int D>
+struct Row<uint16_t, D> {
+    static constexpr int K = D / 16;
+    bf16x8 x[K];
+    __device__ void load(const void* p, bool live, int h) {   // p: the row
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            x[k] = __builtin_bit_cast(bf16x8, live ? reinterpret_cast<const uint4*>(p)[2 * k + h] : uint4{0, 0, 0, 0});
+    }
+    __device__ float dot(const Row& y, const int8_t* rest, int h) const {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const uint2 w = rest ? *reinterpret_cast<const uint2*>(rest + 16 * k + 8 * h) : uint2{0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fmaf((float)x[k][e], rest_add((float)y.x[k][e], e < 4 ? w.x : w.y, e % 4), s);
+        }
+        return s;
+    }
+};
+template <int D>
+struct Row<float, D> {
+    static constexpr int K = D / 8;
+    f32x4 x[K];
+    __device__ void load(const void* p, bool live, int h) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) x[k] = live ? reinterpret_cast<const f32x4*>(p)[2 * k + h] : zero4();
+    }
+    __device__ float dot(const Row& y, const int8_t*, int) const {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = fmaf(x[k][e], y.x[k][e], s);
+        return s;
+    }
+};
+
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+
+// C = (rows row0 .. row0 + 31 of the tile) (row b of each lane)^T
+template <int D>
+__device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const Row<uint16_t, D>& b, int l32, int h) {
+    f32x16 c = zero16();
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const bf16x8 a = __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const uint4*>(t + Rows<uint16_t, D>::piece(row0 + l32, 2 * k + h)));
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.x[k], c, 0, 0, 0);
+    }
+    return c;
+}
+template <int D>
+__device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const Row<float, D>& b, int l32, int h) {
+    f32x16 c = zero16();
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(t + Rows<float, D>::piece(row0 + l32, 2 * k + h));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b.x[k][e], c, 0, 0, 0);
+    }
+    return c;
+}
+
+// Weights of 32 rows (a C, register r at row 8 (r / 4) + 4 h + r % 4) as the operand of a product over them.
+template <typename E>
+struct Weights;
+template <>
+struct Weights<uint16_t> {
+    bf16x8 b[2];
+    __device__ explicit Weights(const f32x16& w) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            b[k] = __builtin_bit_cast(bf16x8, uint4{cvt_pk_bf16(w[8 * k], w[8 * k + 1]), cvt_pk_bf16(w[8 * k + 2], w[8 * k + 3]),
+                                                    cvt_pk_bf16(w[8 * k + 4], w[8 * k + 5]),
+                                                    cvt_pk_bf16(w[8 * k + 6], w[8 * k + 7])});
+    }
+};
+template <>
+struct Weights<float> {
+    const f32x16& w;
+    __device__ explicit Weights(const f32x16& w) : w(w) {}
+};
+
+// c += (columns 32 t .. 32 t + 31 of rows row0 .. row0 + 31)^T w
+template <int D>
+__device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int t, const Weights<uint16_t>& w, f32x16 c,
+                                           int l32, int h) {
+    using R = Rows<uint16_t, D>;
+    const int s = l32 & 15, col = 32 * t + (l32 & 16) + 4 * (s & 3);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = row0 + 16 * k + 4 * h + (s >> 2);
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(x + R::at(r, col)));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(x + R::at(r + 8, col)));
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), w.b[k], c, 0, 0, 0);
+    }
+    return c;
+}
+template <int D>
+__device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int t, const Weights<float>& w, f32x16 c,
+                                           int l32, int h) {
+    using R = Rows<float, D>;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const float a = *reinterpret_cast<const float*>(x + R::at(row0 + 8 * (r / 4) + 4 * h + r % 4, 32 * t + l32));
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], c, 0, 0, 0);
+    }
+    return c;
+}
+
+__device__ __forceinline__ float elem(const unsigned char* p, uint16_t) {
+    return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p));
+}
+__device__ __forceinline__ float elem(const unsigned char* p, float) { return *reinterpret_cast<const float*>(p); }
+
+// The same element by element, without the rows whose weight is masked: for values that are not finite.
+// scratch: 512 floats of the wave's own.
+template <typename E, int D>
+__device__ __forceinline__ f32x16 cols_apart(const unsigned char* x, int row0, int t, const f32x16& w, float* scratch, int l32,
+                                             int h) {
+    f32x16 c = zero16();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) scratch[((e & 4) * 2 + 4 * h + (e & 3)) * 32 + l32] = w[8 * k + e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            const float f = scratch[i * 32 + l32];
+            if (__float_as_uint(f) == kMasked) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                c[r] = fmaf(f, elem(x + Rows<E, D>::at(row0 + 16 * k + i, 32 * t + 8 * (r / 4) + 4 * h + r % 4), E{}), c[r]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    return c;
+}
+
+// What the operands' rounding left of the weights.
+__device__ __forceinline__ f32x16 left_of(const f32x16& w, const Weights<uint16_t>& b) {
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = w[r] - (float)b.b[r / 8][r % 8];
+    return x;
+}
+
+// o += (rows row0 .. row0 + 31)^T w.  masked: some weights are, and values that are not finite must not reach them.
+// two: bf16 weights enter in two parts.
+template <typename E, int D>
+__device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, bool masked, bool two,
+                                         float* scratch, int l32, int h) {
+    const Weights<E> b(w);
+    if (!masked && !two) {
+#pragma unroll
+        for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, b, o[t], l32, h);
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < Rows<E, D>::DP / 32; ++t) {
+        f32x16 c = cols_dot<D>(x, row0, t, b, zero16(), l32, h);
+        if constexpr (sizeof(E) == 2) {
+            if (two) c = cols_dot<D>(x, row0, t, Weights<E>(left_of(w, b)), c, l32, h);
+        }
+        float top = 0.f;   // NaN where one of c is not finite
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top += c[r] * 0.f;
+        if (masked && __any(!(top == 0.f))) c = cols_apart<E, D>(x, row0, t, w, scratch, l32, h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] += c[r];
+    }
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+struct WinArgs {
+    const void *q, *k, *v, *y, *dy;
+    void *o, *dq, *dk, *dv;   // o: y of the forward
+    const int* len;
+    float2* stat;             // [B, T, H]: largest score times log2(e) scale, sum of exponentials about it
+    int8_t* rest;             // [B, R, H, D]: what the rounding of y to bf16 left (rest_of)
+    float* part;              // forward: partial O [nsplit][B T H][D]; dk, dv: the first tokens' sums
+    float2* pstat;            // forward: [nsplit][B T H]
+    float* rows;              // backward: [3][B H][T64] m, 1 / l, D
+    int B, T, Tk, H, Hk, W, sinks, blocks, nsplit, nseg, T64, R;
+    float scale, c;           // c = scale log2(e)
+    bool few;                 // rows see few tokens
+};
+
+// Workgroups go around the chip's 8 dies: a run of neighbours, which read the same keys, on one of them.
+__device__ __forceinline__ int block_of(int n) {
+    const int per = (n + 7) / 8;
+    return (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+}
+
+__device__ __forceinline__ int end_of(const WinArgs& a, int b) {
+    return a.len ? min(max(a.len[b], 0), a.Tk) : a.Tk;
+}
+
+// A tile of kTile rows from row r0 on of `rows` into LDS, by the four waves; rows past them are zero.
+template <typename E, int D>
+struct Loader {
+    using R = Rows<E, D>;
+    static constexpr int N = kTile * R::NC / 64 / 4;   // loads a wave
+    uint32_t off[N];
+    uint32_t stride;
+    __device__ Loader(uint32_t stride, int wave, int lane) : stride(stride) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = (i * 4 + wave) * 64 + lane, r = x / R::NC, c = (x % R::NC) ^ R::key(r);
+            off[i] = c < R::NR ? r * stride + c * 16 : 0x80000000u;
+        }
+    }
+    __device__ void load(const void* base, int r0, int rows, uint32_t dst, int wave) const {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(base) + (size_t)r0 * stride;
+        const int n = min(rows - r0, kTile);
+        const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, n > 0 ? (uint32_t)(n - 1) * stride + D * (uint32_t)sizeof(E) : 0u,
+                         0x00020000u};
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_lds(rs, dst + (uint32_t)(i * 4 + wave) * 1024, off[i]);
+    }
+};
+
+__device__ __forceinline__ uint32_t lds_of(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p;
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, const float (&x)[4], int8_t* rest) {
+    const uint2 y{cvt_pk_bf16(x[0], x[1]), cvt_pk_bf16(x[2], x[3])};
+    *reinterpret_cast<uint2*>(p) = y;
+    if (rest) *reinterpret_cast<uint32_t*>(rest) = rest_of(x, y);
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4], int8_t*) {
+    *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
+}
+
+// A lane's column of a C over columns 32 t + 8 (r / 4) + 4 h + r % 4 of row p, 16 or 8 bytes at a time.
+template <typename E, int D>
+__device__ __forceinline__ void store_row(E* p, const Acc<E, D>& o, float f, int h, int8_t* rest = nullptr) {
+#pragma unroll
+    for (int t = 0; t < Rows<E, D>::DP / 32; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = 32 * t + 8 * j;
+            if (col >= D) continue;
+            const float x[4] = {o[t][4 * j] * f, o[t][4 * j + 1] * f, o[t][4 * j + 2] * f, o[t][4 * j + 3] * f};
+            store4(p + col + 4 * h, x, rest ? rest + col + 4 * h : nullptr);
+        }
+}
+template <typename E, int D>
+__device__ __forceinline__ void store_zero(E* p, int h) {
+#pragma unroll
+    for (int c = 0; c < D * (int)sizeof(E) / 32; ++c) reinterpret_cast<uint4*>(p)[2 * c + h] = uint4{0, 0, 0, 0};
+}
+
+// The tiles that a workgroup of queries p0 .. p1 reads: the window's, after the first tokens' where they lie apart.
+struct Tiles {
+    int t0, n;
+    bool lead;
+    __device__ Tiles(const WinArgs& a, int p0, int p1) {
+        t0 = max(0, p0 - a.W + 1) / kTile;
+        lead = t0 > 0 && a.sinks > 0;
+        n = p1 / kTile - t0 + 1 + (lead ? 1 : 0);
+    }
+    __device__ int operator[](int i) const { return lead ? (i == 0 ? 0 : t0 + i - 1) : t0 + i; }
+};
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(WinArgs a) {
+    using R = Rows<E, D>;
+    constexpr int DT = R::DP / 32;
+    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
+    __shared__ float scratch[4][512];
+    int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
+    const int split = id % a.nsplit;
+    id /= a.nsplit;
+    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
+    const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
+    const int qi = q0 + 32 * wave + l32, pos = past + qi;
+    const bool live = qi < a.T && pos < end;
+    const size_t row = ((size_t)b * a.T + min(qi, a.T - 1)) * a.H + head;
+    const uint32_t stride = (uint32_t)(a.Hk * D * (int)sizeof(E));
+    const E* kb = (const E*)a.k + ((size_t)b * a.Tk * a.Hk + kh) * D;
+    const E* vb = (const E*)a.v + ((size_t)b * a.Tk * a.Hk + kh) * D;
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = zero16();
+    float mx = -INFINITY, mc = -INFINITY, l = 0.f;   // largest score, times c, and the lane's share of the sum
+    if (p1 >= p0) {
+        const Tiles tiles(a, p0, p1);
+        const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
+        const Loader<E, D> ld(stride, wave, lane);
+        const uint32_t lds0 = lds_of(sm);
+        auto issue = [&](int i) {
+            const int r0 = tiles[i] * kTile;
+            const uint32_t to = lds0 + (uint32_t)((i - i0) & 1) * 2 * R::BYTES;
+            ld.load(kb, r0, end, to, wave);
+            ld.load(vb, r0, end, to + R::BYTES, wave);
+        };
+        if (i0 < i1) issue(i0);
+        Row<E, D> q;
+        q.load((const E*)a.q + row * D, live, h);
+        const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);   // the wave's positions
+        const bool two = a.few || w0 < kRows;
+        for (int i = i0; i < i1; ++i) {
+            wait_vm_all();
+            barrier_lds();
+            if (i + 1 < i1) issue(i + 1);
+            const unsigned char *K = sm[(i - i0) & 1], *V = K + R::BYTES;
+            const int j0 = tiles[i] * kTile;
+            if (j0 > w1 || w1 < w0 || (j0 + kTile - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
+            const bool masked = j0 + kTile - 1 > w0 || j0 <= w1 - a.W;
+            f32x16 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) s[u] = rows_dot<D>(K, 32 * u, q, l32, h);
+            if (masked) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4;
+                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[u][r] = -INFINITY;
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+            top = fmaxf(top, other_half(top));
+            if (__any(top > mx)) {
+                mx = fmaxf(mx, top);
+                const float now = mx == -INFINITY ? -INFINITY : mx * a.c;
+                const float f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
+                mc = now;
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[t][r] *= f;
+            }
+            const float base = mc == -INFINITY ? 0.f : mc;   // nothing visible yet: weights 2^-inf
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
+                    l += s[u][r];
+                }
+            if (masked) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4;
+                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[u][r] = __uint_as_float(kMasked);
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) add_cols<E, D>(o, V, 32 * u, s[u], masked, two, scratch[wave], l32, h);
+        }
+        l += other_half(l);
+    }
+    if (qi >= a.T) return;
+    if (a.nsplit > 1) {
+        const size_t at = (size_t)split * a.B * a.T * a.H + row;
+        if (!live) l = 0.f, mc = -INFINITY;
+        if (live) store_row<float, D>(a.part + at * D, o, 1.f, h);
+        if (h == 0) a.pstat[at] = float2{mc, l};
+        return;
+    }
+    E* y = (E*)a.o + row * D;
+    if (live && l != 0.f)
+        store_row<E, D>(y, o, 1.f / l, h, qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr);
+    else
+        store_zero<E, D>(y, h);
+    if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc, l} : float2{0.f, 0.f};
+}
+
+// Joins nsplit partial rows: y = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Four columns a thread.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void win_join_kernel(size_t rows, int nsplit, const float* __restrict__ part,
+                                                       const float2* __restrict__ pstat, E* __restrict__ y,
+                                                       float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
+                                                       int R) {
+    const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, row = x / (D / 4);
+    const int col = (int)(x % (D / 4)) * 4;
+    if (row >= rows) return;
+    float m = -INFINITY;
+    for (int s = 0; s < nsplit; ++s) m = fmaxf(m, pstat[s * rows + row].x);
+    float l = 0.f;
+    f32x4 o = zero4();
+    for (int s = 0; s < nsplit; ++s) {
+        const float2 st = pstat[s * rows + row];
+        if (st.y == 0.f) continue;
+        const float f = exp2_hw(st.x - m);
+        l = fmaf(f, st.y, l);
+        const f32x4 p = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * D + col);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(f, p[e], o[e]);
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const float x4[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+    const int qi = R > 0 ? (int)(row / H % T) : 0;
+    store4(y + row * D + col, x4, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + col : nullptr);
+    if (stat && col == 0) stat[row] = l != 0.f ? float2{m, l} : float2{0.f, 0.f};
+}
+
+// The ring caches after the last token of each sequence: slot < sinks holds that token, slot sinks + x the last
+// token t >= sinks with (t - sinks) mod W = x; slots without a token are zero.  16 bytes a thread.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void win_cache_kernel(WinArgs a, uint4* __restrict__ ck, uint4* __restrict__ cv) {
+    const int per = a.Hk * D * (int)sizeof(E) / 16, slots = a.sinks + a.W;
+    const size_t n = (size_t)a.B * slots * per;
+    for (size_t x = (size_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (size_t)gridDim.x * 256) {
+        const int c = (int)(x % per), slot = (int)(x / per % slots), b = (int)(x / per / slots), end = end_of(a, b);
+        int tok = slot;
+        if (slot >= a.sinks && end - 1 > slot) tok = end - 1 - (end - 1 - slot) % a.W;
+        const bool held = tok < end;
+        const size_t at = ((size_t)b * a.Tk + (held ? tok : 0)) * per + c;
+        ck[x] = held ? ((const uint4*)a.k)[at] : uint4{0, 0, 0, 0};
+        cv[x] = held ? ((const uint4*)a.v)[at] : uint4{0, 0, 0, 0};
+    }
+}
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(WinArgs a) {
+    using R = Rows<E, D>;
+    constexpr int DT = R::DP / 32;
+    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
+    __shared__ float scratch[4][512];
+    const int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
+    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
+    const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
+    const int qi = q0 + 32 * wave + l32, pos = past + qi;
+    const bool live = qi < a.T && pos < end;
+    const size_t row = ((size_t)b * a.T + min(qi, a.T - 1)) * a.H + head;
+    const uint32_t stride = (uint32_t)(a.Hk * D * (int)sizeof(E));
+    const E* kb = (const E*)a.k + ((size_t)b * a.Tk * a.Hk + kh) * D;
+    const E* vb = (const E*)a.v + ((size_t)b * a.Tk * a.Hk + kh) * D;
+    E* dq = (E*)a.dq + row * D;
+    const size_t nrow = (size_t)a.B * a.H * a.T64, at = ((size_t)b * a.H + head) * a.T64 + qi;
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = zero16();
+    if (p1 >= p0) {
+        const Tiles tiles(a, p0, p1);
+        const Loader<E, D> ld(stride, wave, lane);
+        const uint32_t lds0 = lds_of(sm);
+        auto issue = [&](int i) {
+            const int r0 = tiles[i] * kTile;
+            const uint32_t to = lds0 + (uint32_t)(i & 1) * 2 * R::BYTES;
+            ld.load(kb, r0, end, to, wave);
+            ld.load(vb, r0, end, to + R::BYTES, wave);
+        };
+        issue(0);
+        Row<E, D> q, g;
+        q.load((const E*)a.q + row * D, live, h);
+        g.load((const E*)a.dy + row * D, live, h);
+        float Dq;
+        {
+            Row<E, D> y;
+            y.load((const E*)a.y + row * D, live, h);
+            Dq = g.dot(y, live && qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr, h);
+            Dq += other_half(Dq);
+        }
+        const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
+        const float li = st.y == 0.f ? 0.f : 1.f / st.y;
+        if (h == 0 && qi < a.T64) {
+            a.rows[at] = st.x;
+            a.rows[nrow + at] = li;
+            a.rows[2 * nrow + at] = Dq;
+        }
+        const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);
+        const bool two = a.few || w0 < kRows;
+        for (int i = 0; i < tiles.n; ++i) {
+            wait_vm_all();
+            barrier_lds();
+            if (i + 1 < tiles.n) issue(i + 1);
+            const unsigned char *K = sm[i & 1], *V = K + R::BYTES;
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+                const int j0 = tiles[i] * kTile + 32 * u;
+                if (j0 > w1 || w1 < w0 || (j0 + 31 <= w0 - a.W && j0 >= a.sinks)) continue;
+                const bool masked = j0 + 31 > w0 || j0 <= w1 - a.W;
+                f32x16 s = rows_dot<D>(K, 32 * u, q, l32, h);
+                const f32x16 dp = rows_dot<D>(V, 32 * u, g, l32, h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * li * (dp[r] - Dq);
+                if (masked) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 8 * (r / 4) + 4 * h + r % 4;
+                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[r] = __uint_as_float(kMasked);
+                    }
+                }
+                add_cols<E, D>(o, K, 32 * u, s, masked, two, scratch[wave], l32, h);
+            }
+        }
+    } else if (h == 0 && qi < a.T64) {
+        a.rows[at] = a.rows[nrow + at] = a.rows[2 * nrow + at] = 0.f;
+    }
+    if (qi >= a.T) return;
+    if (live)
+        store_row<E, D>(dq, o, a.scale, h);
+    else
+        store_zero<E, D>(dq, h);
+}
+
+// dk, dv.  Workgroup (b, kh, kb): 128 tokens; after those, nseg segments of the queries behind the first 128 tokens'
+// window for each (b, kh), whose waves take (32 of the first tokens, every second 32 queries).
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
+    using R = Rows<E, D>;
+    constexpr int DT = R::DP / 32;
+    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
+    __shared__ __align__(16) float srow[2][3][kTile];
+    __shared__ float scratch[4][512];
+    int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
+    const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
+    const int job = id % per, bk = id / per, kh = bk % a.Hk, b = bk / a.Hk;
+    const bool seg = job >= nk;
+    const int k0 = seg ? 0 : job * kRows, w0 = k0 + 32 * (seg ? wave / 2 : wave);   // the wave's first token
+    const int G = a.H / a.Hk, past = a.Tk - a.T, end = end_of(a, b);
+    const int tok = w0 + l32;
+    const bool live = tok < end;
+    // positions of the queries: those that the window reaches, or a segment of those behind
+    const int behind = max(past, kRows - 1 + min(a.W, a.Tk));
+    const int plo = seg ? behind + (job - nk) * kSeg : max(past, k0);
+    const int phi = min(seg ? plo + kSeg - 1 : k0 + kRows - 2 + min(a.W, a.Tk), end - 1);
+    const bool works = !seg || w0 < a.sinks;
+
+    f32x16 ok[DT], ov[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) ok[t] = ov[t] = zero16();
+    if (phi >= plo) {
+        const size_t krow = ((size_t)b * a.Tk + min(tok, a.Tk - 1)) * a.Hk + kh;
+        const uint32_t stride = (uint32_t)(a.H * D * (int)sizeof(E));
+        const Loader<E, D> ld(stride, wave, lane);
+        const uint32_t lds0 = lds_of(sm), srow0 = lds_of(srow);
+        const int t0 = (plo - past) / kTile, nt = (phi - past) / kTile - t0 + 1, n = nt * G;
+        const size_t nrow = (size_t)a.B * a.H * a.T64;
+        auto issue = [&](int i) {
+            const int head = kh * G + i / nt, r0 = (t0 + i % nt) * kTile;
+            const uint32_t to = lds0 + (uint32_t)(i & 1) * 2 * R::BYTES;
+            const size_t first = ((size_t)b * a.T * a.H + head) * D;
+            ld.load((const E*)a.q + first, r0, end - past, to, wave);
+            ld.load((const E*)a.dy + first, r0, end - past, to + R::BYTES, wave);
+            if (wave < 3) {   // m, 1 / l or D of the tile's rows: 16 lanes' pieces
+                const uintptr_t p = reinterpret_cast<uintptr_t>(a.rows + wave * nrow + ((size_t)b * a.H + head) * a.T64 + r0);
+                const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, kTile * 4u, 0x00020000u};
+                if (lane < 16) load_lds(rs, srow0 + (uint32_t)((i & 1) * 3 + wave) * kTile * 4, (uint32_t)lane * 16);
+            }
+        };
+        issue(0);
+        Row<E, D> k, v;
+        k.load((const E*)a.k + krow * D, live, h);
+        v.load((const E*)a.v + krow * D, live, h);
+        for (int i = 0; i < n; ++i) {
+            wait_vm_all();
+            barrier_lds();
+            if (i + 1 < n) issue(i + 1);
+            const unsigned char *Q = sm[i & 1], *G_ = Q + R::BYTES;
+            const int pt = past + (t0 + i % nt) * kTile;
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+                const int pp = pt + 32 * u;   // the rows' first position
+                if (!works || (seg && u != wave % 2) || pp + 31 < max(w0, plo) || pp > phi ||
+                    (pp - a.W >= w0 + 31 && w0 >= a.sinks))
+                    continue;
+                const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
+                const bool two = a.few || pp < kRows;
+                f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
+                const float* sr = &srow[i & 1][0][32 * u];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 m = *reinterpret_cast<const f32x4*>(sr + 8 * j + 4 * h);
+                    const f32x4 li = *reinterpret_cast<const f32x4*>(sr + kTile + 8 * j + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
+                }
+                if (masked) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int p = pp + 8 * (r / 4) + 4 * h + r % 4;
+                        if (!(tok <= p && (tok > p - a.W || tok < a.sinks) && p >= plo && p <= phi))
+                            s[r] = __uint_as_float(kMasked);
+                    }
+                }
+                add_cols<E, D>(ov, G_, 32 * u, s, masked, two, scratch[wave], l32, h);
+                const f32x16 dp = rows_dot<D>(G_, 32 * u, v, l32, h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 Dq = *reinterpret_cast<const f32x4*>(sr + 2 * kTile + 8 * j + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 4 * j + e;
+                        s[r] = masked && __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * (dp[r] - Dq[e]);
+                    }
+                }
+                add_cols<E, D>(ok, Q, 32 * u, s, masked, two, scratch[wave], l32, h);
+            }
+        }
+    }
+    if (a.nseg > 0 && k0 == 0 && w0 < a.sinks) {   // the first tokens' sums: slot 0 the window's, 1 + 2 s + (0, 1) a segment's
+        const int slot = seg ? 1 + 2 * (job - nk) + wave % 2 : 0;
+        if (tok < a.sinks) {
+            float* p = a.part + (((size_t)bk * (1 + 2 * a.nseg) + slot) * 2 * a.sinks + tok) * D;
+            store_row<float, D>(p, ok, a.scale, h);
+            store_row<float, D>(p + (size_t)a.sinks * D, ov, 1.f, h);
+        }
+        if (tok < a.sinks) return;
+    }
+    if (seg || tok >= a.Tk) return;
+    const size_t krow = ((size_t)b * a.Tk + tok) * a.Hk + kh;
+    E *dk = (E*)a.dk + krow * D, *dv = (E*)a.dv + krow * D;
+    if (live) {
+        store_row<E, D>(dk, ok, a.scale, h);
+        store_row<E, D>(dv, ov, 1.f, h);
+    } else {
+        store_zero<E, D>(dk, h);
+        store_zero<E, D>(dv, h);
+    }
+}
+
+// dk, dv of the first tokens: their slots added up in order, four columns a thread.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void win_first_kernel(WinArgs a) {
+    const int n = min(a.sinks, a.Tk), slots = 1 + 2 * a.nseg;
+    const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, total = (size_t)a.B * a.Hk * 2 * n * (D / 4);
+    if (x >= total) return;
+    const int col = (int)(x % (D / 4)) * 4, tok = (int)(x / (D / 4) % n), of = (int)(x / (D / 4) / n % 2);
+    const int bk = (int)(x / (D / 4) / n / 2), kh = bk % a.Hk, b = bk / a.Hk;
+    f32x4 s = zero4();
+    for (int i = 0; i < slots; ++i)
+        s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
+    E* p = (E*)(of ? a.dv : a.dk) + (((size_t)b * a.Tk + tok) * a.Hk + kh) * D + col;
+    if constexpr (sizeof(E) == 2)
+        *reinterpret_cast<uint2*>(p) = uint2{cvt_pk_bf16(s[0], s[1]), cvt_pk_bf16(s[2], s[3])};
+    else
+        *reinterpret_cast<float4*>(p) = float4{s[0], s[1], s[2], s[3]};
+}
+
+// ---------------------------------------------------------------- one token for S sequences
+
+struct StepArgs {
+    const void *q, *k, *v;
+    void *ck, *cv, *y;
+    const int* pos;
+    float* part;
+    float2* pstat;
+    int S, H, Hk, W, sinks, blocks, nsplit, groups;
+    float c;
+};
+
+// Workgroup (s, kh, 16 query heads, split): its waves take chunks of 32 (fp32: 16) slots in turn and join at the
+// end.  K goes from memory straight into operands, V through LDS of the wave's own, to be read across.
+// S^T = K Q^T (slots x heads) in 16 x 16 tiles, O^T += V^T P^T.
+template <typename E, int D>
+struct StepCfg {
+    static constexpr int CH = sizeof(E) == 2 ? 32 : 16, DP = D < 16 ? 16 : D, DT = D / 16;
+    static constexpr int NC = D * (int)sizeof(E) / 16;                       // pieces a row
+    static constexpr int NK = sizeof(E) == 2 ? (D + 31) / 32 : D / 16;       // pieces of a lane's row of K
+    static constexpr int NL = (CH * NC + 63) / 64;                           // loads of a chunk of V
+    static constexpr int VB = CH * NC * 16 > D * 64 ? CH * NC * 16 : D * 64;  // V's chunk, later O [D][16]
+};
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
+    using C = StepCfg<E, D>;
+    __shared__ __align__(16) unsigned char sv[4][C::VB];
+    __shared__ float2 sst[4][16];
+    int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l16 = lane % 16, g4 = lane / 16;
+    const int split = id % a.nsplit;
+    id /= a.nsplit;
+    const int hg = id % a.groups, kh = id / a.groups % a.Hk, s = id / a.groups / a.Hk;
+    const int G = a.H / a.Hk, slots = a.sinks + a.W, pos = a.pos[s];
+    const int held = pos < 0 ? 0 : min(pos, slots - 1) + 1;
+    const int now = pos < a.sinks ? pos : a.sinks + (pos - a.sinks) % a.W;   // the new token's slot
+    const int nch = (held + C::CH - 1) / C::CH, per = (nch + a.nsplit - 1) / a.nsplit;
+    const int c0 = split * per, c1 = min(c0 + per, nch);
+    const int hq = hg * 16 + l16;   // the lane's query head of those that share kh
+    const size_t qrow = (size_t)s * a.H + kh * G + min(hq, G - 1);
+    const size_t first = ((size_t)s * slots * a.Hk + kh) * D, rowlen = (size_t)a.Hk * D;
+    const E *nk = (const E*)a.k + ((size_t)s * a.Hk + kh) * D, *nv = (const E*)a.v + ((size_t)s * a.Hk + kh) * D;
+    E *ck = (E*)a.ck + first, *cv = (E*)a.cv + first;
+    unsigned char* V = sv[wave];
+    auto key = [](int r) { return C::NC >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : C::NC >= 4 ? (r & 2) | ((r >> 2) & 1) : 0; };
+
+    uint4 qf[C::NK];
+#pragma unroll
+    for (int k = 0; k < C::NK; ++k)
+        qf[k] = hq < G && 4 * k + g4 < C::NC ? reinterpret_cast<const uint4*>((const E*)a.q + qrow * D)[4 * k + g4] : uint4{0, 0, 0, 0};
+    f32x4 o[C::DT];
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) o[t] = zero4();
+    float mx = -INFINITY, mc = -INFINITY, l = 0.f;
+
+    constexpr int RT = C::CH / 16;
+    uint4 kf[2][RT][C::NK], vf[2][C::NL];
+    auto load = [&](int c, uint4 (&kk)[RT][C::NK], uint4 (&vv)[C::NL]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int j = c * C::CH + 16 * t + l16;
+            const E* p = j == now || j >= held ? nk : ck + j * rowlen;
+#pragma unroll
+            for (int k = 0; k < C::NK; ++k)
+                kk[t][k] = 4 * k + g4 < C::NC ? reinterpret_cast<const uint4*>(p)[4 * k + g4] : uint4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < C::NL; ++i) {
+            const int x = i * 64 + lane, j = c * C::CH + x / C::NC;
+            const E* p = j == now || j >= held ? nv : cv + j * rowlen;
+            vv[i] = reinterpret_cast<const uint4*>(p)[x % C::NC];
+        }
+    };
+    auto work = [&](int c, const uint4 (&kk)[RT][C::NK], const uint4 (&vv)[C::NL]) {
+        const int j0 = c * C::CH;
+        // V into LDS, zero where no token is; the new token into the caches, by the one workgroup that has its slot
+#pragma unroll
+        for (int i = 0; i < C::NL; ++i) {
+            const int x = i * 64 + lane, r = x / C::NC, p = x % C::NC;
+            if (r < C::CH)
+                *reinterpret_cast<uint4*>(V + (r * C::NC + (p ^ key(r))) * 16) = j0 + r < held ? vv[i] : uint4{0, 0, 0, 0};
+            if (hg == 0 && r < C::CH && j0 + r == now) reinterpret_cast<uint4*>(cv + (j0 + r) * rowlen)[p] = vv[i];
+        }
+        if (hg == 0) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                if (j0 + 16 * t + l16 == now) {
+#pragma unroll
+                    for (int k = 0; k < C::NK; ++k)
+                        if (4 * k + g4 < C::NC) reinterpret_cast<uint4*>(ck + now * rowlen)[4 * k + g4] = kk[t][k];
+                }
+        }
+        f32x4 sc[RT];
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            f32x4 x = zero4();
+#pragma unroll
+            for (int k = 0; k < C::NK; ++k) {
+                if constexpr (sizeof(E) == 2) {
+                    x = mfma_bf16(__builtin_bit_cast(bf16x8, kk[t][k]), __builtin_bit_cast(bf16x8, qf[k]), x);
+                } else {
+                    const f32x4 p = __builtin_bit_cast(f32x4, kk[t][k]), q = __builtin_bit_cast(f32x4, qf[k]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(p[e], q[e], x, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (j0 + 16 * t + 4 * g4 + r >= held) x[r] = -INFINITY;
+                top = fmaxf(top, x[r]);
+            }
+            sc[t] = x;
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > mx)) {
+            mx = fmaxf(mx, top);
+            const float next = mx == -INFINITY ? -INFINITY : mx * a.c;
+            const float f = next == -INFINITY ? 0.f : exp2_hw(mc - next);
+            mc = next;
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < C::DT; ++t) o[t] *= f;
+        }
+        const float base = mc == -INFINITY ? 0.f : mc;
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                sc[t][r] = exp2_hw(fmaf(sc[t][r], a.c, -base));
+                l += sc[t][r];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if constexpr (sizeof(E) == 2) {
+            const bf16x8 w = __builtin_bit_cast(bf16x8, uint4{cvt_pk_bf16(sc[0][0], sc[0][1]), cvt_pk_bf16(sc[0][2], sc[0][3]),
+                                                              cvt_pk_bf16(sc[1][0], sc[1][1]), cvt_pk_bf16(sc[1][2], sc[1][3])});
+#pragma unroll
+            for (int t = 0; t < C::DT; ++t) {
+                const int r = 4 * g4 + (l16 >> 2), col = 16 * t + 4 * (l16 & 3);
+                auto at = [&](int r) { return V + (r * C::NC + ((col / 8) ^ key(r))) * 16 + (col % 8) * 2; };
+                const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)at(r));
+                const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)at(r + 16));
+                o[t] = mfma_bf16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), w, o[t]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 4 * g4 + r, col = 16 * t + l16;
+                    const float x = *reinterpret_cast<const float*>(V + (row * C::NC + ((col / 4) ^ key(row))) * 16 + (col % 4) * 4);
+                    o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, sc[0][r], o[t], 0, 0, 0);
+                }
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    // two chunks in registers: the next is on its way while one is worked on
+    int c = c0 + wave;
+    if (c < c1) load(c, kf[0], vf[0]);
+    for (; c < c1; c += 8) {
+        if (c + 4 < c1) load(c + 4, kf[1], vf[1]);
+        work(c, kf[0], vf[0]);
+        if (c + 4 >= c1) break;
+        if (c + 8 < c1) load(c + 8, kf[0], vf[0]);
+        work(c + 4, kf[1], vf[1]);
+    }
+    // the waves' maxima and sums, and their O about the common maximum
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g4 == 0) sst[wave][l16] = float2{mc, l};
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, sst[w][l16].x);
+    const float f = mc == -INFINITY ? 0.f : exp2_hw(mc - m);
+    float* O = reinterpret_cast<float*>(V);   // [D][16]
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) O[(16 * t + 4 * g4 + r) * 16 + l16] = mc == -INFINITY ? 0.f : o[t][r] * f;
+    __syncthreads();
+    const int nh = min(16, G - hg * 16);
+    for (int x = threadIdx.x; x < nh * D; x += 256) {
+        const int hh = x / D, d = x % D;
+        float sum = 0.f, tot = 0.f, mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            sum += reinterpret_cast<const float*>(sv[w])[d * 16 + hh];
+            mm = fmaxf(mm, sst[w][hh].x);
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 st = sst[w][hh];
+            if (st.y != 0.f) tot = fmaf(exp2_hw(st.x - mm), st.y, tot);
+        }
+        const size_t row = (size_t)s * a.H + kh * G + hg * 16 + hh;
+        if (a.nsplit > 1) {
+            const size_t at = (size_t)split * a.S * a.H + row;
+            a.part[at * D + d] = sum;
+            if (d == 0) a.pstat[at] = float2{mm, tot};
+        } else {
+            const float r = tot == 0.f ? 0.f : sum / tot;
+            if constexpr (sizeof(E) == 2)
+                ((uint16_t*)a.y)[row * D + d] = f32_to_bf16(r);
+            else
+                ((float*)a.y)[row * D + d] = r;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- launches
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Whether every row sees few tokens.  Else those at the first kRows positions are taken as such.
+bool sees_few(const WinShape& s) {
+    return ((int64_t)s.window + s.sinks < s.Tk ? (int64_t)s.window + s.sinks : s.Tk) < kFew;
+}
+
+// Rows of a sequence, from the first on, whose y is saved with 8 more bits (bf16).
+int rest_rows(const WinShape& s) {
+    const int first = s.Tk - s.T < kRows ? kRows - (s.Tk - s.T) : 0;
+    return !s.bf16 ? 0 : sees_few(s) || first > s.T ? s.T : first;
+}
+
+WinArgs args_of(const WinShape& s, const void* q, const void* k, const void* v, const int* len) {
+    WinArgs a{};
+    a.q = q, a.k = k, a.v = v, a.len = len;
+    a.B = s.B, a.T = s.T, a.Tk = s.Tk, a.H = s.H, a.Hk = s.Hk;
+    a.W = s.window < s.Tk ? s.window : (s.Tk > 0 ? s.Tk : 1);
+    a.sinks = s.sinks, a.scale = s.scale, a.c = s.scale * 1.4426950408889634f;
+    a.nsplit = 1, a.few = sees_few(s);
+    a.T64 = (s.T + kTile - 1) / kTile * kTile;
+    return a;
+}
+
+// The saved context: stat, then the rest of y.
+void with_saved(const WinShape& s, WinArgs& a, void* saved) {
+    a.stat = static_cast<float2*>(saved);
+    a.rest = static_cast<int8_t*>(saved) + align256((size_t)s.B * s.T * s.H * sizeof(float2));
+    a.R = rest_rows(s);
+}
+
+unsigned grid_of(int64_t blocks) { return (unsigned)((blocks + 7) / 8 * 8); }
+
+// Tiles of keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least
+// two tiles to each.
+int splits(const WinShape& s) {
+    const int64_t blocks = (int64_t)s.B * s.H * ((s.T + kRows - 1) / kRows);
+    const int64_t reach = (int64_t)s.window + kRows < s.Tk ? (int64_t)s.window + kRows : s.Tk;
+    const int64_t tiles = (reach + kTile - 1) / kTile + (s.sinks > 0);
+    int64_t n = blocks > 0 ? 512 / blocks : 1;
+    if (n > tiles / 2) n = tiles / 2;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+int segments(const WinShape& s) {
+    if (s.sinks == 0) return 0;
+    const int64_t W = s.window < s.Tk ? s.window : s.Tk, past = s.Tk - s.T;
+    const int64_t behind = past > kRows - 1 + W ? past : kRows - 1 + W, n = s.Tk - behind;
+    return n > 0 ? (int)((n + kSeg - 1) / kSeg) : 0;
+}
+
+template <typename E, int D>
+hipError_t fwd(const WinShape& s, WinArgs a, void* ck, void* cv, hipStream_t st) {
+    if (a.T > 0) {
+        hipLaunchKernelGGL((win_fwd_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
+        if (a.nsplit > 1) {
+            const size_t rows = (size_t)a.B * a.T * a.H;
+            hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
+                               a.nsplit, a.part, a.pstat, (E*)a.o, a.stat, a.rest, a.T, a.H, a.R);
+        }
+    }
+    if (ck) {
+        WinArgs c = a;
+        c.W = s.window;
+        const size_t n = (size_t)s.B * (s.sinks + (size_t)s.window) * s.Hk * D * sizeof(E) / 16;
+        hipLaunchKernelGGL((win_cache_kernel<E, D>), dim3((unsigned)(n / 256 + 1 < 8192 ? n / 256 + 1 : 8192)), dim3(256), 0, st, c,
+                           (uint4*)ck, (uint4*)cv);
+    }
+    return hipGetLastError();
+}
+
+template <typename E, int D>
+hipError_t bwd(WinArgs a, hipStream_t st) {
+    const int nq = (a.T + kRows - 1) / kRows, nk = (a.Tk + kRows - 1) / kRows;
+    if (nk == 0) return hipSuccess;
+    a.blocks = a.B * a.H * nq;
+    if (a.blocks > 0) hipLaunchKernelGGL((win_dq_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
+    a.blocks = a.B * a.Hk * (nk + a.nseg);
+    hipLaunchKernelGGL((win_dkv_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
+    if (a.nseg > 0) {
+        const size_t n = (size_t)a.B * a.Hk * 2 * (a.sinks < a.Tk ? a.sinks : a.Tk) * (D / 4);
+        hipLaunchKernelGGL((win_first_kernel<E, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+template <typename F>
+hipError_t by_type(bool bf16, int d, F&& f) {
+    switch (d) {
+        case 16: return bf16 ? f(uint16_t{}, std::integral_constant<int, 16>{}) : f(float{}, std::integral_constant<int, 16>{});
+        case 32: return bf16 ? f(uint16_t{}, std::integral_constant<int, 32>{}) : f(float{}, std::integral_constant<int, 32>{});
+        case 64: return bf16 ? f(uint16_t{}, std::integral_constant<int, 64>{}) : f(float{}, std::integral_constant<int, 64>{});
+        case 128: return bf16 ? f(uint16_t{}, std::integral_constant<int, 128>{}) : f(float{}, std::integral_constant<int, 128>{});
+    }
+    return hipErrorInvalidValue;
+}
+
+int step_groups(const StepShape& s) { return (s.H / s.Hk + 15) / 16; }
+
+// Slots are dealt to several workgroups where sequences and heads are too few for four workgroups a CU, at
+// least two chunks to a wave.
+int step_splits(const StepShape& s) {
+    const int64_t blocks = (int64_t)s.S * s.Hk * step_groups(s);
+    const int64_t chunks = ((int64_t)s.window + s.sinks + (s.bf16 ? 31 : 15)) / (s.bf16 ? 32 : 16);
+    int64_t n = 1024 / blocks;
+    if (n > chunks / 8) n = chunks / 8;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+}  // namespace
+
+int64_t window_blocks(const WinShape& s) {
+    const int64_t nq = ((int64_t)s.T + kRows - 1) / kRows, nk = ((int64_t)s.Tk + kRows - 1) / kRows;
+    const int64_t fwd = (int64_t)s.B * s.H * nq, dkv = (int64_t)s.B * s.Hk * (nk + segments(s));
+    return fwd > dkv ? fwd : dkv;
+}
+
+size_t window_saved(const WinShape& s) {
+    return align256((size_t)s.B * s.T * s.H * sizeof(float2)) + (size_t)s.B * rest_rows(s) * s.H * s.d;
+}
+
+size_t window_workspace(const WinShape& s, bool backward) {
+    const size_t rows = (size_t)s.B * s.T * s.H;
+    if (!backward) {
+        const int n = splits(s);
+        return n > 1 ? align256(n * rows * s.d * sizeof(float)) + n * rows * sizeof(float2) : 0;
+    }
+    const size_t t64 = (size_t)(s.T + kTile - 1) / kTile * kTile;
+    const size_t first = (size_t)s.B * s.Hk * (1 + 2 * (size_t)segments(s)) * 2 * s.sinks * s.d * sizeof(float);
+    return align256(3 * s.B * s.H * t64 * sizeof(float)) + (segments(s) > 0 ? first : 0);
+}
+
+hipError_t launch_window_fwd(const WinShape& s, const void* q, const void* k, const void* v, const int* len, void* y,
+                             void* saved, void* ck, void* cv, void* ws, hipStream_t st) {
+    WinArgs a = args_of(s, q, k, v, len);
+    a.o = y;
+    if (saved) with_saved(s, a, saved);
+    a.nsplit = splits(s);
+    const size_t rows = (size_t)s.B * s.T * s.H;
+    if (a.nsplit > 1) {
+        a.part = static_cast<float*>(ws);
+        a.pstat = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(a.nsplit * rows * s.d * sizeof(float)));
+    }
+    a.blocks = s.B * s.H * ((s.T + kRows - 1) / kRows) * a.nsplit;
+    return by_type(s.bf16, s.d, [&](auto e, auto d) { return fwd<decltype(e), decltype(d)::value>(s, a, ck, cv, st); });
+}
+
+hipError_t launch_window_bwd(const WinShape& s, const void* q, const void* k, const void* v, const int* len, const void* y,
+                             const void* saved, const void* dy, void* dq, void* dk, void* dv, void* ws, hipStream_t st) {
+    WinArgs a = args_of(s, q, k, v, len);
+    a.y = y, a.dy = dy, a.dq = dq, a.dk = dk, a.dv = dv;
+    with_saved(s, a, const_cast<void*>(saved));
+    a.rows = static_cast<float*>(ws);
+    a.nseg = segments(s);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(3 * (size_t)s.B * s.H * a.T64 * sizeof(float)));
+    return by_type(s.bf16, s.d, [&](auto e, auto d) { return bwd<decltype(e), decltype(d)::value>(a, st); });
+}
+
+size_t window_step_workspace(const StepShape& s) {
+    const int n = step_splits(s);
+    const size_t rows = (size_t)s.S * s.H;
+    return n > 1 ? align256(n * rows * s.d * sizeof(float)) + n * rows * sizeof(float2) : 0;
+}
+
+hipError_t launch_window_step(const StepShape& s, const void* q, const void* k, const void* v, const int* pos, void* ck,
+                              void* cv, void* y, void* ws, hipStream_t st) {
+    StepArgs a{};
+    a.q = q, a.k = k, a.v = v, a.pos = pos, a.ck = ck, a.cv = cv, a.y = y;
+    a.S = s.S, a.H = s.H, a.Hk = s.Hk, a.W = s.window, a.sinks = s.sinks;
+    a.nsplit = step_splits(s), a.groups = step_groups(s), a.c = s.scale * 1.4426950408889634f;
+    a.blocks = s.S * s.Hk * a.groups * a.nsplit;
+    const size_t rows = (size_t)s.S * s.H;
+    if (a.nsplit > 1) {
+        a.part = static_cast<float*>(ws);
+        a.pstat = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(a.nsplit * rows * s.d * sizeof(float)));
+    }
+    return by_type(s.bf16, s.d, [&](auto e, auto dd) {
+        using E = decltype(e);
+        constexpr int D = decltype(dd)::value;
+        hipLaunchKernelGGL((win_step_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
+        if (a.nsplit > 1)
+            hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
+                               a.nsplit, a.part, a.pstat, (E*)a.y, (float2*)nullptr, (int8_t*)nullptr, 1, a.H, 0);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace kla
