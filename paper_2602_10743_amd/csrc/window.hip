@@ -27,9 +27,9 @@
 // tokens (fewer than kFew) little averages out, and D, which is common to a row's dS, is as large as dy . v: there P and
 // dS enter in two parts, and y is saved with 8 more bits for D.  fp32 inputs keep fp32 operands throughout.
 //
-// Not finite values: what is masked is left out by selection, but a product with a zero weight is not.  Tiles
-// that hold masked places form their product apart, and where that is not finite form it again element by
-// element without the masked places.
+// Values that are not finite: scores of masked places are left out by selection, but the products with a zero weight
+// are not, and an infinity or NaN there would reach rows that do not see it.  So a workgroup whose sums are not finite
+// walks its tiles once more, its products element by element without the masked places.
 #include <type_traits>
 
 #include "kla_buf.hpp"
@@ -210,12 +210,10 @@ __device__ __forceinline__ float elem(const unsigned char* p, uint16_t) {
 }
 __device__ __forceinline__ float elem(const unsigned char* p, float) { return *reinterpret_cast<const float*>(p); }
 
-// The same element by element, without the rows whose weight is masked: for values that are not finite.
-// scratch: 512 floats of the wave's own.
+// The same element by element, without the rows whose weight is masked.  scratch: 512 floats of the wave's own.
 template <typename E, int D>
-__device__ __forceinline__ f32x16 cols_apart(const unsigned char* x, int row0, int t, const f32x16& w, float* scratch, int l32,
-                                             int h) {
-    f32x16 c = zero16();
+__device__ __forceinline__ void cols_apart(f32x16& c, const unsigned char* x, int row0, int t, const f32x16& w, float* scratch,
+                                           int l32, int h) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -232,7 +230,6 @@ __device__ __forceinline__ f32x16 cols_apart(const unsigned char* x, int row0, i
         }
         __builtin_amdgcn_wave_barrier();
     }
-    return c;
 }
 
 // What the operands' rounding left of the weights.
@@ -243,30 +240,45 @@ __device__ __forceinline__ f32x16 left_of(const f32x16& w, const Weights<uint16_
     return x;
 }
 
-// o += (rows row0 .. row0 + 31)^T w.  masked: some weights are, and values that are not finite must not reach them.
-// two: bf16 weights enter in two parts.
-template <typename E, int D>
-__device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, bool masked, bool two,
-                                         float* scratch, int l32, int h) {
-    const Weights<E> b(w);
-    if (!masked && !two) {
+// o += (rows row0 .. row0 + 31)^T w.  two: bf16 weights enter in two parts.
+template <bool CAREFUL, typename E, int D>
+__device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, bool two, float* scratch,
+                                         int l32, int h) {
+    if constexpr (CAREFUL) {
+#pragma unroll
+        for (int t = 0; t < Rows<E, D>::DP / 32; ++t) cols_apart<E, D>(o[t], x, row0, t, w, scratch, l32, h);
+    } else {
+        const Weights<E> b(w);
 #pragma unroll
         for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, b, o[t], l32, h);
-        return;
-    }
-#pragma unroll
-    for (int t = 0; t < Rows<E, D>::DP / 32; ++t) {
-        f32x16 c = cols_dot<D>(x, row0, t, b, zero16(), l32, h);
         if constexpr (sizeof(E) == 2) {
-            if (two) c = cols_dot<D>(x, row0, t, Weights<E>(left_of(w, b)), c, l32, h);
+            if (two) {
+                const Weights<E> rest(left_of(w, b));
+#pragma unroll
+                for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, rest, o[t], l32, h);
+            }
         }
-        float top = 0.f;   // NaN where one of c is not finite
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top += c[r] * 0.f;
-        if (masked && __any(!(top == 0.f))) c = cols_apart<E, D>(x, row0, t, w, scratch, l32, h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] += c[r];
     }
+}
+
+template <int N>
+__device__ __forceinline__ bool finite(const f32x16 (&o)[N]) {
+    float z = 0.f;   // NaN where one is not
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z = fmaf(o[t][r], 0.f, z);
+    return z == 0.f;
+}
+
+// Whether any thread of the workgroup says so.  Orders LDS before and after.
+__device__ __forceinline__ bool any_of(bool x, int* flag) {
+    __syncthreads();
+    if (threadIdx.x == 0) *flag = 0;
+    __syncthreads();
+    if (x) *flag = 1;
+    __syncthreads();
+    return *flag != 0;
 }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -290,6 +302,12 @@ struct WinArgs {
 __device__ __forceinline__ int block_of(int n) {
     const int per = (n + 7) / 8;
     return (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+}
+
+// Whether token j is visible to the query at position p.  Without branches: selections of single registers of a
+// matrix tile by control flow have come out wrong (the compiler lost the copy of a branch's tile), and cost more.
+__device__ __forceinline__ bool visible(const WinArgs& a, int j, int p) {
+    return (j <= p) & ((j > p - a.W) | (j < a.sinks));
 }
 
 __device__ __forceinline__ int end_of(const WinArgs& a, int b) {
@@ -370,6 +388,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
     constexpr int DT = R::DP / 32;
     __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
     __shared__ float scratch[4][512];
+    __shared__ int flag;
     int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
@@ -388,7 +407,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
     f32x16 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
-    float mx = -INFINITY, mc = -INFINITY, l = 0.f;   // largest score, times c, and the lane's share of the sum
+    float mc = -INFINITY, l = 0.f;   // largest score times c, and the lane's share of the sum
     if (p1 >= p0) {
         const Tiles tiles(a, p0, p1);
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
@@ -400,67 +419,75 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
             ld.load(kb, r0, end, to, wave);
             ld.load(vb, r0, end, to + R::BYTES, wave);
         };
-        if (i0 < i1) issue(i0);
         Row<E, D> q;
         q.load((const E*)a.q + row * D, live, h);
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);   // the wave's positions
         const bool two = a.few || w0 < kRows;
-        for (int i = i0; i < i1; ++i) {
-            wait_vm_all();
-            barrier_lds();
-            if (i + 1 < i1) issue(i + 1);
-            const unsigned char *K = sm[(i - i0) & 1], *V = K + R::BYTES;
-            const int j0 = tiles[i] * kTile;
-            if (j0 > w1 || w1 < w0 || (j0 + kTile - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
-            const bool masked = j0 + kTile - 1 > w0 || j0 <= w1 - a.W;
-            f32x16 s[2];
+        auto sees = [&](int j) { return visible(a, j, pos); };
+        auto walk = [&](auto careful) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            constexpr int U = CAREFUL ? 1 : 2;   // 32 tokens each at once
+            float mx = -INFINITY;
+            if (i0 < i1) issue(i0);
+            for (int i = i0; i < i1; ++i) {
+                wait_vm_all();
+                barrier_lds();
+                if (i + 1 < i1) issue(i + 1);
+                const unsigned char *K = sm[(i - i0) & 1], *V = K + R::BYTES;
+#pragma unroll 1
+                for (int u0 = 0; u0 < kTile; u0 += 32 * U) {
+                    const int j0 = tiles[i] * kTile + u0;
+                    if (j0 > w1 || w1 < w0 || (j0 + 32 * U - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
+                    const bool masked = j0 + 32 * U - 1 > w0 || j0 <= w1 - a.W;
+                    f32x16 s[U];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] = rows_dot<D>(K, 32 * u, q, l32, h);
-            if (masked) {
+                    for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
+                    if (masked) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                        for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4;
-                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[u][r] = -INFINITY;
+                            for (int r = 0; r < 16; ++r)
+                                s[u][r] = sees(j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4) ? s[u][r] : -INFINITY;
                     }
-            }
-            float top = s[0][0];
+                    float top = s[0][0];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-            top = fmaxf(top, other_half(top));
-            if (__any(top > mx)) {
-                mx = fmaxf(mx, top);
-                const float now = mx == -INFINITY ? -INFINITY : mx * a.c;
-                const float f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
-                mc = now;
-                l *= f;
+                        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+                    top = fmaxf(top, other_half(top));
+                    if (__any(top > mx)) {
+                        mx = fmaxf(mx, top);
+                        const float now = mx == -INFINITY ? -INFINITY : mx * a.c;
+                        const float f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
+                        mc = now;
+                        l *= f;
 #pragma unroll
-                for (int t = 0; t < DT; ++t)
+                        for (int t = 0; t < DT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[t][r] *= f;
-            }
-            const float base = mc == -INFINITY ? 0.f : mc;   // nothing visible yet: weights 2^-inf
+                            for (int r = 0; r < 16; ++r) o[t][r] *= f;
+                    }
+                    const float base = mc == -INFINITY ? 0.f : mc;   // nothing visible yet: weights 2^-inf
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
-                    l += s[u][r];
+                        for (int r = 0; r < 16; ++r) {
+                            s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
+                            l += s[u][r];
+                            if constexpr (CAREFUL)
+                                s[u][r] = sees(j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4) ? s[u][r] : __uint_as_float(kMasked);
+                        }
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        add_cols<CAREFUL, E, D>(o, V, u0 + 32 * u, s[u], two, scratch[wave], l32, h);
                 }
-            if (masked) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4;
-                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[u][r] = __uint_as_float(kMasked);
-                    }
             }
+        };
+        walk(std::false_type{});
+        if (any_of(live && !finite(o), &flag)) {
+            mc = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) add_cols<E, D>(o, V, 32 * u, s[u], masked, two, scratch[wave], l32, h);
+            for (int t = 0; t < DT; ++t) o[t] = zero16();
+            walk(std::true_type{});
         }
         l += other_half(l);
     }
@@ -532,6 +559,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
     constexpr int DT = R::DP / 32;
     __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
     __shared__ float scratch[4][512];
+    __shared__ int flag;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
@@ -560,7 +588,6 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
             ld.load(kb, r0, end, to, wave);
             ld.load(vb, r0, end, to + R::BYTES, wave);
         };
-        issue(0);
         Row<E, D> q, g;
         q.load((const E*)a.q + row * D, live, h);
         g.load((const E*)a.dy + row * D, live, h);
@@ -580,29 +607,37 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
         }
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);
         const bool two = a.few || w0 < kRows;
-        for (int i = 0; i < tiles.n; ++i) {
-            wait_vm_all();
-            barrier_lds();
-            if (i + 1 < tiles.n) issue(i + 1);
-            const unsigned char *K = sm[i & 1], *V = K + R::BYTES;
+        auto walk = [&](auto careful) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            issue(0);
+            for (int i = 0; i < tiles.n; ++i) {
+                wait_vm_all();
+                barrier_lds();
+                if (i + 1 < tiles.n) issue(i + 1);
+                const unsigned char *K = sm[i & 1], *V = K + R::BYTES;
 #pragma unroll 1
-            for (int u = 0; u < 2; ++u) {
-                const int j0 = tiles[i] * kTile + 32 * u;
-                if (j0 > w1 || w1 < w0 || (j0 + 31 <= w0 - a.W && j0 >= a.sinks)) continue;
-                const bool masked = j0 + 31 > w0 || j0 <= w1 - a.W;
-                f32x16 s = rows_dot<D>(K, 32 * u, q, l32, h);
-                const f32x16 dp = rows_dot<D>(V, 32 * u, g, l32, h);
+                for (int u = 0; u < 2; ++u) {
+                    const int j0 = tiles[i] * kTile + 32 * u;
+                    if (j0 > w1 || w1 < w0 || (j0 + 31 <= w0 - a.W && j0 >= a.sinks)) continue;
+                    const bool masked = j0 + 31 > w0 || j0 <= w1 - a.W;
+                    f32x16 s = rows_dot<D>(K, 32 * u, q, l32, h);
+                    const f32x16 dp = rows_dot<D>(V, 32 * u, g, l32, h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * li * (dp[r] - Dq);
-                if (masked) {
+                    for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * li * (dp[r] - Dq);
+                    if (masked) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 8 * (r / 4) + 4 * h + r % 4;
-                        if (!(j <= pos && (j > pos - a.W || j < a.sinks))) s[r] = __uint_as_float(kMasked);
+                        for (int r = 0; r < 16; ++r)
+                            s[r] = visible(a, j0 + 8 * (r / 4) + 4 * h + r % 4, pos) ? s[r] : __uint_as_float(kMasked);
                     }
+                    add_cols<CAREFUL, E, D>(o, K, 32 * u, s, two, scratch[wave], l32, h);
                 }
-                add_cols<E, D>(o, K, 32 * u, s, masked, two, scratch[wave], l32, h);
             }
+        };
+        walk(std::false_type{});
+        if (any_of(live && !finite(o), &flag)) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] = zero16();
+            walk(std::true_type{});
         }
     } else if (h == 0 && qi < a.T64) {
         a.rows[at] = a.rows[nrow + at] = a.rows[2 * nrow + at] = 0.f;
@@ -623,6 +658,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
     __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
     __shared__ __align__(16) float srow[2][3][kTile];
     __shared__ float scratch[4][512];
+    __shared__ int flag;
     int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
@@ -661,54 +697,62 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
                 if (lane < 16) load_lds(rs, srow0 + (uint32_t)((i & 1) * 3 + wave) * kTile * 4, (uint32_t)lane * 16);
             }
         };
-        issue(0);
         Row<E, D> k, v;
         k.load((const E*)a.k + krow * D, live, h);
         v.load((const E*)a.v + krow * D, live, h);
-        for (int i = 0; i < n; ++i) {
-            wait_vm_all();
-            barrier_lds();
-            if (i + 1 < n) issue(i + 1);
-            const unsigned char *Q = sm[i & 1], *G_ = Q + R::BYTES;
-            const int pt = past + (t0 + i % nt) * kTile;
+        auto walk = [&](auto careful) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            issue(0);
+            for (int i = 0; i < n; ++i) {
+                wait_vm_all();
+                barrier_lds();
+                if (i + 1 < n) issue(i + 1);
+                const unsigned char *Q = sm[i & 1], *G_ = Q + R::BYTES;
+                const int pt = past + (t0 + i % nt) * kTile;
 #pragma unroll 1
-            for (int u = 0; u < 2; ++u) {
-                const int pp = pt + 32 * u;   // the rows' first position
-                if (!works || (seg && u != wave % 2) || pp + 31 < max(w0, plo) || pp > phi ||
-                    (pp - a.W >= w0 + 31 && w0 >= a.sinks))
-                    continue;
-                const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
-                const bool two = a.few || pp < kRows;
-                f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
-                const float* sr = &srow[i & 1][0][32 * u];
+                for (int u = 0; u < 2; ++u) {
+                    const int pp = pt + 32 * u;   // the rows' first position
+                    if (!works || (seg && u != wave % 2) || pp + 31 < max(w0, plo) || pp > phi ||
+                        (pp - a.W >= w0 + 31 && w0 >= a.sinks))
+                        continue;
+                    const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
+                    const bool two = a.few || pp < kRows;
+                    f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
+                    const float* sr = &srow[i & 1][0][32 * u];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 m = *reinterpret_cast<const f32x4*>(sr + 8 * j + 4 * h);
-                    const f32x4 li = *reinterpret_cast<const f32x4*>(sr + kTile + 8 * j + 4 * h);
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 m = *reinterpret_cast<const f32x4*>(sr + 8 * j + 4 * h);
+                        const f32x4 li = *reinterpret_cast<const f32x4*>(sr + kTile + 8 * j + 4 * h);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
-                }
-                if (masked) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int p = pp + 8 * (r / 4) + 4 * h + r % 4;
-                        if (!(tok <= p && (tok > p - a.W || tok < a.sinks) && p >= plo && p <= phi))
-                            s[r] = __uint_as_float(kMasked);
+                        for (int e = 0; e < 4; ++e) s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
                     }
-                }
-                add_cols<E, D>(ov, G_, 32 * u, s, masked, two, scratch[wave], l32, h);
-                const f32x16 dp = rows_dot<D>(G_, 32 * u, v, l32, h);
+                    if (masked) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 Dq = *reinterpret_cast<const f32x4*>(sr + 2 * kTile + 8 * j + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * j + e;
-                        s[r] = masked && __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * (dp[r] - Dq[e]);
+                        for (int r = 0; r < 16; ++r) {
+                            const int p = pp + 8 * (r / 4) + 4 * h + r % 4;
+                            s[r] = (visible(a, tok, p) & (p >= plo) & (p <= phi)) ? s[r] : __uint_as_float(kMasked);
+                        }
                     }
+                    add_cols<CAREFUL, E, D>(ov, G_, 32 * u, s, two, scratch[wave], l32, h);
+                    const f32x16 dp = rows_dot<D>(G_, 32 * u, v, l32, h);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 Dq = *reinterpret_cast<const f32x4*>(sr + 2 * kTile + 8 * j + 4 * h);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int r = 4 * j + e;
+                            s[r] = __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * (dp[r] - Dq[e]);
+                        }
+                    }
+                    add_cols<CAREFUL, E, D>(ok, Q, 32 * u, s, two, scratch[wave], l32, h);
                 }
-                add_cols<E, D>(ok, Q, 32 * u, s, masked, two, scratch[wave], l32, h);
             }
+        };
+        walk(std::false_type{});
+        if (any_of(live && !(finite(ok) && finite(ov)), &flag)) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) ok[t] = ov[t] = zero16();
+            walk(std::true_type{});
         }
     }
     if (a.nseg > 0 && k0 == 0 && w0 < a.sinks) {   // the first tokens' sums: slot 0 the window's, 1 + 2 s + (0, 1) a segment's
@@ -861,7 +905,7 @@ __global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (j0 + 16 * t + 4 * g4 + r >= held) x[r] = -INFINITY;
+                x[r] = j0 + 16 * t + 4 * g4 + r >= held ? -INFINITY : x[r];
                 top = fmaxf(top, x[r]);
             }
             sc[t] = x;
