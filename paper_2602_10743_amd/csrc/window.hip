@@ -9,7 +9,7 @@
 // values go through LDS, loaded a tile ahead.  Scores are formed transposed, S^T = K Q^T (tokens x queries), so
 // that a query is a lane's column: its running maximum and sum are one value a lane and one exchange between the
 // wave's halves, and S^T, rounded to the operands' type, is the operand of O^T += V^T P^T as it stands.
-//   m, l: largest score and sum of exponentials about it; O is rescaled only where a maximum grew.
+//   m, l: a reference near the largest score and the sum of exponentials about it.
 //   dS = P (dy . v - D),  D = dy . y,  dq = scale dS K
 // dk, dv: a wave owns 32 tokens and walks the queries that see them, of all heads that share them, with
 // S = Q K^T (queries x tokens) in the same way: dV^T += dy^T P, dK^T += Q^T dS.  No sum has more than one
@@ -43,23 +43,49 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
 constexpr int kTile = 64;    // tokens (queries in the dk, dv pass) a tile
 constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgroup
+// The exponents' reference lies this far above the largest score (times c, rounded up) that moved it: weights are at
+// most 1, and a row is rescaled only when a score passes the reference, not whenever the maximum grows, which one of
+// a wave's 32 rows does in nearly every tile.  The backward takes it lower by as much (a whole number, exactly), with
+// the sum multiplied accordingly: small weights then end where exp2's range does below the largest, not 2^8 above.
+constexpr float kAhead = 8.f, kAheadExp = 256.f;
 constexpr int kFew = 256;    // visible tokens below which a row sees few
 constexpr int kSeg = 512;    // queries a segment of the first tokens' sums
 constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which no weight is otherwise
 
-// Rows of D elements in LDS, in 16-byte pieces: piece c of row r lies at c ^ key(r), so that 8 rows read at one
-// piece, and 4 rows read across at two pieces, touch different banks.  16 columns are padded with zeros to 32.
+// Rows of D elements in LDS, in 16-byte pieces: piece c of row r lies at c ^ key(r), so that 16 rows read at one
+// piece, 4 rows of bf16 read across at four pieces, and rows of fp32 read across at eight, 4 rows apart, touch
+// different columns of 64 banks.  256-byte rows of bf16 have every four of them 16 bytes further on instead of half
+// of the key: reads then need four addresses a lane, and constant offsets, instead of eight.  16 columns are
+// padded with zeros to 32.
 template <typename E, int D>
 struct Rows {
     static constexpr int DP = D < 32 ? 32 : D, NC = DP * (int)sizeof(E) / 16, NR = D * (int)sizeof(E) / 16;
-    static constexpr int BYTES = kTile * NC * 16;
+    static constexpr bool APART = sizeof(E) == 2 && NC == 16;
+    static constexpr int UNIT = 1024 + (APART ? 16 : 0);   // bytes of a wave's load, 1024 / (16 NC) rows
+    static constexpr int BYTES = kTile * NC / 64 * UNIT;
     __device__ static int key(int r) {
-        return NC >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : (r & 2) | ((r >> 2) & 1);
+        if (APART) return (r & 3) << 2;
+        if (sizeof(E) == 4) return NC >= 16 ? ((r & 4) << 1) | ((r & 8) >> 1) | (r & 3) : (r >> 1) & 7;
+        return NC == 8 ? ((r & 2) << 1) | ((r >> 2) & 3) : (r >> 2) & 3;
     }
-    __device__ static int piece(int r, int c) { return r * NC * 16 + ((c ^ key(r)) << 4); }
+    __device__ static int row(int r) { return r * NC * 16 + (APART ? (r >> 2) * 16 : 0); }
     __device__ static int at(int r, int col) {
         constexpr int PER = 16 / (int)sizeof(E);
-        return piece(r, col / PER) + (col % PER) * (int)sizeof(E);
+        return row(r) + (((col / PER) ^ key(r)) << 4) + (col % PER) * (int)sizeof(E);
+    }
+    // piece 2 k + h of row l32, k a constant; rows a multiple of 16 further on lie row() of that further
+    __device__ static int row_at(int l32, int h, int k) {
+        if (APART) return row(l32) + (((k >> 1) ^ (l32 & 3)) << 6) + h * 16 + (k & 1) * 32;
+        return row(l32) + (((2 * k + h) ^ key(l32)) << 4);
+    }
+    // for a read across (bf16): lane s of 16 addresses row 4 h + s / 4 (second: 8 further on) at column
+    // 32 t + (l32 & 16) + 4 (s % 4)
+    __device__ static int col_at(int l32, int h, int t, bool second) {
+        const int s = l32 & 15, r = 4 * h + (s >> 2);
+        if (APART)
+            return row(4) * h + (s >> 2) * NC * 16 + ((t ^ (s >> 2)) << 6) + ((l32 & 16) << 1) + ((s & 2) << 3) + ((s & 1) << 3) +
+                   (second ? row(8) : 0);
+        return at(r + (second ? 8 : 0), 32 * t + (l32 & 16) + 4 * (s & 3));
     }
 };
 
@@ -140,8 +166,8 @@ __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, con
     f32x16 c = zero16();
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-        const bf16x8 a = __builtin_bit_cast(
-            bf16x8, *reinterpret_cast<const uint4*>(t + Rows<uint16_t, D>::piece(row0 + l32, 2 * k + h)));
+        using R = Rows<uint16_t, D>;
+        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + R::row(row0) + R::row_at(l32, h, k)));
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.x[k], c, 0, 0, 0);
     }
     return c;
@@ -151,7 +177,8 @@ __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, con
     f32x16 c = zero16();
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(t + Rows<float, D>::piece(row0 + l32, 2 * k + h));
+        using R = Rows<float, D>;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(t + R::row(row0) + R::row_at(l32, h, k));
 #pragma unroll
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b.x[k][e], c, 0, 0, 0);
     }
@@ -183,12 +210,11 @@ template <int D>
 __device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int t, const Weights<uint16_t>& w, f32x16 c,
                                            int l32, int h) {
     using R = Rows<uint16_t, D>;
-    const int s = l32 & 15, col = 32 * t + (l32 & 16) + 4 * (s & 3);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int r = row0 + 16 * k + 4 * h + (s >> 2);
-        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(x + R::at(r, col)));
-        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(x + R::at(r + 8, col)));
+        const unsigned char* p = x + R::row(row0 + 16 * k);
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, t, false)));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, t, true)));
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), w.b[k], c, 0, 0, 0);
     }
     return c;
@@ -199,7 +225,7 @@ __device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int
     using R = Rows<float, D>;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const float a = *reinterpret_cast<const float*>(x + R::at(row0 + 8 * (r / 4) + 4 * h + r % 4, 32 * t + l32));
+        const float a = *reinterpret_cast<const float*>(x + R::row(row0) + R::at(8 * (r / 4) + 4 * h + r % 4, 32 * t + l32));
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], c, 0, 0, 0);
     }
     return c;
@@ -288,7 +314,7 @@ struct WinArgs {
     const void *q, *k, *v, *y, *dy;
     void *o, *dq, *dk, *dv;   // o: y of the forward
     const int* len;
-    float2* stat;             // [B, T, H]: largest score times log2(e) scale, sum of exponentials about it
+    float2* stat;             // [B, T, H]: the exponents' reference less kAhead and the sum of exponentials about it
     int8_t* rest;             // [B, R, H, D]: what the rounding of y to bf16 left (rest_of)
     float* part;              // forward: partial O [nsplit][B T H][D]; dk, dv: the first tokens' sums
     float2* pstat;            // forward: [nsplit][B T H]
@@ -334,7 +360,7 @@ struct Loader {
         const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, n > 0 ? (uint32_t)(n - 1) * stride + D * (uint32_t)sizeof(E) : 0u,
                          0x00020000u};
 #pragma unroll
-        for (int i = 0; i < N; ++i) load_lds(rs, dst + (uint32_t)(i * 4 + wave) * 1024, off[i]);
+        for (int i = 0; i < N; ++i) load_lds(rs, dst + (uint32_t)(i * 4 + wave) * R::UNIT, off[i]);
     }
 };
 
@@ -407,7 +433,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
     f32x16 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
-    float mc = -INFINITY, l = 0.f;   // largest score times c, and the lane's share of the sum
+    float mc = -INFINITY, l = 0.f;   // the exponents' reference, and the lane's share of the sum
     if (p1 >= p0) {
         const Tiles tiles(a, p0, p1);
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
@@ -427,7 +453,6 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
             constexpr int U = CAREFUL ? 1 : 2;   // 32 tokens each at once
-            float mx = -INFINITY;
             if (i0 < i1) issue(i0);
             for (int i = i0; i < i1; ++i) {
                 wait_vm_all();
@@ -455,10 +480,9 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
 #pragma unroll
                         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
                     top = fmaxf(top, other_half(top));
-                    if (__any(top > mx)) {
-                        mx = fmaxf(mx, top);
-                        const float now = mx == -INFINITY ? -INFINITY : mx * a.c;
-                        const float f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
+                    top *= a.c;
+                    if (__any(top > mc)) {
+                        const float now = top > mc ? ceilf(top) + kAhead : mc, f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
                         mc = now;
                         l *= f;
 #pragma unroll
@@ -504,7 +528,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
         store_row<E, D>(y, o, 1.f / l, h, qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr);
     else
         store_zero<E, D>(y, h);
-    if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc, l} : float2{0.f, 0.f};
+    if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc - kAhead, l * kAheadExp} : float2{0.f, 0.f};
 }
 
 // Joins nsplit partial rows: y = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Four columns a thread.
@@ -533,7 +557,7 @@ __global__ __launch_bounds__(256) void win_join_kernel(size_t rows, int nsplit, 
     const float x4[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
     const int qi = R > 0 ? (int)(row / H % T) : 0;
     store4(y + row * D + col, x4, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + col : nullptr);
-    if (stat && col == 0) stat[row] = l != 0.f ? float2{m, l} : float2{0.f, 0.f};
+    if (stat && col == 0) stat[row] = l != 0.f ? float2{m - kAhead, l * kAheadExp} : float2{0.f, 0.f};
 }
 
 // The ring caches after the last token of each sequence: slot < sinks holds that token, slot sinks + x the last
@@ -599,7 +623,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
             Dq += other_half(Dq);
         }
         const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
-        const float li = st.y == 0.f ? 0.f : 1.f / st.y;
+        const float li = st.y == 0.f ? 0.f : 1.f / st.y, Dl = Dq * li;
         if (h == 0 && qi < a.T64) {
             a.rows[at] = st.x;
             a.rows[nrow + at] = li;
@@ -623,7 +647,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
                     f32x16 s = rows_dot<D>(K, 32 * u, q, l32, h);
                     const f32x16 dp = rows_dot<D>(V, 32 * u, g, l32, h);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * li * (dp[r] - Dq);
+                    for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
                     if (masked) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
