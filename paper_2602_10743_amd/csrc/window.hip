@@ -266,10 +266,10 @@ __device__ __forceinline__ f32x16 left_of(const f32x16& w, const Weights<uint16_
     return x;
 }
 
-// o += (rows row0 .. row0 + 31)^T w.  two: bf16 weights enter in two parts.
-template <bool CAREFUL, typename E, int D>
-__device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, bool two, float* scratch,
-                                         int l32, int h) {
+// o += (rows row0 .. row0 + 31)^T w.  TWO: bf16 weights enter in two parts.
+template <bool CAREFUL, bool TWO, typename E, int D>
+__device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, float* scratch, int l32,
+                                         int h) {
     if constexpr (CAREFUL) {
 #pragma unroll
         for (int t = 0; t < Rows<E, D>::DP / 32; ++t) cols_apart<E, D>(o[t], x, row0, t, w, scratch, l32, h);
@@ -277,12 +277,10 @@ __device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, i
         const Weights<E> b(w);
 #pragma unroll
         for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, b, o[t], l32, h);
-        if constexpr (sizeof(E) == 2) {
-            if (two) {
-                const Weights<E> rest(left_of(w, b));
+        if constexpr (sizeof(E) == 2 && TWO) {
+            const Weights<E> rest(left_of(w, b));
 #pragma unroll
-                for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, rest, o[t], l32, h);
-            }
+            for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, rest, o[t], l32, h);
         }
     }
 }
@@ -308,7 +306,35 @@ __device__ __forceinline__ bool any_of(bool x, int* flag) {
 }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The value of the lane 32 away: of two copies the instruction swaps one's upper half with the other's lower one.
+__device__ __forceinline__ void both_halves(float x, float& lower, float& upper) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    lower = __uint_as_float(p[0]);
+    upper = __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    float a, b;
+    both_halves(x, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float halves_max(float x) {
+    float a, b;
+    both_halves(x, a, b);
+    return fmaxf(a, b);
+}
+
+// Groups for the scheduler, which left alone reads LDS one or two operands before their use and waits for each:
+// reads run `ahead`, then one product, `reads` reads and `valu` other operations in turn.
+template <int MFMA, int READS, int AHEAD, int VALU>
+__device__ __forceinline__ void paced() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < MFMA; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (AHEAD + i * READS / MFMA < READS) __builtin_amdgcn_sched_group_barrier(0x100, READS / MFMA > 0 ? READS / MFMA : 1, 0);
+        if (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+    }
+}
 
 struct WinArgs {
     const void *q, *k, *v, *y, *dy;
@@ -333,7 +359,26 @@ __device__ __forceinline__ int block_of(int n) {
 // Whether token j is visible to the query at position p.  Without branches: selections of single registers of a
 // matrix tile by control flow have come out wrong (the compiler lost the copy of a branch's tile), and cost more.
 __device__ __forceinline__ bool visible(const WinArgs& a, int j, int p) {
-    return (j <= p) & ((j > p - a.W) | (j < a.sinks));
+    return ((uint32_t)(p - j) < (uint32_t)a.W) | ((j <= p) & (j < a.sinks));
+}
+
+// C tiles U from tokens j0 on, of the query at p: what it does not see is set to `none`.
+template <int U>
+__device__ __forceinline__ void hide(const WinArgs& a, f32x16 (&s)[U], int j0, int p, int h, float none) {
+    const int d = p - j0 - 4 * h;
+    if (j0 < a.sinks) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[u][r] = visible(a, j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4, p) ? s[u][r] : none;
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[u][r] = (uint32_t)(d - (32 * u + 8 * (r / 4) + r % 4)) < (uint32_t)a.W ? s[u][r] : none;
+    }
 }
 
 __device__ __forceinline__ int end_of(const WinArgs& a, int b) {
@@ -396,6 +441,14 @@ __device__ __forceinline__ void store_zero(E* p, int h) {
     for (int c = 0; c < D * (int)sizeof(E) / 32; ++c) reinterpret_cast<uint4*>(p)[2 * c + h] = uint4{0, 0, 0, 0};
 }
 
+template <typename E, int D>
+struct Shared {
+    alignas(16) unsigned char tile[2][2 * Rows<E, D>::BYTES];   // two of keys and values, or of queries and dy
+    alignas(16) float row[2][3][kTile];                         // dk, dv: the queries' m, 1 / l, D
+    float scratch[4][512];
+    int flag;
+};
+
 // The tiles that a workgroup of queries p0 .. p1 reads: the window's, after the first tokens' where they lie apart.
 struct Tiles {
     int t0, n;
@@ -408,19 +461,12 @@ struct Tiles {
     __device__ int operator[](int i) const { return lead ? (i == 0 ? 0 : t0 + i - 1) : t0 + i; }
 };
 
-template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(WinArgs a) {
+// TWO: weights enter in two parts.
+template <typename E, int D, bool TWO>
+__device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int split, int qb, int head, int b) {
     using R = Rows<E, D>;
     constexpr int DT = R::DP / 32;
-    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
-    __shared__ float scratch[4][512];
-    __shared__ int flag;
-    int id = block_of(a.blocks);
-    if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
-    const int split = id % a.nsplit;
-    id /= a.nsplit;
-    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
     const int qi = q0 + 32 * wave + l32, pos = past + qi;
@@ -438,7 +484,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
         const Tiles tiles(a, p0, p1);
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
         const Loader<E, D> ld(stride, wave, lane);
-        const uint32_t lds0 = lds_of(sm);
+        const uint32_t lds0 = lds_of(sh.tile);
         auto issue = [&](int i) {
             const int r0 = tiles[i] * kTile;
             const uint32_t to = lds0 + (uint32_t)((i - i0) & 1) * 2 * R::BYTES;
@@ -448,72 +494,74 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
         Row<E, D> q;
         q.load((const E*)a.q + row * D, live, h);
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);   // the wave's positions
-        const bool two = a.few || w0 < kRows;
-        auto sees = [&](int j) { return visible(a, j, pos); };
+        // U: 32 tokens each at once, from u0 on
+        auto step = [&](auto careful, bool masked, int i, int u0, int j0) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            constexpr int U = CAREFUL ? 1 : 2;
+            const unsigned char *K = sh.tile[(i - i0) & 1], *V = K + R::BYTES;
+            f32x16 s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
+            if (!CAREFUL && sizeof(E) == 2) paced<2 * D / 16, 2 * D / 16, D / 16, 0>();
+            if (masked) hide<U>(a, s, j0, pos, h, -INFINITY);
+            float top = s[0][0];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+            top = halves_max(top) * a.c;
+            if (__any(top > mc)) {
+                const float now = top > mc ? ceilf(top) + kAhead : mc, f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
+                mc = now;
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[t][r] *= f;
+            }
+            const float base = mc == -INFINITY ? 0.f : mc;   // nothing visible yet: weights 2^-inf
+            float sum[4] = {l, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
+                    sum[r % 4] += s[u][r];
+                }
+            if constexpr (CAREFUL) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
+            l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, V, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
+            if (!CAREFUL && !TWO && sizeof(E) == 2) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 40, 0);
+                paced<4 * DT, 8 * DT, 0, 20 / DT>();
+            }
+        };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int U = CAREFUL ? 1 : 2;   // 32 tokens each at once
+            constexpr int US = CAREFUL ? 32 : kTile;
             if (i0 < i1) issue(i0);
             for (int i = i0; i < i1; ++i) {
                 wait_vm_all();
                 barrier_lds();
                 if (i + 1 < i1) issue(i + 1);
-                const unsigned char *K = sm[(i - i0) & 1], *V = K + R::BYTES;
 #pragma unroll 1
-                for (int u0 = 0; u0 < kTile; u0 += 32 * U) {
+                for (int u0 = 0; u0 < kTile; u0 += US) {
                     const int j0 = tiles[i] * kTile + u0;
-                    if (j0 > w1 || w1 < w0 || (j0 + 32 * U - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
-                    const bool masked = j0 + 32 * U - 1 > w0 || j0 <= w1 - a.W;
-                    f32x16 s[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
-                    if (masked) {
-#pragma unroll
-                        for (int u = 0; u < U; ++u)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                s[u][r] = sees(j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4) ? s[u][r] : -INFINITY;
-                    }
-                    float top = s[0][0];
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-                    top = fmaxf(top, other_half(top));
-                    top *= a.c;
-                    if (__any(top > mc)) {
-                        const float now = top > mc ? ceilf(top) + kAhead : mc, f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
-                        mc = now;
-                        l *= f;
-#pragma unroll
-                        for (int t = 0; t < DT; ++t)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) o[t][r] *= f;
-                    }
-                    const float base = mc == -INFINITY ? 0.f : mc;   // nothing visible yet: weights 2^-inf
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
-                            l += s[u][r];
-                            if constexpr (CAREFUL)
-                                s[u][r] = sees(j0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4) ? s[u][r] : __uint_as_float(kMasked);
-                        }
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        add_cols<CAREFUL, E, D>(o, V, u0 + 32 * u, s[u], two, scratch[wave], l32, h);
+                    if (j0 > w1 || w1 < w0 || (j0 + US - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
+                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, i, u0, j0);
                 }
             }
         };
         walk(std::false_type{});
-        if (any_of(live && !finite(o), &flag)) {
+        if (any_of(live && !finite(o), &sh.flag)) {
             mc = -INFINITY, l = 0.f;
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] = zero16();
             walk(std::true_type{});
         }
-        l += other_half(l);
+        l = halves_sum(l);
     }
     if (qi >= a.T) return;
     if (a.nsplit > 1) {
@@ -529,6 +577,20 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(Wi
     else
         store_zero<E, D>(y, h);
     if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc - kAhead, l * kAheadExp} : float2{0.f, 0.f};
+}
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(WinArgs a) {
+    __shared__ Shared<E, D> sh;
+    int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int split = id % a.nsplit;
+    id /= a.nsplit;
+    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    if (sizeof(E) == 2 && (a.few || a.Tk - a.T + qb * kRows < kRows))
+        win_fwd<E, D, sizeof(E) == 2>(a, sh, split, qb, head, b);
+    else
+        win_fwd<E, D, false>(a, sh, split, qb, head, b);
 }
 
 // Joins nsplit partial rows: y = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Four columns a thread.
@@ -577,17 +639,11 @@ __global__ __launch_bounds__(256) void win_cache_kernel(WinArgs a, uint4* __rest
     }
 }
 
-template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(WinArgs a) {
+template <typename E, int D, bool TWO>
+__device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int qb, int head, int b) {
     using R = Rows<E, D>;
     constexpr int DT = R::DP / 32;
-    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
-    __shared__ float scratch[4][512];
-    __shared__ int flag;
-    const int id = block_of(a.blocks);
-    if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
-    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
     const int qi = q0 + 32 * wave + l32, pos = past + qi;
@@ -605,7 +661,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
     if (p1 >= p0) {
         const Tiles tiles(a, p0, p1);
         const Loader<E, D> ld(stride, wave, lane);
-        const uint32_t lds0 = lds_of(sm);
+        const uint32_t lds0 = lds_of(sh.tile);
         auto issue = [&](int i) {
             const int r0 = tiles[i] * kTile;
             const uint32_t to = lds0 + (uint32_t)(i & 1) * 2 * R::BYTES;
@@ -620,7 +676,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
             Row<E, D> y;
             y.load((const E*)a.y + row * D, live, h);
             Dq = g.dot(y, live && qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr, h);
-            Dq += other_half(Dq);
+            Dq = halves_sum(Dq);
         }
         const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
         const float li = st.y == 0.f ? 0.f : 1.f / st.y, Dl = Dq * li;
@@ -630,35 +686,47 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
             a.rows[2 * nrow + at] = Dq;
         }
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);
-        const bool two = a.few || w0 < kRows;
+        // U: 32 tokens each at once, from u0 on
+        auto step = [&](auto careful, bool masked, int i, int u0, int j0) {
+            constexpr bool CAREFUL = decltype(careful)::value;
+            constexpr int U = CAREFUL ? 1 : 2;
+            const unsigned char *K = sh.tile[i & 1], *V = K + R::BYTES;
+            f32x16 s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
+                const f32x16 dp = rows_dot<D>(V, u0 + 32 * u, g, l32, h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
+            }
+            if (!CAREFUL && sizeof(E) == 2) {
+                constexpr int M = D / 16;   // products of S, and of dP
+                paced<2 * M, 4 * M, 6, 0>();
+                paced<2 * M, 0, 0, 36 / M>();
+            }
+            if (masked) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
+#pragma unroll
+            for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, K, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
+            if (!CAREFUL && !TWO && sizeof(E) == 2) paced<4 * DT, 8 * DT, 8, 4>();
+        };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
+            constexpr int US = CAREFUL ? 32 : kTile;
             issue(0);
             for (int i = 0; i < tiles.n; ++i) {
                 wait_vm_all();
                 barrier_lds();
                 if (i + 1 < tiles.n) issue(i + 1);
-                const unsigned char *K = sm[i & 1], *V = K + R::BYTES;
 #pragma unroll 1
-                for (int u = 0; u < 2; ++u) {
-                    const int j0 = tiles[i] * kTile + 32 * u;
-                    if (j0 > w1 || w1 < w0 || (j0 + 31 <= w0 - a.W && j0 >= a.sinks)) continue;
-                    const bool masked = j0 + 31 > w0 || j0 <= w1 - a.W;
-                    f32x16 s = rows_dot<D>(K, 32 * u, q, l32, h);
-                    const f32x16 dp = rows_dot<D>(V, 32 * u, g, l32, h);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
-                    if (masked) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            s[r] = visible(a, j0 + 8 * (r / 4) + 4 * h + r % 4, pos) ? s[r] : __uint_as_float(kMasked);
-                    }
-                    add_cols<CAREFUL, E, D>(o, K, 32 * u, s, two, scratch[wave], l32, h);
+                for (int u0 = 0; u0 < kTile; u0 += US) {
+                    const int j0 = tiles[i] * kTile + u0;
+                    if (j0 > w1 || w1 < w0 || (j0 + US - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
+                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, i, u0, j0);
                 }
             }
         };
         walk(std::false_type{});
-        if (any_of(live && !finite(o), &flag)) {
+        if (any_of(live && !finite(o), &sh.flag)) {
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] = zero16();
             walk(std::true_type{});
@@ -673,21 +741,25 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
         store_zero<E, D>(dq, h);
 }
 
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(WinArgs a) {
+    __shared__ Shared<E, D> sh;
+    const int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    if (sizeof(E) == 2 && (a.few || a.Tk - a.T + qb * kRows < kRows))
+        win_dq<E, D, sizeof(E) == 2>(a, sh, qb, head, b);
+    else
+        win_dq<E, D, false>(a, sh, qb, head, b);
+}
+
 // dk, dv.  Workgroup (b, kh, kb): 128 tokens; after those, nseg segments of the queries behind the first 128 tokens'
 // window for each (b, kh), whose waves take (32 of the first tokens, every second 32 queries).
-template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
+template <typename E, int D, bool TWO>
+__device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D>& sh, int job, int nk, int bk, int kh, int b) {
     using R = Rows<E, D>;
     constexpr int DT = R::DP / 32;
-    __shared__ __align__(16) unsigned char sm[2][2 * R::BYTES];
-    __shared__ __align__(16) float srow[2][3][kTile];
-    __shared__ float scratch[4][512];
-    __shared__ int flag;
-    int id = block_of(a.blocks);
-    if (id >= a.blocks) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
-    const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
-    const int job = id % per, bk = id / per, kh = bk % a.Hk, b = bk / a.Hk;
     const bool seg = job >= nk;
     const int k0 = seg ? 0 : job * kRows, w0 = k0 + 32 * (seg ? wave / 2 : wave);   // the wave's first token
     const int G = a.H / a.Hk, past = a.Tk - a.T, end = end_of(a, b);
@@ -706,7 +778,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
         const size_t krow = ((size_t)b * a.Tk + min(tok, a.Tk - 1)) * a.Hk + kh;
         const uint32_t stride = (uint32_t)(a.H * D * (int)sizeof(E));
         const Loader<E, D> ld(stride, wave, lane);
-        const uint32_t lds0 = lds_of(sm), srow0 = lds_of(srow);
+        const uint32_t lds0 = lds_of(sh.tile), srow0 = lds_of(sh.row);
         const int t0 = (plo - past) / kTile, nt = (phi - past) / kTile - t0 + 1, n = nt * G;
         const size_t nrow = (size_t)a.B * a.H * a.T64;
         auto issue = [&](int i) {
@@ -731,7 +803,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
                 wait_vm_all();
                 barrier_lds();
                 if (i + 1 < n) issue(i + 1);
-                const unsigned char *Q = sm[i & 1], *G_ = Q + R::BYTES;
+                const unsigned char *Q = sh.tile[i & 1], *G_ = Q + R::BYTES;
                 const int pt = past + (t0 + i % nt) * kTile;
 #pragma unroll 1
                 for (int u = 0; u < 2; ++u) {
@@ -740,9 +812,8 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
                         (pp - a.W >= w0 + 31 && w0 >= a.sinks))
                         continue;
                     const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
-                    const bool two = a.few || pp < kRows;
                     f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
-                    const float* sr = &srow[i & 1][0][32 * u];
+                    const float* sr = &sh.row[i & 1][0][32 * u];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const f32x4 m = *reinterpret_cast<const f32x4*>(sr + 8 * j + 4 * h);
@@ -751,13 +822,20 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
                         for (int e = 0; e < 4; ++e) s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
                     }
                     if (masked) {
+                        const int d = pp + 4 * h - tok;
+                        if (w0 < a.sinks || pp < plo || pp + 31 > phi) {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int p = pp + 8 * (r / 4) + 4 * h + r % 4;
-                            s[r] = (visible(a, tok, p) & (p >= plo) & (p <= phi)) ? s[r] : __uint_as_float(kMasked);
+                            for (int r = 0; r < 16; ++r) {
+                                const int p = pp + 8 * (r / 4) + 4 * h + r % 4;
+                                s[r] = (visible(a, tok, p) & (p >= plo) & (p <= phi)) ? s[r] : __uint_as_float(kMasked);
+                            }
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                s[r] = (uint32_t)(d + 8 * (r / 4) + r % 4) < (uint32_t)a.W ? s[r] : __uint_as_float(kMasked);
                         }
                     }
-                    add_cols<CAREFUL, E, D>(ov, G_, 32 * u, s, two, scratch[wave], l32, h);
+                    add_cols<CAREFUL, TWO, E, D>(ov, G_, 32 * u, s, sh.scratch[wave], l32, h);
                     const f32x16 dp = rows_dot<D>(G_, 32 * u, v, l32, h);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -768,12 +846,12 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
                             s[r] = __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * (dp[r] - Dq[e]);
                         }
                     }
-                    add_cols<CAREFUL, E, D>(ok, Q, 32 * u, s, two, scratch[wave], l32, h);
+                    add_cols<CAREFUL, TWO, E, D>(ok, Q, 32 * u, s, sh.scratch[wave], l32, h);
                 }
             }
         };
         walk(std::false_type{});
-        if (any_of(live && !(finite(ok) && finite(ov)), &flag)) {
+        if (any_of(live && !(finite(ok) && finite(ov)), &sh.flag)) {
 #pragma unroll
             for (int t = 0; t < DT; ++t) ok[t] = ov[t] = zero16();
             walk(std::true_type{});
@@ -798,6 +876,20 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(Wi
         store_zero<E, D>(dk, h);
         store_zero<E, D>(dv, h);
     }
+}
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
+    __shared__ Shared<E, D> sh;
+    const int id = block_of(a.blocks);
+    if (id >= a.blocks) return;
+    const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
+    const int job = id % per, bk = id / per, kh = bk % a.Hk, b = bk / a.Hk;
+    // the first rows' queries are those of the first 128 tokens' workgroup
+    if (sizeof(E) == 2 && (a.few || (job == 0 && a.Tk - a.T < kRows)))
+        win_dkv<E, D, sizeof(E) == 2>(a, sh, job, nk, bk, kh, b);
+    else
+        win_dkv<E, D, false>(a, sh, job, nk, bk, kh, b);
 }
 
 // dk, dv of the first tokens: their slots added up in order, four columns a thread.
