@@ -62,7 +62,8 @@ struct Rows {
     static constexpr int DP = D < 32 ? 32 : D, NC = DP * (int)sizeof(E) / 16, NR = D * (int)sizeof(E) / 16;
     static constexpr bool APART = sizeof(E) == 2 && NC == 16;
     static constexpr int UNIT = 1024 + (APART ? 16 : 0);   // bytes of a wave's load, 1024 / (16 NC) rows
-    static constexpr int BYTES = kTile * NC / 64 * UNIT;
+    static constexpr int bytes(int rows) { return rows * NC / 64 * UNIT; }
+    static constexpr int BYTES = bytes(kTile);
     __device__ static int key(int r) {
         if (APART) return (r & 3) << 2;
         if (sizeof(E) == 4) return NC >= 16 ? ((r & 4) << 1) | ((r & 8) >> 1) | (r & 3) : (r >> 1) & 7;
@@ -385,11 +386,11 @@ __device__ __forceinline__ int end_of(const WinArgs& a, int b) {
     return a.len ? min(max(a.len[b], 0), a.Tk) : a.Tk;
 }
 
-// A tile of kTile rows from row r0 on of `rows` into LDS, by the four waves; rows past them are zero.
-template <typename E, int D>
+// A tile of TT rows from row r0 on of `rows` into LDS, by the four waves; rows past them are zero.
+template <typename E, int D, int TT = kTile>
 struct Loader {
     using R = Rows<E, D>;
-    static constexpr int N = kTile * R::NC / 64 / 4;   // loads a wave
+    static constexpr int N = TT * R::NC / 64 / 4;   // loads a wave
     uint32_t off[N];
     uint32_t stride;
     __device__ Loader(uint32_t stride, int wave, int lane) : stride(stride) {
@@ -401,7 +402,7 @@ struct Loader {
     }
     __device__ void load(const void* base, int r0, int rows, uint32_t dst, int wave) const {
         const uintptr_t p = reinterpret_cast<uintptr_t>(base) + (size_t)r0 * stride;
-        const int n = min(rows - r0, kTile);
+        const int n = min(rows - r0, TT);
         const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, n > 0 ? (uint32_t)(n - 1) * stride + D * (uint32_t)sizeof(E) : 0u,
                          0x00020000u};
 #pragma unroll
@@ -441,31 +442,42 @@ __device__ __forceinline__ void store_zero(E* p, int h) {
     for (int c = 0; c < D * (int)sizeof(E) / 32; ++c) reinterpret_cast<uint4*>(p)[2 * c + h] = uint4{0, 0, 0, 0};
 }
 
-template <typename E, int D>
+template <typename E, int D, int TT = kTile>
 struct Shared {
-    alignas(16) unsigned char tile[2][2 * Rows<E, D>::BYTES];   // two of keys and values, or of queries and dy
-    alignas(16) float row[2][3][kTile];                         // dk, dv: the queries' m, 1 / l, D
+    alignas(16) unsigned char tile[2][2 * Rows<E, D>::bytes(TT)];   // two of keys and values, or of queries and dy
     float scratch[4][512];
     int flag;
 };
 
+template <typename E, int D>
+struct SharedDkv : Shared<E, D> {
+    alignas(16) float row[2][3][kTile];   // the queries' m, 1 / l, D
+};
+
 // The tiles that a workgroup of queries p0 .. p1 reads: the window's, after the first tokens' where they lie apart.
+template <int TT>
 struct Tiles {
     int t0, n;
-    bool lead;
+    int first;
     __device__ Tiles(const WinArgs& a, int p0, int p1) {
-        t0 = max(0, p0 - a.W + 1) / kTile;
-        lead = t0 > 0 && a.sinks > 0;
-        n = p1 / kTile - t0 + 1 + (lead ? 1 : 0);
+        t0 = max(0, p0 - a.W + 1) / TT;
+        first = min(t0, (a.sinks + TT - 1) / TT);   // tiles before it that hold first tokens
+        n = p1 / TT - t0 + 1 + first;
     }
-    __device__ int operator[](int i) const { return lead ? (i == 0 ? 0 : t0 + i - 1) : t0 + i; }
+    __device__ int operator[](int i) const { return i < first ? i : t0 + i - first; }
+};
+
+// Tokens a tile and waves a SIMD of the forward.
+template <typename E, int D>
+struct FwdTile {
+    static constexpr int TT = sizeof(E) == 2 && D == 128 ? 32 : 64, WAVES = sizeof(E) == 4 ? 1 : D == 128 ? 3 : 2;
 };
 
 // TWO: weights enter in two parts.
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int split, int qb, int head, int b) {
+__device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E, D>::TT>& sh, int split, int qb, int head, int b) {
     using R = Rows<E, D>;
-    constexpr int DT = R::DP / 32;
+    constexpr int DT = R::DP / 32, TT = FwdTile<E, D>::TT, BYTES = R::bytes(TT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
@@ -481,15 +493,15 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int 
     for (int t = 0; t < DT; ++t) o[t] = zero16();
     float mc = -INFINITY, l = 0.f;   // the exponents' reference, and the lane's share of the sum
     if (p1 >= p0) {
-        const Tiles tiles(a, p0, p1);
+        const Tiles<TT> tiles(a, p0, p1);
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
-        const Loader<E, D> ld(stride, wave, lane);
+        const Loader<E, D, TT> ld(stride, wave, lane);
         const uint32_t lds0 = lds_of(sh.tile);
         auto issue = [&](int i) {
-            const int r0 = tiles[i] * kTile;
-            const uint32_t to = lds0 + (uint32_t)((i - i0) & 1) * 2 * R::BYTES;
+            const int r0 = tiles[i] * TT;
+            const uint32_t to = lds0 + (uint32_t)((i - i0) & 1) * 2 * BYTES;
             ld.load(kb, r0, end, to, wave);
-            ld.load(vb, r0, end, to + R::BYTES, wave);
+            ld.load(vb, r0, end, to + BYTES, wave);
         };
         Row<E, D> q;
         q.load((const E*)a.q + row * D, live, h);
@@ -497,12 +509,12 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int 
         // U: 32 tokens each at once, from u0 on
         auto step = [&](auto careful, bool masked, int i, int u0, int j0) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int U = CAREFUL ? 1 : 2;
-            const unsigned char *K = sh.tile[(i - i0) & 1], *V = K + R::BYTES;
+            constexpr int U = CAREFUL ? 1 : TT / 32;
+            const unsigned char *K = sh.tile[(i - i0) & 1], *V = K + BYTES;
             f32x16 s[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
-            if (!CAREFUL && sizeof(E) == 2) paced<2 * D / 16, 2 * D / 16, D / 16, 0>();
+            if (!CAREFUL && sizeof(E) == 2) paced<U * D / 16, U * D / 16, U * D / 32, 0>();
             if (masked) hide<U>(a, s, j0, pos, h, -INFINITY);
             float top = s[0][0];
 #pragma unroll
@@ -535,20 +547,20 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int 
             if (!CAREFUL && !TWO && sizeof(E) == 2) {
                 __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, 40, 0);
-                paced<4 * DT, 8 * DT, 0, 20 / DT>();
+                paced<2 * U * DT, 4 * U * DT, 0, 20 / DT>();
             }
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int US = CAREFUL ? 32 : kTile;
+            constexpr int US = CAREFUL ? 32 : TT;
             if (i0 < i1) issue(i0);
             for (int i = i0; i < i1; ++i) {
                 wait_vm_all();
                 barrier_lds();
                 if (i + 1 < i1) issue(i + 1);
 #pragma unroll 1
-                for (int u0 = 0; u0 < kTile; u0 += US) {
-                    const int j0 = tiles[i] * kTile + u0;
+                for (int u0 = 0; u0 < TT; u0 += US) {
+                    const int j0 = tiles[i] * TT + u0;
                     if (j0 > w1 || w1 < w0 || (j0 + US - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
                     step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, i, u0, j0);
                 }
@@ -580,8 +592,8 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D>& sh, int 
 }
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_fwd_kernel(WinArgs a) {
-    __shared__ Shared<E, D> sh;
+__global__ __launch_bounds__(256, (FwdTile<E, D>::WAVES)) void win_fwd_kernel(WinArgs a) {
+    __shared__ Shared<E, D, FwdTile<E, D>::TT> sh;
     int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int split = id % a.nsplit;
@@ -659,7 +671,7 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int q
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
     if (p1 >= p0) {
-        const Tiles tiles(a, p0, p1);
+        const Tiles<kTile> tiles(a, p0, p1);
         const Loader<E, D> ld(stride, wave, lane);
         const uint32_t lds0 = lds_of(sh.tile);
         auto issue = [&](int i) {
@@ -756,7 +768,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
 // dk, dv.  Workgroup (b, kh, kb): 128 tokens; after those, nseg segments of the queries behind the first 128 tokens'
 // window for each (b, kh), whose waves take (32 of the first tokens, every second 32 queries).
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D>& sh, int job, int nk, int bk, int kh, int b) {
+__device__ __forceinline__ void win_dkv(const WinArgs& a, SharedDkv<E, D>& sh, int job, int nk, int bk, int kh, int b) {
     using R = Rows<E, D>;
     constexpr int DT = R::DP / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
@@ -880,7 +892,7 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D>& sh, int 
 
 template <typename E, int D>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
-    __shared__ Shared<E, D> sh;
+    __shared__ SharedDkv<E, D> sh;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
