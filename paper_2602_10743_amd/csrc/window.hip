@@ -41,7 +41,6 @@ namespace {
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
-constexpr int kTile = 64;    // tokens (queries in the dk, dv pass) a tile
 constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgroup
 // The exponents' reference lies this far above the largest score (times c, rounded up) that moved it: weights are at
 // most 1, and a row is rescaled only when a score passes the reference, not whenever the maximum grows, which one of
@@ -63,7 +62,6 @@ struct Rows {
     static constexpr bool APART = sizeof(E) == 2 && NC == 16;
     static constexpr int UNIT = 1024 + (APART ? 16 : 0);   // bytes of a wave's load, 1024 / (16 NC) rows
     static constexpr int bytes(int rows) { return rows * NC / 64 * UNIT; }
-    static constexpr int BYTES = bytes(kTile);
     __device__ static int key(int r) {
         if (APART) return (r & 3) << 2;
         if (sizeof(E) == 4) return NC >= 16 ? ((r & 4) << 1) | ((r & 8) >> 1) | (r & 3) : (r >> 1) & 7;
@@ -186,6 +184,24 @@ __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, con
     return c;
 }
 
+// The same with b's rows in LDS, l32 of them from p on.
+struct RowsAt {
+    const unsigned char* p;
+};
+template <int D>
+__device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const RowsAt& b, int l32, int h) {
+    using R = Rows<uint16_t, D>;
+    f32x16 c = zero16();
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const int at = R::row_at(l32, h, k);
+        const bf16x8 x = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + R::row(row0) + at));
+        const bf16x8 y = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(b.p + at));
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+    }
+    return c;
+}
+
 // Weights of 32 rows (a C, register r at row 8 (r / 4) + 4 h + r % 4) as the operand of a product over them.
 template <typename E>
 struct Weights;
@@ -237,23 +253,25 @@ __device__ __forceinline__ float elem(const unsigned char* p, uint16_t) {
 }
 __device__ __forceinline__ float elem(const unsigned char* p, float) { return *reinterpret_cast<const float*>(p); }
 
-// The same element by element, without the rows whose weight is masked.  scratch: 512 floats of the wave's own.
+// The same element by element, without the rows whose weight is masked.  scratch: 128 floats of the wave's own.
 template <typename E, int D>
 __device__ __forceinline__ void cols_apart(f32x16& c, const unsigned char* x, int row0, int t, const f32x16& w, float* scratch,
                                            int l32, int h) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < 8; ++k) {   // rows 4 k .. 4 k + 3, of half k % 2
+        if (h == k % 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) scratch[((e & 4) * 2 + 4 * h + (e & 3)) * 32 + l32] = w[8 * k + e];
+            for (int e = 0; e < 4; ++e) scratch[e * 32 + l32] = w[4 * (k / 2) + e];
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const float f = scratch[i * 32 + l32];
             if (__float_as_uint(f) == kMasked) continue;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                c[r] = fmaf(f, elem(x + Rows<E, D>::at(row0 + 16 * k + i, 32 * t + 8 * (r / 4) + 4 * h + r % 4), E{}), c[r]);
+                c[r] = fmaf(f, elem(x + Rows<E, D>::at(row0 + 4 * k + i, 32 * t + 8 * (r / 4) + 4 * h + r % 4), E{}), c[r]);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -387,7 +405,7 @@ __device__ __forceinline__ int end_of(const WinArgs& a, int b) {
 }
 
 // A tile of TT rows from row r0 on of `rows` into LDS, by the four waves; rows past them are zero.
-template <typename E, int D, int TT = kTile>
+template <typename E, int D, int TT>
 struct Loader {
     using R = Rows<E, D>;
     static constexpr int N = TT * R::NC / 64 / 4;   // loads a wave
@@ -442,17 +460,45 @@ __device__ __forceinline__ void store_zero(E* p, int h) {
     for (int c = 0; c < D * (int)sizeof(E) / 32; ++c) reinterpret_cast<uint4*>(p)[2 * c + h] = uint4{0, 0, 0, 0};
 }
 
-template <typename E, int D, int TT = kTile>
+// How a pass (forward, dq, or dk and dv) goes over its tiles: TT tokens (queries for dk, dv) a tile, NB tiles in LDS
+// (one worked on, the others on their way), U halves of 32 at once, WAVES a SIMD.  At 128 bf16 columns tiles of 32
+// leave the forward registers for three waves a SIMD (B8 T2048 H16 window 512: 107 us, with tiles of 64 and two
+// waves 121).  fp32 products take four times as long as they need for their operands' latency: one wave will do.
+enum Pass { kFwd, kDq, kDkv };
+template <typename E, int D, Pass P>
+struct Geo {
+    static constexpr bool BF = sizeof(E) == 2;
+    static constexpr int TT = Rows<E, D>::NC < 8 || (BF ? D < 128 : D < 64 || (D == 128 && P != kFwd)) ? 64 : 32;
+    static constexpr int U = BF && P != kDkv ? TT / 32 : 1;
+    static constexpr int PAIR = 2 * Rows<E, D>::bytes(TT);
+    static constexpr int WAVES = !BF ? (D < 128 ? 2 : 1) : D == 128 && P == kFwd ? 3 : 2;
+    static constexpr int NB = BF && D < 128 && P != kFwd ? 3 : 2;
+    // dk, dv at 128 bf16 columns: the tokens' keys stay in LDS; with them in registers, beside their values and both
+    // sums, some of each were stored and loaded again around every tile.
+    static constexpr bool KEYS = BF && D == 128 && P == kDkv;
+};
+
+template <typename E, int D, Pass P>
 struct Shared {
-    alignas(16) unsigned char tile[2][2 * Rows<E, D>::bytes(TT)];   // two of keys and values, or of queries and dy
-    float scratch[4][512];
+    using G = Geo<E, D, P>;
+    alignas(16) unsigned char tile[G::NB][G::PAIR];   // of keys and values, or of queries and dy
+    alignas(16) float row[P == kDkv ? G::NB : 1][3][P == kDkv ? G::TT : 1];   // the queries' m, 1 / l, D
+    alignas(16) unsigned char keys[G::KEYS ? Rows<E, D>::bytes(kRows) : 16];
+    float scratch[4][128];
     int flag;
 };
 
-template <typename E, int D>
-struct SharedDkv : Shared<E, D> {
-    alignas(16) float row[2][3][kTile];   // the queries' m, 1 / l, D
-};
+// Before tile i of n: waits until it is there, L loads a tile and wave, the tiles up to NB - 2 after it under way.
+template <int NB, int L>
+__device__ __forceinline__ void wait_tile(int i, int n) {
+    if (i + NB - 2 < n)
+        wait_vm_le<(NB - 2) * L>();
+    else if (NB > 3 && i + 1 < n)
+        wait_vm_le<L>();
+    else
+        wait_vm_all();
+    barrier_lds();
+}
 
 // The tiles that a workgroup of queries p0 .. p1 reads: the window's, after the first tokens' where they lie apart.
 template <int TT>
@@ -467,17 +513,12 @@ struct Tiles {
     __device__ int operator[](int i) const { return i < first ? i : t0 + i - first; }
 };
 
-// Tokens a tile and waves a SIMD of the forward.
-template <typename E, int D>
-struct FwdTile {
-    static constexpr int TT = sizeof(E) == 2 && D == 128 ? 32 : 64, WAVES = sizeof(E) == 4 ? 1 : D == 128 ? 3 : 2;
-};
-
 // TWO: weights enter in two parts.
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E, D>::TT>& sh, int split, int qb, int head, int b) {
+__device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh, int split, int qb, int head, int b) {
     using R = Rows<E, D>;
-    constexpr int DT = R::DP / 32, TT = FwdTile<E, D>::TT, BYTES = R::bytes(TT);
+    using G = Geo<E, D, kFwd>;
+    constexpr int DT = R::DP / 32, TT = G::TT, NB = G::NB, BYTES = R::bytes(TT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
@@ -497,9 +538,11 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
         const Loader<E, D, TT> ld(stride, wave, lane);
         const uint32_t lds0 = lds_of(sh.tile);
+        int into = 0;   // the place of the next tile
         auto issue = [&](int i) {
             const int r0 = tiles[i] * TT;
-            const uint32_t to = lds0 + (uint32_t)((i - i0) & 1) * 2 * BYTES;
+            const uint32_t to = lds0 + (uint32_t)into * 2 * BYTES;
+            into = into + 1 < NB ? into + 1 : 0;
             ld.load(kb, r0, end, to, wave);
             ld.load(vb, r0, end, to + BYTES, wave);
         };
@@ -507,10 +550,10 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E
         q.load((const E*)a.q + row * D, live, h);
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);   // the wave's positions
         // U: 32 tokens each at once, from u0 on
-        auto step = [&](auto careful, bool masked, int i, int u0, int j0) {
+        auto step = [&](auto careful, bool masked, const unsigned char* K, int u0, int j0) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int U = CAREFUL ? 1 : TT / 32;
-            const unsigned char *K = sh.tile[(i - i0) & 1], *V = K + BYTES;
+            constexpr int U = CAREFUL ? 1 : G::U;
+            const unsigned char* V = K + BYTES;
             f32x16 s[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
@@ -552,17 +595,20 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int US = CAREFUL ? 32 : TT;
-            if (i0 < i1) issue(i0);
+            constexpr int US = CAREFUL ? 32 : 32 * G::U;
+            into = 0;
+            for (int i = i0; i < min(i0 + NB - 1, i1); ++i) issue(i);
+            int at = 0;
             for (int i = i0; i < i1; ++i) {
-                wait_vm_all();
-                barrier_lds();
-                if (i + 1 < i1) issue(i + 1);
+                wait_tile<NB, 2 * Loader<E, D, TT>::N>(i, i1);
+                if (i + NB - 1 < i1) issue(i + NB - 1);
+                const unsigned char* K = sh.tile[at];
+                at = at + 1 < NB ? at + 1 : 0;
 #pragma unroll 1
                 for (int u0 = 0; u0 < TT; u0 += US) {
                     const int j0 = tiles[i] * TT + u0;
                     if (j0 > w1 || w1 < w0 || (j0 + US - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
-                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, i, u0, j0);
+                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, K, u0, j0);
                 }
             }
         };
@@ -592,8 +638,8 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, FwdTile<E
 }
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, (FwdTile<E, D>::WAVES)) void win_fwd_kernel(WinArgs a) {
-    __shared__ Shared<E, D, FwdTile<E, D>::TT> sh;
+__global__ __launch_bounds__(256, (Geo<E, D, kFwd>::WAVES)) void win_fwd_kernel(WinArgs a) {
+    __shared__ Shared<E, D, kFwd> sh;
     int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int split = id % a.nsplit;
@@ -652,9 +698,10 @@ __global__ __launch_bounds__(256) void win_cache_kernel(WinArgs a, uint4* __rest
 }
 
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int qb, int head, int b) {
+__device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, int qb, int head, int b) {
     using R = Rows<E, D>;
-    constexpr int DT = R::DP / 32;
+    using G = Geo<E, D, kDq>;
+    constexpr int DT = R::DP / 32, TT = G::TT, NB = G::NB, BYTES = R::bytes(TT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
@@ -671,14 +718,16 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int q
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
     if (p1 >= p0) {
-        const Tiles<kTile> tiles(a, p0, p1);
-        const Loader<E, D> ld(stride, wave, lane);
+        const Tiles<TT> tiles(a, p0, p1);
+        const Loader<E, D, TT> ld(stride, wave, lane);
         const uint32_t lds0 = lds_of(sh.tile);
+        int into = 0;   // the place of the next tile
         auto issue = [&](int i) {
-            const int r0 = tiles[i] * kTile;
-            const uint32_t to = lds0 + (uint32_t)(i & 1) * 2 * R::BYTES;
+            const int r0 = tiles[i] * TT;
+            const uint32_t to = lds0 + (uint32_t)into * 2 * BYTES;
+            into = into + 1 < NB ? into + 1 : 0;
             ld.load(kb, r0, end, to, wave);
-            ld.load(vb, r0, end, to + R::BYTES, wave);
+            ld.load(vb, r0, end, to + BYTES, wave);
         };
         Row<E, D> q, g;
         q.load((const E*)a.q + row * D, live, h);
@@ -699,10 +748,10 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int q
         }
         const int w0 = p0 + 32 * wave, w1 = min(w0 + 31, p1);
         // U: 32 tokens each at once, from u0 on
-        auto step = [&](auto careful, bool masked, int i, int u0, int j0) {
+        auto step = [&](auto careful, bool masked, const unsigned char* K, int u0, int j0) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int U = CAREFUL ? 1 : 2;
-            const unsigned char *K = sh.tile[i & 1], *V = K + R::BYTES;
+            constexpr int U = CAREFUL ? 1 : G::U;
+            const unsigned char* V = K + BYTES;
             f32x16 s[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -713,27 +762,30 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int q
             }
             if (!CAREFUL && sizeof(E) == 2) {
                 constexpr int M = D / 16;   // products of S, and of dP
-                paced<2 * M, 4 * M, 6, 0>();
-                paced<2 * M, 0, 0, 36 / M>();
+                paced<2 * M, 2 * U * M, 6, 0>();
+                if (U > 1) paced<2 * M, 0, 0, 36 / M>();
             }
             if (masked) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
 #pragma unroll
             for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, K, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
-            if (!CAREFUL && !TWO && sizeof(E) == 2) paced<4 * DT, 8 * DT, 8, 4>();
+            if (!CAREFUL && !TWO && sizeof(E) == 2) paced<2 * U * DT, 4 * U * DT, 8, 4>();
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            constexpr int US = CAREFUL ? 32 : kTile;
-            issue(0);
+            constexpr int US = CAREFUL ? 32 : 32 * G::U;
+            into = 0;
+            for (int i = 0; i < min(NB - 1, tiles.n); ++i) issue(i);
+            int at = 0;
             for (int i = 0; i < tiles.n; ++i) {
-                wait_vm_all();
-                barrier_lds();
-                if (i + 1 < tiles.n) issue(i + 1);
+                wait_tile<NB, 2 * Loader<E, D, TT>::N>(i, tiles.n);
+                if (i + NB - 1 < tiles.n) issue(i + NB - 1);
+                const unsigned char* K = sh.tile[at];
+                at = at + 1 < NB ? at + 1 : 0;
 #pragma unroll 1
-                for (int u0 = 0; u0 < kTile; u0 += US) {
-                    const int j0 = tiles[i] * kTile + u0;
+                for (int u0 = 0; u0 < TT; u0 += US) {
+                    const int j0 = tiles[i] * TT + u0;
                     if (j0 > w1 || w1 < w0 || (j0 + US - 1 <= w0 - a.W && j0 >= a.sinks)) continue;
-                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, i, u0, j0);
+                    step(careful, j0 + US - 1 > w0 || j0 <= w1 - a.W, K, u0, j0);
                 }
             }
         };
@@ -754,8 +806,8 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D>& sh, int q
 }
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(WinArgs a) {
-    __shared__ Shared<E, D> sh;
+__global__ __launch_bounds__(256, (Geo<E, D, kDq>::WAVES)) void win_dq_kernel(WinArgs a) {
+    __shared__ Shared<E, D, kDq> sh;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
@@ -768,9 +820,10 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dq_kernel(Win
 // dk, dv.  Workgroup (b, kh, kb): 128 tokens; after those, nseg segments of the queries behind the first 128 tokens'
 // window for each (b, kh), whose waves take (32 of the first tokens, every second 32 queries).
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_dkv(const WinArgs& a, SharedDkv<E, D>& sh, int job, int nk, int bk, int kh, int b) {
+__device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh, int job, int nk, int bk, int kh, int b) {
     using R = Rows<E, D>;
-    constexpr int DT = R::DP / 32;
+    using Gm = Geo<E, D, kDkv>;
+    constexpr int DT = R::DP / 32, TT = Gm::TT, NB = Gm::NB, BYTES = R::bytes(TT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
     const bool seg = job >= nk;
     const int k0 = seg ? 0 : job * kRows, w0 = k0 + 32 * (seg ? wave / 2 : wave);   // the wave's first token
@@ -789,49 +842,68 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, SharedDkv<E, D>& sh, i
     if (phi >= plo) {
         const size_t krow = ((size_t)b * a.Tk + min(tok, a.Tk - 1)) * a.Hk + kh;
         const uint32_t stride = (uint32_t)(a.H * D * (int)sizeof(E));
-        const Loader<E, D> ld(stride, wave, lane);
-        const uint32_t lds0 = lds_of(sh.tile), srow0 = lds_of(sh.row);
-        const int t0 = (plo - past) / kTile, nt = (phi - past) / kTile - t0 + 1, n = nt * G;
+        const Loader<E, D, TT> ld(stride, wave, lane);
+        const uint32_t lds0 = lds_of(sh.tile), row0 = lds_of(sh.row);
+        const int t0 = (plo - past) / TT, nt = (phi - past) / TT - t0 + 1, n = nt * G;
         const size_t nrow = (size_t)a.B * a.H * a.T64;
-        auto issue = [&](int i) {
-            const int head = kh * G + i / nt, r0 = (t0 + i % nt) * kTile;
-            const uint32_t to = lds0 + (uint32_t)(i & 1) * 2 * R::BYTES;
-            const size_t first = ((size_t)b * a.T * a.H + head) * D;
+        int into = 0, next_t = t0, next_h = kh * G;   // the next tile: its place, its queries and head
+        auto issue = [&]() {
+            const int r0 = next_t * TT;
+            const uint32_t to = lds0 + (uint32_t)into * 2 * BYTES;
+            const size_t first = ((size_t)b * a.T * a.H + next_h) * D;
             ld.load((const E*)a.q + first, r0, end - past, to, wave);
-            ld.load((const E*)a.dy + first, r0, end - past, to + R::BYTES, wave);
-            if (wave < 3) {   // m, 1 / l or D of the tile's rows: 16 lanes' pieces
-                const uintptr_t p = reinterpret_cast<uintptr_t>(a.rows + wave * nrow + ((size_t)b * a.H + head) * a.T64 + r0);
-                const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, kTile * 4u, 0x00020000u};
-                if (lane < 16) load_lds(rs, srow0 + (uint32_t)((i & 1) * 3 + wave) * kTile * 4, (uint32_t)lane * 16);
-            }
+            ld.load((const E*)a.dy + first, r0, end - past, to + BYTES, wave);
+            // m, 1 / l or D of the tile's rows, 16 bytes a lane; the fourth wave as the third
+            const int of = min(wave, 2);
+            const uintptr_t p = reinterpret_cast<uintptr_t>(a.rows + of * nrow + ((size_t)b * a.H + next_h) * a.T64 + r0);
+            const words_t rs{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, TT * 4u, 0x00020000u};
+            if (lane < TT / 4) load_lds(rs, row0 + (uint32_t)(into * 3 + of) * TT * 4, (uint32_t)lane * 16);
+            into = into + 1 < NB ? into + 1 : 0;
+            if (++next_t == t0 + nt) next_t = t0, ++next_h;
         };
-        Row<E, D> k, v;
-        k.load((const E*)a.k + krow * D, live, h);
+        std::conditional_t<Gm::KEYS, RowsAt, Row<E, D>> k;
+        Row<E, D> v;
         v.load((const E*)a.v + krow * D, live, h);
+        if constexpr (Gm::KEYS) {
+            const Loader<E, D, kRows> lk((uint32_t)(a.Hk * D * (int)sizeof(E)), wave, lane);
+            lk.load((const E*)a.k + ((size_t)b * a.Tk * a.Hk + kh) * D, k0, end, lds_of(sh.keys), wave);
+            k.p = sh.keys + R::row(w0 - k0);
+        } else {
+            k.load((const E*)a.k + krow * D, live, h);
+        }
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            issue(0);
+            into = 0, next_t = t0, next_h = kh * G;
+            for (int i = 0; i < min(NB - 1, n); ++i) issue();
+            int at = 0, tile = t0;
             for (int i = 0; i < n; ++i) {
-                wait_vm_all();
-                barrier_lds();
-                if (i + 1 < n) issue(i + 1);
-                const unsigned char *Q = sh.tile[i & 1], *G_ = Q + R::BYTES;
-                const int pt = past + (t0 + i % nt) * kTile;
+                wait_tile<NB, 2 * Loader<E, D, TT>::N + 1>(i, n);
+                if (i + NB - 1 < n) issue();
+                const unsigned char *Q = sh.tile[at], *G_ = Q + BYTES;
+                const float* rows = &sh.row[at][0][0];
+                const int pt = past + tile * TT;
+                at = at + 1 < NB ? at + 1 : 0;
+                tile = tile + 1 < t0 + nt ? tile + 1 : t0;
 #pragma unroll 1
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < TT / 32; ++u) {
                     const int pp = pt + 32 * u;   // the rows' first position
-                    if (!works || (seg && u != wave % 2) || pp + 31 < max(w0, plo) || pp > phi ||
+                    if (!works || (seg && (pp / 32 & 1) != wave % 2) || pp + 31 < max(w0, plo) || pp > phi ||
                         (pp - a.W >= w0 + 31 && w0 >= a.sinks))
                         continue;
                     const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
                     f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
-                    const float* sr = &sh.row[i & 1][0][32 * u];
+                    f32x16 ds = rows_dot<D>(G_, 32 * u, v, l32, h);
+                    const float* sr = rows + 32 * u;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const f32x4 m = *reinterpret_cast<const f32x4*>(sr + 8 * j + 4 * h);
-                        const f32x4 li = *reinterpret_cast<const f32x4*>(sr + kTile + 8 * j + 4 * h);
+                        const f32x4 li = *reinterpret_cast<const f32x4*>(sr + TT + 8 * j + 4 * h);
+                        const f32x4 Dq = *reinterpret_cast<const f32x4*>(sr + 2 * TT + 8 * j + 4 * h);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
+                        for (int e = 0; e < 4; ++e) {
+                            s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
+                            ds[4 * j + e] -= Dq[e];
+                        }
                     }
                     if (masked) {
                         const int d = pp + 4 * h - tok;
@@ -848,17 +920,14 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, SharedDkv<E, D>& sh, i
                         }
                     }
                     add_cols<CAREFUL, TWO, E, D>(ov, G_, 32 * u, s, sh.scratch[wave], l32, h);
-                    const f32x16 dp = rows_dot<D>(G_, 32 * u, v, l32, h);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4 Dq = *reinterpret_cast<const f32x4*>(sr + 2 * kTile + 8 * j + 4 * h);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = 4 * j + e;
-                            s[r] = __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * (dp[r] - Dq[e]);
-                        }
+                    for (int r = 0; r < 16; ++r) {
+                        if constexpr (CAREFUL)
+                            ds[r] = __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * ds[r];
+                        else
+                            ds[r] *= s[r];
                     }
-                    add_cols<CAREFUL, TWO, E, D>(ok, Q, 32 * u, s, sh.scratch[wave], l32, h);
+                    add_cols<CAREFUL, TWO, E, D>(ok, Q, 32 * u, ds, sh.scratch[wave], l32, h);
                 }
             }
         };
@@ -891,8 +960,8 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, SharedDkv<E, D>& sh, i
 }
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 2 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
-    __shared__ SharedDkv<E, D> sh;
+__global__ __launch_bounds__(256, (Geo<E, D, kDkv>::WAVES)) void win_dkv_kernel(WinArgs a) {
+    __shared__ Shared<E, D, kDkv> sh;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
     const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
@@ -1158,7 +1227,7 @@ WinArgs args_of(const WinShape& s, const void* q, const void* k, const void* v, 
     a.W = s.window < s.Tk ? s.window : (s.Tk > 0 ? s.Tk : 1);
     a.sinks = s.sinks, a.scale = s.scale, a.c = s.scale * 1.4426950408889634f;
     a.nsplit = 1, a.few = sees_few(s);
-    a.T64 = (s.T + kTile - 1) / kTile * kTile;
+    a.T64 = (s.T + 63) / 64 * 64;
     return a;
 }
 
@@ -1171,12 +1240,11 @@ void with_saved(const WinShape& s, WinArgs& a, void* saved) {
 
 unsigned grid_of(int64_t blocks) { return (unsigned)((blocks + 7) / 8 * 8); }
 
-// Tiles of keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least
-// two tiles to each.
+// Keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least 128 to each.
 int splits(const WinShape& s) {
     const int64_t blocks = (int64_t)s.B * s.H * ((s.T + kRows - 1) / kRows);
     const int64_t reach = (int64_t)s.window + kRows < s.Tk ? (int64_t)s.window + kRows : s.Tk;
-    const int64_t tiles = (reach + kTile - 1) / kTile + (s.sinks > 0);
+    const int64_t tiles = (reach + 63) / 64 + (s.sinks > 0);
     int64_t n = blocks > 0 ? 512 / blocks : 1;
     if (n > tiles / 2) n = tiles / 2;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
@@ -1265,7 +1333,7 @@ size_t window_workspace(const WinShape& s, bool backward) {
         const int n = splits(s);
         return n > 1 ? align256(n * rows * s.d * sizeof(float)) + n * rows * sizeof(float2) : 0;
     }
-    const size_t t64 = (size_t)(s.T + kTile - 1) / kTile * kTile;
+    const size_t t64 = (size_t)(s.T + 63) / 64 * 64;
     const size_t first = (size_t)s.B * s.Hk * (1 + 2 * (size_t)segments(s)) * 2 * s.sinks * s.d * sizeof(float);
     return align256(3 * s.B * s.H * t64 * sizeof(float)) + (segments(s) > 0 ? first : 0);
 }
