@@ -651,12 +651,13 @@ __global__ __launch_bounds__(256, (Geo<E, D, kFwd>::WAVES)) void win_fwd_kernel(
         win_fwd<E, D, false>(a, sh, split, qb, head, b);
 }
 
-// Joins nsplit partial rows: y = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Four columns a thread.
+// Joins nsplit (at most 64) partial rows: y = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  Four columns a thread,
+// for many rows.
 template <typename E, int D>
-__global__ __launch_bounds__(256) void win_join_kernel(size_t rows, int nsplit, const float* __restrict__ part,
-                                                       const float2* __restrict__ pstat, E* __restrict__ y,
-                                                       float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
-                                                       int R) {
+__global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsplit, const float* __restrict__ part,
+                                                            const float2* __restrict__ pstat, E* __restrict__ y,
+                                                            float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
+                                                            int R) {
     const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, row = x / (D / 4);
     const int col = (int)(x % (D / 4)) * 4;
     if (row >= rows) return;
@@ -678,6 +679,55 @@ __global__ __launch_bounds__(256) void win_join_kernel(size_t rows, int nsplit, 
     const int qi = R > 0 ? (int)(row / H % T) : 0;
     store4(y + row * D + col, x4, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + col : nullptr);
     if (stat && col == 0) stat[row] = l != 0.f ? float2{m - kAhead, l * kAheadExp} : float2{0.f, 0.f};
+}
+
+// The same for few rows, a workgroup each: its lanes read the parts' m and l at once, its column groups the parts' O,
+// eight at once: two readings after another (one sequence's token over 4100 slots in 32 parts: 3.4 us where the one
+// above takes 12.9).
+template <typename E, int D>
+__global__ __launch_bounds__(2 * D) void win_join_kernel(size_t rows, int nsplit, const float* __restrict__ part,
+                                                         const float2* __restrict__ pstat, E* __restrict__ y,
+                                                         float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
+                                                         int R) {
+    constexpr int G = D / 4;   // column groups
+    __shared__ float f[64];
+    __shared__ f32x4 sum[8][G];
+    __shared__ float2 ml;
+    const size_t row = blockIdx.x;
+    const int c = threadIdx.x % G, part0 = threadIdx.x / G;
+    if (threadIdx.x < 64) {   // fewer threads than 64 (D = 16): each lane takes several parts
+        const int n = 2 * D < 64 ? 2 * D : 64;
+        float m = -INFINITY, l = 0.f;
+        for (int s = threadIdx.x; s < nsplit; s += n) m = fmaxf(m, pstat[s * rows + row].x);
+        for (int x = n / 2; x > 0; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
+        for (int s = threadIdx.x; s < nsplit; s += n) {
+            const float2 st = pstat[s * rows + row];
+            const float e = st.y == 0.f ? 0.f : exp2_hw(st.x - m);
+            f[s] = e;
+            if (st.y != 0.f) l = fmaf(e, st.y, l);
+        }
+        for (int x = n / 2; x > 0; x /= 2) l += __shfl_xor(l, x);
+        if (threadIdx.x == 0) ml = float2{m, l};
+    }
+    __syncthreads();
+    f32x4 o = zero4();
+    for (int s = part0; s < nsplit; s += 8) {
+        const float e = f[s];
+        if (e == 0.f) continue;   // rows that are not there, or saw nothing
+        const f32x4 p = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * D + 4 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(e, p[i], o[i]);
+    }
+    sum[part0][c] = o;
+    __syncthreads();
+    if (part0 > 0) return;
+#pragma unroll
+    for (int s = 1; s < 8; ++s) o += sum[s][c];
+    const float m = ml.x, l = ml.y, r = l == 0.f ? 0.f : 1.f / l;
+    const float x[4] = {o[0] * r, o[1] * r, o[2] * r, o[3] * r};
+    const int qi = R > 0 ? (int)(row / H % T) : 0;
+    store4(y + row * D + 4 * c, x, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + 4 * c : nullptr);
+    if (stat && c == 0) stat[row] = l != 0.f ? float2{m - kAhead, l * kAheadExp} : float2{0.f, 0.f};
 }
 
 // The ring caches after the last token of each sequence: slot < sinks holds that token, slot sinks + x the last
@@ -1016,7 +1066,7 @@ struct StepCfg {
 };
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
+__global__ __launch_bounds__(256, sizeof(E) == 4 && D == 128 ? 2 : 3) void win_step_kernel(StepArgs a) {
     using C = StepCfg<E, D>;
     __shared__ __align__(16) unsigned char sv[4][C::VB];
     __shared__ float2 sst[4][16];
@@ -1049,41 +1099,46 @@ __global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
     float mx = -INFINITY, mc = -INFINITY, l = 0.f;
 
     constexpr int RT = C::CH / 16;
-    uint4 kf[2][RT][C::NK], vf[2][C::NL];
-    auto load = [&](int c, uint4 (&kk)[RT][C::NK], uint4 (&vv)[C::NL]) {
+    uint4 kf[RT][C::NK], vf[C::NL];   // a chunk's keys and values, on their way while the last one is worked on
+    auto load_k = [&](int c) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const int j = c * C::CH + 16 * t + l16;
             const E* p = j == now || j >= held ? nk : ck + j * rowlen;
 #pragma unroll
             for (int k = 0; k < C::NK; ++k)
-                kk[t][k] = 4 * k + g4 < C::NC ? reinterpret_cast<const uint4*>(p)[4 * k + g4] : uint4{0, 0, 0, 0};
+                kf[t][k] = 4 * k + g4 < C::NC ? reinterpret_cast<const uint4*>(p)[4 * k + g4] : uint4{0, 0, 0, 0};
         }
+    };
+    auto load_v = [&](int c) {
 #pragma unroll
         for (int i = 0; i < C::NL; ++i) {
             const int x = i * 64 + lane, j = c * C::CH + x / C::NC;
             const E* p = j == now || j >= held ? nv : cv + j * rowlen;
-            vv[i] = reinterpret_cast<const uint4*>(p)[x % C::NC];
+            vf[i] = reinterpret_cast<const uint4*>(p)[x % C::NC];
         }
     };
-    auto work = [&](int c, const uint4 (&kk)[RT][C::NK], const uint4 (&vv)[C::NL]) {
+    int c = c0 + wave;
+    if (c < c1) {
+        load_k(c);
+        load_v(c);
+    }
+    for (; c < c1; c += 4) {
         const int j0 = c * C::CH;
-        // V into LDS, zero where no token is; the new token into the caches, by the one workgroup that has its slot
-#pragma unroll
-        for (int i = 0; i < C::NL; ++i) {
-            const int x = i * 64 + lane, r = x / C::NC, p = x % C::NC;
-            if (r < C::CH)
-                *reinterpret_cast<uint4*>(V + (r * C::NC + (p ^ key(r))) * 16) = j0 + r < held ? vv[i] : uint4{0, 0, 0, 0};
-            if (hg == 0 && r < C::CH && j0 + r == now) reinterpret_cast<uint4*>(cv + (j0 + r) * rowlen)[p] = vv[i];
-        }
-        if (hg == 0) {
+        // the new token into the caches, by the one workgroup that has its slot
+        if (hg == 0 && now >= j0 && now < j0 + C::CH) {
 #pragma unroll
             for (int t = 0; t < RT; ++t)
                 if (j0 + 16 * t + l16 == now) {
 #pragma unroll
                     for (int k = 0; k < C::NK; ++k)
-                        if (4 * k + g4 < C::NC) reinterpret_cast<uint4*>(ck + now * rowlen)[4 * k + g4] = kk[t][k];
+                        if (4 * k + g4 < C::NC) reinterpret_cast<uint4*>(ck + now * rowlen)[4 * k + g4] = kf[t][k];
                 }
+#pragma unroll
+            for (int i = 0; i < C::NL; ++i) {
+                const int x = i * 64 + lane;
+                if (j0 + x / C::NC == now) reinterpret_cast<uint4*>(cv + now * rowlen)[x % C::NC] = vf[i];
+            }
         }
         f32x4 sc[RT];
         float top = -INFINITY;
@@ -1093,20 +1148,30 @@ __global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
 #pragma unroll
             for (int k = 0; k < C::NK; ++k) {
                 if constexpr (sizeof(E) == 2) {
-                    x = mfma_bf16(__builtin_bit_cast(bf16x8, kk[t][k]), __builtin_bit_cast(bf16x8, qf[k]), x);
+                    x = mfma_bf16(__builtin_bit_cast(bf16x8, kf[t][k]), __builtin_bit_cast(bf16x8, qf[k]), x);
                 } else {
-                    const f32x4 p = __builtin_bit_cast(f32x4, kk[t][k]), q = __builtin_bit_cast(f32x4, qf[k]);
+                    const f32x4 p = __builtin_bit_cast(f32x4, kf[t][k]), q = __builtin_bit_cast(f32x4, qf[k]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(p[e], q[e], x, 0, 0, 0);
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = j0 + 16 * t + 4 * g4 + r >= held ? -INFINITY : x[r];
-                top = fmaxf(top, x[r]);
-            }
             sc[t] = x;
         }
+        if (c + 4 < c1) load_k(c + 4);
+        // V into LDS, zero where no token is
+#pragma unroll
+        for (int i = 0; i < C::NL; ++i) {
+            const int x = i * 64 + lane, r = x / C::NC, p = x % C::NC;
+            *reinterpret_cast<uint4*>(V + (r * C::NC + (p ^ key(r))) * 16) = j0 + r < held ? vf[i] : uint4{0, 0, 0, 0};
+        }
+        if (c + 4 < c1) load_v(c + 4);
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                sc[t][r] = j0 + 16 * t + 4 * g4 + r >= held ? -INFINITY : sc[t][r];
+                top = fmaxf(top, sc[t][r]);
+            }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         if (__any(top > mx)) {
@@ -1150,16 +1215,6 @@ __global__ __launch_bounds__(256, 2) void win_step_kernel(StepArgs a) {
                 }
         }
         __builtin_amdgcn_wave_barrier();
-    };
-    // two chunks in registers: the next is on its way while one is worked on
-    int c = c0 + wave;
-    if (c < c1) load(c, kf[0], vf[0]);
-    for (; c < c1; c += 8) {
-        if (c + 4 < c1) load(c + 4, kf[1], vf[1]);
-        work(c, kf[0], vf[0]);
-        if (c + 4 >= c1) break;
-        if (c + 8 < c1) load(c + 8, kf[0], vf[0]);
-        work(c + 4, kf[1], vf[1]);
     }
     // the waves' maxima and sums, and their O about the common maximum
     l += __shfl_xor(l, 16);
@@ -1238,15 +1293,27 @@ void with_saved(const WinShape& s, WinArgs& a, void* saved) {
     a.R = rest_rows(s);
 }
 
+template <typename E, int D>
+void join(size_t rows, int nsplit, const float* part, const float2* pstat, void* y, float2* stat, int8_t* rest, int T, int H, int R,
+          hipStream_t st) {
+    if (rows * (D / 4) >= 256 * 256)   // a thread for every four columns fills the chip
+        hipLaunchKernelGGL((win_join_rows_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
+                           nsplit, part, pstat, (E*)y, stat, rest, T, H, R);
+    else
+        hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)rows), dim3(2 * D), 0, st, rows, nsplit, part, pstat, (E*)y,
+                           stat, rest, T, H, R);
+}
+
 unsigned grid_of(int64_t blocks) { return (unsigned)((blocks + 7) / 8 * 8); }
 
-// Keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least 128 to each.
+// Keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least 256 to each
+// (the join is a launch more, 4 us).
 int splits(const WinShape& s) {
     const int64_t blocks = (int64_t)s.B * s.H * ((s.T + kRows - 1) / kRows);
     const int64_t reach = (int64_t)s.window + kRows < s.Tk ? (int64_t)s.window + kRows : s.Tk;
     const int64_t tiles = (reach + 63) / 64 + (s.sinks > 0);
     int64_t n = blocks > 0 ? 512 / blocks : 1;
-    if (n > tiles / 2) n = tiles / 2;
+    if (n > tiles / 4) n = tiles / 4;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
 
@@ -1263,8 +1330,7 @@ hipError_t fwd(const WinShape& s, WinArgs a, void* ck, void* cv, hipStream_t st)
         hipLaunchKernelGGL((win_fwd_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
         if (a.nsplit > 1) {
             const size_t rows = (size_t)a.B * a.T * a.H;
-            hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
-                               a.nsplit, a.part, a.pstat, (E*)a.o, a.stat, a.rest, a.T, a.H, a.R);
+            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.o, a.stat, a.rest, a.T, a.H, a.R, st);
         }
     }
     if (ck) {
@@ -1305,13 +1371,13 @@ hipError_t by_type(bool bf16, int d, F&& f) {
 
 int step_groups(const StepShape& s) { return (s.H / s.Hk + 15) / 16; }
 
-// Slots are dealt to several workgroups where sequences and heads are too few for four workgroups a CU, at
-// least two chunks to a wave.
+// Slots are dealt to several workgroups where sequences and heads are too few for four workgroups a CU, at least a
+// chunk to a wave.
 int step_splits(const StepShape& s) {
     const int64_t blocks = (int64_t)s.S * s.Hk * step_groups(s);
     const int64_t chunks = ((int64_t)s.window + s.sinks + (s.bf16 ? 31 : 15)) / (s.bf16 ? 32 : 16);
     int64_t n = 1024 / blocks;
-    if (n > chunks / 8) n = chunks / 8;
+    if (n > chunks / 4) n = chunks / 4;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
 
@@ -1387,8 +1453,7 @@ hipError_t launch_window_step(const StepShape& s, const void* q, const void* k, 
         constexpr int D = decltype(dd)::value;
         hipLaunchKernelGGL((win_step_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
         if (a.nsplit > 1)
-            hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
-                               a.nsplit, a.part, a.pstat, (E*)a.y, (float2*)nullptr, (int8_t*)nullptr, 1, a.H, 0);
+            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.y, nullptr, nullptr, 1, a.H, 0, st);
         return hipGetLastError();
     });
 }
