@@ -48,7 +48,6 @@ constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgro
 // the sum multiplied accordingly: small weights then end where exp2's range does below the largest, not 2^8 above.
 constexpr float kAhead = 8.f, kAheadExp = 256.f;
 constexpr int kFew = 256;    // visible tokens below which a row sees few
-constexpr int kSeg = 512;    // queries a segment of the first tokens' sums
 constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which no weight is otherwise
 
 // Rows of D elements in LDS, in 16-byte pieces: piece c of row r lies at c ^ key(r), so that 16 rows read at one
@@ -364,7 +363,8 @@ struct WinArgs {
     float* part;              // forward: partial O [nsplit][B T H][D]; dk, dv: the first tokens' sums
     float2* pstat;            // forward: [nsplit][B T H]
     float* rows;              // backward: [3][B H][T64] m, 1 / l, D
-    int B, T, Tk, H, Hk, W, sinks, blocks, nsplit, nseg, T64, R;
+    float* kpart;             // dk, dv: [B Hk][ksplit][2][Tk][D], where a workgroup's queries are dealt to several
+    int B, T, Tk, H, Hk, W, sinks, blocks, nsplit, nseg, seg, ksplit, T64, R;
     float scale, c;           // c = scale log2(e)
     bool few;                 // rows see few tokens
 };
@@ -867,10 +867,11 @@ __global__ __launch_bounds__(256, (Geo<E, D, kDq>::WAVES)) void win_dq_kernel(Wi
         win_dq<E, D, false>(a, sh, qb, head, b);
 }
 
-// dk, dv.  Workgroup (b, kh, kb): 128 tokens; after those, nseg segments of the queries behind the first 128 tokens'
-// window for each (b, kh), whose waves take (32 of the first tokens, every second 32 queries).
+// dk, dv.  Workgroup (b, kh, kb, split): 128 tokens and a share of the queries that see them; after those, nseg segments
+// of the queries behind the first 128 tokens' window for each (b, kh), whose waves take (32 of the first tokens, every
+// second 32 queries).
 template <typename E, int D, bool TWO>
-__device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh, int job, int nk, int bk, int kh, int b) {
+__device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh, int job, int split, int nk, int bk, int kh, int b) {
     using R = Rows<E, D>;
     using Gm = Geo<E, D, kDkv>;
     constexpr int DT = R::DP / 32, TT = Gm::TT, NB = Gm::NB, BYTES = R::bytes(TT);
@@ -882,8 +883,8 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
     const bool live = tok < end;
     // positions of the queries: those that the window reaches, or a segment of those behind
     const int behind = max(past, kRows - 1 + min(a.W, a.Tk));
-    const int plo = seg ? behind + (job - nk) * kSeg : max(past, k0);
-    const int phi = min(seg ? plo + kSeg - 1 : k0 + kRows - 2 + min(a.W, a.Tk), end - 1);
+    const int plo = seg ? behind + (job - nk) * a.seg : max(past, k0);
+    const int phi = min(seg ? plo + a.seg - 1 : k0 + kRows - 2 + min(a.W, a.Tk), end - 1);
     const bool works = !seg || w0 < a.sinks;
 
     f32x16 ok[DT], ov[DT];
@@ -894,9 +895,11 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
         const uint32_t stride = (uint32_t)(a.H * D * (int)sizeof(E));
         const Loader<E, D, TT> ld(stride, wave, lane);
         const uint32_t lds0 = lds_of(sh.tile), row0 = lds_of(sh.row);
-        const int t0 = (plo - past) / TT, nt = (phi - past) / TT - t0 + 1, n = nt * G;
+        const int t0 = (plo - past) / TT, nt = (phi - past) / TT - t0 + 1, all = nt * G;
+        // this workgroup's n of all tiles, from i0 on
+        const int share = seg ? all : (all + a.ksplit - 1) / a.ksplit, i0 = seg ? 0 : min(split * share, all), n = min(share, all - i0);
         const size_t nrow = (size_t)a.B * a.H * a.T64;
-        int into = 0, next_t = t0, next_h = kh * G;   // the next tile: its place, its queries and head
+        int into, next_t, next_h;   // the next tile: its place, its queries and head
         auto issue = [&]() {
             const int r0 = next_t * TT;
             const uint32_t to = lds0 + (uint32_t)into * 2 * BYTES;
@@ -923,9 +926,9 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
         }
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
-            into = 0, next_t = t0, next_h = kh * G;
+            into = 0, next_t = t0 + i0 % nt, next_h = kh * G + i0 / nt;
+            int at = 0, tile = next_t;
             for (int i = 0; i < min(NB - 1, n); ++i) issue();
-            int at = 0, tile = t0;
             for (int i = 0; i < n; ++i) {
                 wait_tile<NB, 2 * Loader<E, D, TT>::N + 1>(i, n);
                 if (i + NB - 1 < n) issue();
@@ -988,7 +991,7 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
             walk(std::true_type{});
         }
     }
-    if (a.nseg > 0 && k0 == 0 && w0 < a.sinks) {   // the first tokens' sums: slot 0 the window's, 1 + 2 s + (0, 1) a segment's
+    if (a.nseg > 0 && (seg || (a.ksplit == 1 && k0 == 0)) && w0 < a.sinks) {   // the first tokens' sums: slot 0 the window's, 1 + 2 s + (0, 1) a segment's
         const int slot = seg ? 1 + 2 * (job - nk) + wave % 2 : 0;
         if (tok < a.sinks) {
             float* p = a.part + (((size_t)bk * (1 + 2 * a.nseg) + slot) * 2 * a.sinks + tok) * D;
@@ -998,6 +1001,12 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
         if (tok < a.sinks) return;
     }
     if (seg || tok >= a.Tk) return;
+    if (a.ksplit > 1) {
+        float* p = a.kpart + ((((size_t)bk * a.ksplit + split) * 2) * a.Tk + tok) * D;
+        store_row<float, D>(p, ok, a.scale, h);
+        store_row<float, D>(p + (size_t)a.Tk * D, ov, 1.f, h);
+        return;
+    }
     const size_t krow = ((size_t)b * a.Tk + tok) * a.Hk + kh;
     E *dk = (E*)a.dk + krow * D, *dv = (E*)a.dv + krow * D;
     if (live) {
@@ -1014,31 +1023,34 @@ __global__ __launch_bounds__(256, (Geo<E, D, kDkv>::WAVES)) void win_dkv_kernel(
     __shared__ Shared<E, D, kDkv> sh;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
-    const int nk = (a.Tk + kRows - 1) / kRows, per = nk + a.nseg;
-    const int job = id % per, bk = id / per, kh = bk % a.Hk, b = bk / a.Hk;
+    const int nk = (a.Tk + kRows - 1) / kRows, per = nk * a.ksplit + a.nseg;
+    const int at = id % per, bk = id / per, kh = bk % a.Hk, b = bk / a.Hk;
+    const int job = at < nk * a.ksplit ? at / a.ksplit : at - nk * (a.ksplit - 1), split = at % a.ksplit;
     // the first rows' queries are those of the first 128 tokens' workgroup
     if (sizeof(E) == 2 && (a.few || (job == 0 && a.Tk - a.T < kRows)))
-        win_dkv<E, D, sizeof(E) == 2>(a, sh, job, nk, bk, kh, b);
+        win_dkv<E, D, sizeof(E) == 2>(a, sh, job, split, nk, bk, kh, b);
     else
-        win_dkv<E, D, false>(a, sh, job, nk, bk, kh, b);
+        win_dkv<E, D, false>(a, sh, job, split, nk, bk, kh, b);
 }
 
-// dk, dv of the first tokens: their slots added up in order, four columns a thread.
+// dk, dv from their parts, added up in order, four columns a thread: of the first n tokens, or of all where the
+// queries were dealt to several workgroups.
 template <typename E, int D>
-__global__ __launch_bounds__(256) void win_first_kernel(WinArgs a) {
-    const int n = min(a.sinks, a.Tk), slots = 1 + 2 * a.nseg;
+__global__ __launch_bounds__(256) void win_sum_kernel(WinArgs a, int n) {
+    const int slots = 1 + 2 * a.nseg;
     const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, total = (size_t)a.B * a.Hk * 2 * n * (D / 4);
     if (x >= total) return;
     const int col = (int)(x % (D / 4)) * 4, tok = (int)(x / (D / 4) % n), of = (int)(x / (D / 4) / n % 2);
     const int bk = (int)(x / (D / 4) / n / 2), kh = bk % a.Hk, b = bk / a.Hk;
     f32x4 s = zero4();
-    for (int i = 0; i < slots; ++i)
-        s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
-    E* p = (E*)(of ? a.dv : a.dk) + (((size_t)b * a.Tk + tok) * a.Hk + kh) * D + col;
-    if constexpr (sizeof(E) == 2)
-        *reinterpret_cast<uint2*>(p) = uint2{cvt_pk_bf16(s[0], s[1]), cvt_pk_bf16(s[2], s[3])};
-    else
-        *reinterpret_cast<float4*>(p) = float4{s[0], s[1], s[2], s[3]};
+    if (a.ksplit > 1)
+        for (int i = 0; i < a.ksplit; ++i)
+            s += *reinterpret_cast<const f32x4*>(a.kpart + ((((size_t)bk * a.ksplit + i) * 2 + of) * a.Tk + tok) * D + col);
+    if (a.nseg > 0 && tok < a.sinks)
+        for (int i = a.ksplit > 1 ? 1 : 0; i < slots; ++i)
+            s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
+    const float f[4] = {s[0], s[1], s[2], s[3]};
+    store4((E*)(of ? a.dv : a.dk) + (((size_t)b * a.Tk + tok) * a.Hk + kh) * D + col, f, nullptr);
 }
 
 // ---------------------------------------------------------------- one token for S sequences
@@ -1281,7 +1293,7 @@ WinArgs args_of(const WinShape& s, const void* q, const void* k, const void* v, 
     a.B = s.B, a.T = s.T, a.Tk = s.Tk, a.H = s.H, a.Hk = s.Hk;
     a.W = s.window < s.Tk ? s.window : (s.Tk > 0 ? s.Tk : 1);
     a.sinks = s.sinks, a.scale = s.scale, a.c = s.scale * 1.4426950408889634f;
-    a.nsplit = 1, a.few = sees_few(s);
+    a.nsplit = a.ksplit = 1, a.few = sees_few(s);
     a.T64 = (s.T + 63) / 64 * 64;
     return a;
 }
@@ -1317,11 +1329,31 @@ int splits(const WinShape& s) {
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
 
+// The queries that see 128 tokens are dealt to several workgroups where tokens are too few for a workgroup a CU, at
+// least 128 (of all heads that share the tokens) to each: B3 T777 H6 Hk2 d64 window 100, 42 workgroups of which left
+// most of the chip idle, took 71 us for its backward, dealt to five each 43.
+int key_splits(const WinShape& s) {
+    const int64_t blocks = (int64_t)s.B * s.Hk * (((int64_t)s.Tk + kRows - 1) / kRows);
+    const int64_t W = s.window < s.Tk ? s.window : s.Tk, reach = W + kRows < s.T ? W + kRows : s.T;
+    if (blocks == 0 || blocks >= 256) return 1;
+    int64_t n = 512 / blocks;
+    if (n > reach * (s.H / s.Hk) / 128) n = reach * (s.H / s.Hk) / 128;
+    return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
+}
+
+// Queries a segment of the first tokens' sums: twice as many as a workgroup of 128 tokens walks (each of its waves takes
+// every second 32), and at most 512, so that no segment outlasts the rest (B8 T2048 H16 d128 window 512: 387 us for the
+// backward, with 1024 424).
+int segment(const WinShape& s) {
+    const int64_t W = s.window < s.Tk ? s.window : s.Tk, n = 2 * (W + kRows) < 512 ? 2 * (W + kRows) : 512;
+    return (int)(n / key_splits(s) < 64 ? 64 : n / key_splits(s) / 64 * 64);
+}
+
 int segments(const WinShape& s) {
     if (s.sinks == 0) return 0;
     const int64_t W = s.window < s.Tk ? s.window : s.Tk, past = s.Tk - s.T;
     const int64_t behind = past > kRows - 1 + W ? past : kRows - 1 + W, n = s.Tk - behind;
-    return n > 0 ? (int)((n + kSeg - 1) / kSeg) : 0;
+    return n > 0 ? (int)((n + segment(s) - 1) / segment(s)) : 0;
 }
 
 template <typename E, int D>
@@ -1349,11 +1381,12 @@ hipError_t bwd(WinArgs a, hipStream_t st) {
     if (nk == 0) return hipSuccess;
     a.blocks = a.B * a.H * nq;
     if (a.blocks > 0) hipLaunchKernelGGL((win_dq_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
-    a.blocks = a.B * a.Hk * (nk + a.nseg);
+    a.blocks = a.B * a.Hk * (nk * a.ksplit + a.nseg);
     hipLaunchKernelGGL((win_dkv_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
-    if (a.nseg > 0) {
-        const size_t n = (size_t)a.B * a.Hk * 2 * (a.sinks < a.Tk ? a.sinks : a.Tk) * (D / 4);
-        hipLaunchKernelGGL((win_first_kernel<E, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+    if (a.nseg > 0 || a.ksplit > 1) {
+        const int n = a.ksplit > 1 || a.sinks > a.Tk ? a.Tk : a.sinks;
+        const size_t threads = (size_t)a.B * a.Hk * 2 * n * (D / 4);
+        hipLaunchKernelGGL((win_sum_kernel<E, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, n);
     }
     return hipGetLastError();
 }
@@ -1385,7 +1418,7 @@ int step_splits(const StepShape& s) {
 
 int64_t window_blocks(const WinShape& s) {
     const int64_t nq = ((int64_t)s.T + kRows - 1) / kRows, nk = ((int64_t)s.Tk + kRows - 1) / kRows;
-    const int64_t fwd = (int64_t)s.B * s.H * nq, dkv = (int64_t)s.B * s.Hk * (nk + segments(s));
+    const int64_t fwd = (int64_t)s.B * s.H * nq, dkv = (int64_t)s.B * s.Hk * (nk * key_splits(s) + segments(s));
     return fwd > dkv ? fwd : dkv;
 }
 
@@ -1399,9 +1432,10 @@ size_t window_workspace(const WinShape& s, bool backward) {
         const int n = splits(s);
         return n > 1 ? align256(n * rows * s.d * sizeof(float)) + n * rows * sizeof(float2) : 0;
     }
-    const size_t t64 = (size_t)(s.T + 63) / 64 * 64;
-    const size_t first = (size_t)s.B * s.Hk * (1 + 2 * (size_t)segments(s)) * 2 * s.sinks * s.d * sizeof(float);
-    return align256(3 * s.B * s.H * t64 * sizeof(float)) + (segments(s) > 0 ? first : 0);
+    const size_t t64 = (size_t)(s.T + 63) / 64 * 64, rest = (size_t)s.B * s.Hk * 2 * s.d * sizeof(float);
+    const int nseg = segments(s), n = key_splits(s);
+    return align256(3 * s.B * s.H * t64 * sizeof(float)) + align256(nseg > 0 ? rest * (1 + 2 * (size_t)nseg) * s.sinks : 0) +
+           (n > 1 ? rest * n * s.Tk : 0);
 }
 
 hipError_t launch_window_fwd(const WinShape& s, const void* q, const void* k, const void* v, const int* len, void* y,
@@ -1425,8 +1459,9 @@ hipError_t launch_window_bwd(const WinShape& s, const void* q, const void* k, co
     a.y = y, a.dy = dy, a.dq = dq, a.dk = dk, a.dv = dv;
     with_saved(s, a, const_cast<void*>(saved));
     a.rows = static_cast<float*>(ws);
-    a.nseg = segments(s);
+    a.nseg = segments(s), a.seg = segment(s), a.ksplit = key_splits(s);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(3 * (size_t)s.B * s.H * a.T64 * sizeof(float)));
+    a.kpart = a.part + align256(a.nseg > 0 ? (size_t)s.B * s.Hk * 2 * s.d * sizeof(float) * (1 + 2 * (size_t)a.nseg) * s.sinks : 0) / 4;
     return by_type(s.bf16, s.d, [&](auto e, auto d) { return bwd<decltype(e), decltype(d)::value>(a, st); });
 }
 
