@@ -158,17 +158,47 @@ __device__ __forceinline__ f32x16 zero16() {
     return z;
 }
 
+// N products whose operands come from LDS, read AHEAD products before.  The scheduler, left alone, sinks each read to
+// its product and waits for it; the barriers let only other arithmetic (0x6) pass.
+template <int N, int AHEAD, typename Read, typename Mul>
+__device__ __forceinline__ void stream(Read read, Mul mul) {
+    constexpr int A = AHEAD < N ? AHEAD : N;
+    bf16x8 f[A];
+#pragma unroll
+    for (int i = 0; i < A; ++i) f[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0x6);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        mul(i, f[i % A]);
+        if (i + A < N) f[i % A] = read(i + A);
+        __builtin_amdgcn_sched_barrier(0x6);
+    }
+}
+
+__device__ __forceinline__ bf16x8 read16(const unsigned char* p) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p));
+}
+
 // C = (rows row0 .. row0 + 31 of the tile) (row b of each lane)^T
 template <int D>
 __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const Row<uint16_t, D>& b, int l32, int h) {
+    using R = Rows<uint16_t, D>;
     f32x16 c = zero16();
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        using R = Rows<uint16_t, D>;
-        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + R::row(row0) + R::row_at(l32, h, k)));
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.x[k], c, 0, 0, 0);
-    }
+    stream<D / 16, 4>([&](int k) { return read16(t + R::row(row0) + R::row_at(l32, h, k)); },
+                      [&](int k, const bf16x8& a) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.x[k], c, 0, 0, 0); });
     return c;
+}
+// Two of them in turn, which do not wait for each other's sums.
+template <int D>
+__device__ __forceinline__ void rows_dot_two(const unsigned char* t0, const unsigned char* t1, int row0, const Row<uint16_t, D>& b0,
+                                             const Row<uint16_t, D>& b1, f32x16& c0, f32x16& c1, int l32, int h) {
+    using R = Rows<uint16_t, D>;
+    c0 = c1 = zero16();
+    stream<D / 8, 4>([&](int i) { return read16((i % 2 ? t1 : t0) + R::row(row0) + R::row_at(l32, h, i / 2)); },
+                     [&](int i, const bf16x8& a) {
+                         f32x16& c = i % 2 ? c1 : c0;
+                         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, (i % 2 ? b1 : b0).x[i / 2], c, 0, 0, 0);
+                     });
 }
 template <int D>
 __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const Row<float, D>& b, int l32, int h) {
@@ -183,22 +213,36 @@ __device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, con
     return c;
 }
 
-// The same with b's rows in LDS, l32 of them from p on.
+template <int D>
+__device__ __forceinline__ void rows_dot_two(const unsigned char* t0, const unsigned char* t1, int row0, const Row<float, D>& b0,
+                                             const Row<float, D>& b1, f32x16& c0, f32x16& c1, int l32, int h) {
+    c0 = rows_dot<D>(t0, row0, b0, l32, h);
+    c1 = rows_dot<D>(t1, row0, b1, l32, h);
+}
+
+// The same with b0's rows in LDS, l32 of them from p on.
 struct RowsAt {
     const unsigned char* p;
 };
 template <int D>
-__device__ __forceinline__ f32x16 rows_dot(const unsigned char* t, int row0, const RowsAt& b, int l32, int h) {
+__device__ __forceinline__ void rows_dot_two(const unsigned char* t0, const unsigned char* t1, int row0, const RowsAt& b0,
+                                             const Row<uint16_t, D>& b1, f32x16& c0, f32x16& c1, int l32, int h) {
     using R = Rows<uint16_t, D>;
-    f32x16 c = zero16();
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        const int at = R::row_at(l32, h, k);
-        const bf16x8 x = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(t + R::row(row0) + at));
-        const bf16x8 y = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(b.p + at));
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
-    }
-    return c;
+    c0 = c1 = zero16();
+    bf16x8 q{};
+    stream<3 * D / 16, 5>(   // a row of t0, of b0, of t1 in turn
+        [&](int i) {
+            const int at = R::row_at(l32, h, i / 3);
+            return read16(i % 3 == 1 ? b0.p + at : (i % 3 ? t1 : t0) + R::row(row0) + at);
+        },
+        [&](int i, const bf16x8& a) {
+            if (i % 3 == 0)
+                q = a;
+            else if (i % 3 == 1)
+                c0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, a, c0, 0, 0, 0);
+            else
+                c1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b1.x[i / 3], c1, 0, 0, 0);
+        });
 }
 
 // Weights of 32 rows (a C, register r at row 8 (r / 4) + 4 h + r % 4) as the operand of a product over them.
@@ -221,30 +265,33 @@ struct Weights<float> {
     __device__ explicit Weights(const f32x16& w) : w(w) {}
 };
 
-// c += (columns 32 t .. 32 t + 31 of rows row0 .. row0 + 31)^T w
+// o[t] += (columns 32 t .. 32 t + 31 of rows row0 .. row0 + 31)^T w
 template <int D>
-__device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int t, const Weights<uint16_t>& w, f32x16 c,
-                                           int l32, int h) {
+__device__ __forceinline__ void cols_dot(Acc<uint16_t, D>& o, const unsigned char* x, int row0, const Weights<uint16_t>& w, int l32,
+                                         int h) {
     using R = Rows<uint16_t, D>;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const unsigned char* p = x + R::row(row0 + 16 * k);
-        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, t, false)));
-        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, t, true)));
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), w.b[k], c, 0, 0, 0);
-    }
-    return c;
+    constexpr int DT = R::DP / 32;
+    stream<2 * DT, 4>(
+        [&](int i) {
+            const unsigned char* p = x + R::row(row0 + 16 * (i / DT));
+            const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, i % DT, false)));
+            const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + R::col_at(l32, h, i % DT, true)));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        },
+        [&](int i, const bf16x8& a) {
+            o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w.b[i / DT], o[i % DT], 0, 0, 0);
+        });
 }
 template <int D>
-__device__ __forceinline__ f32x16 cols_dot(const unsigned char* x, int row0, int t, const Weights<float>& w, f32x16 c,
-                                           int l32, int h) {
+__device__ __forceinline__ void cols_dot(Acc<float, D>& o, const unsigned char* x, int row0, const Weights<float>& w, int l32, int h) {
     using R = Rows<float, D>;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const float a = *reinterpret_cast<const float*>(x + R::row(row0) + R::at(8 * (r / 4) + 4 * h + r % 4, 32 * t + l32));
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], c, 0, 0, 0);
-    }
-    return c;
+    for (int t = 0; t < R::DP / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float a = *reinterpret_cast<const float*>(x + R::row(row0) + R::at(8 * (r / 4) + 4 * h + r % 4, 32 * t + l32));
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], o[t], 0, 0, 0);
+        }
 }
 
 __device__ __forceinline__ float elem(const unsigned char* p, uint16_t) {
@@ -293,13 +340,8 @@ __device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, i
         for (int t = 0; t < Rows<E, D>::DP / 32; ++t) cols_apart<E, D>(o[t], x, row0, t, w, scratch, l32, h);
     } else {
         const Weights<E> b(w);
-#pragma unroll
-        for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, b, o[t], l32, h);
-        if constexpr (sizeof(E) == 2 && TWO) {
-            const Weights<E> rest(left_of(w, b));
-#pragma unroll
-            for (int t = 0; t < Rows<E, D>::DP / 32; ++t) o[t] = cols_dot<D>(x, row0, t, rest, o[t], l32, h);
-        }
+        cols_dot<D>(o, x, row0, b, l32, h);
+        if constexpr (sizeof(E) == 2 && TWO) cols_dot<D>(o, x, row0, Weights<E>(left_of(w, b)), l32, h);
     }
 }
 
@@ -339,19 +381,6 @@ __device__ __forceinline__ float halves_max(float x) {
     float a, b;
     both_halves(x, a, b);
     return fmaxf(a, b);
-}
-
-// Groups for the scheduler, which left alone reads LDS one or two operands before their use and waits for each:
-// reads run `ahead`, then one product, `reads` reads and `valu` other operations in turn.
-template <int MFMA, int READS, int AHEAD, int VALU>
-__device__ __forceinline__ void paced() {
-    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-    for (int i = 0; i < MFMA; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (AHEAD + i * READS / MFMA < READS) __builtin_amdgcn_sched_group_barrier(0x100, READS / MFMA > 0 ? READS / MFMA : 1, 0);
-        if (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
-    }
 }
 
 struct WinArgs {
@@ -557,7 +586,6 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
             f32x16 s[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
-            if (!CAREFUL && sizeof(E) == 2) paced<U * D / 16, U * D / 16, U * D / 32, 0>();
             if (masked) hide<U>(a, s, j0, pos, h, -INFINITY);
             float top = s[0][0];
 #pragma unroll
@@ -587,11 +615,6 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
             l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
             for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, V, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
-            if (!CAREFUL && !TWO && sizeof(E) == 2) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 40, 0);
-                paced<2 * U * DT, 4 * U * DT, 0, 20 / DT>();
-            }
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
@@ -662,12 +685,14 @@ __global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsp
     const int col = (int)(x % (D / 4)) * 4;
     if (row >= rows) return;
     float m = -INFINITY;
+#pragma unroll 4
     for (int s = 0; s < nsplit; ++s) m = fmaxf(m, pstat[s * rows + row].x);
     float l = 0.f;
     f32x4 o = zero4();
+#pragma unroll 2
     for (int s = 0; s < nsplit; ++s) {
         const float2 st = pstat[s * rows + row];
-        if (st.y == 0.f) continue;
+        if (st.y == 0.f) continue;   // a row that is not there, or saw nothing: its part was not written
         const float f = exp2_hw(st.x - m);
         l = fmaf(f, st.y, l);
         const f32x4 p = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * D + col);
@@ -805,20 +830,14 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
             f32x16 s[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                s[u] = rows_dot<D>(K, u0 + 32 * u, q, l32, h);
-                const f32x16 dp = rows_dot<D>(V, u0 + 32 * u, g, l32, h);
+                f32x16 dp;
+                rows_dot_two<D>(K, V, u0 + 32 * u, q, g, s[u], dp, l32, h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
-            }
-            if (!CAREFUL && sizeof(E) == 2) {
-                constexpr int M = D / 16;   // products of S, and of dP
-                paced<2 * M, 2 * U * M, 6, 0>();
-                if (U > 1) paced<2 * M, 0, 0, 36 / M>();
             }
             if (masked) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
 #pragma unroll
             for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, K, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
-            if (!CAREFUL && !TWO && sizeof(E) == 2) paced<2 * U * DT, 4 * U * DT, 8, 4>();
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
@@ -944,8 +963,8 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
                         (pp - a.W >= w0 + 31 && w0 >= a.sinks))
                         continue;
                     const bool masked = pp < w0 + 31 || pp + 31 - a.W >= w0 || pp < plo || pp + 31 > phi;
-                    f32x16 s = rows_dot<D>(Q, 32 * u, k, l32, h);
-                    f32x16 ds = rows_dot<D>(G_, 32 * u, v, l32, h);
+                    f32x16 s, ds;
+                    rows_dot_two<D>(Q, G_, 32 * u, k, v, s, ds, l32, h);
                     const float* sr = rows + 32 * u;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -1044,9 +1063,11 @@ __global__ __launch_bounds__(256) void win_sum_kernel(WinArgs a, int n) {
     const int bk = (int)(x / (D / 4) / n / 2), kh = bk % a.Hk, b = bk / a.Hk;
     f32x4 s = zero4();
     if (a.ksplit > 1)
+#pragma unroll 4
         for (int i = 0; i < a.ksplit; ++i)
             s += *reinterpret_cast<const f32x4*>(a.kpart + ((((size_t)bk * a.ksplit + i) * 2 + of) * a.Tk + tok) * D + col);
     if (a.nseg > 0 && tok < a.sinks)
+#pragma unroll 4
         for (int i = a.ksplit > 1 ? 1 : 0; i < slots; ++i)
             s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
     const float f[4] = {s[0], s[1], s[2], s[3]};
