@@ -5,9 +5,9 @@
 // j is visible to the query at position p iff j <= p and (j > p - W or j < sinks).  H query heads share Hk heads
 // of keys and values.  Queries are the last T of Tk tokens; a sequence ends at len.
 //
-// Forward and dq: a wave owns 32 queries of a head, the workgroup's four 128.  Tiles of 64 tokens' keys and
+// Forward and dq: a wave owns 32 queries of a head, the workgroup's four 128.  Tiles of 32 or 64 tokens' keys and
 // values go through LDS, loaded a tile ahead.  Scores are formed transposed, S^T = K Q^T (tokens x queries), so
-// that a query is a lane's column: its running maximum and sum are one value a lane and one exchange between the
+// that a query is a lane's column: its running reference and sum are one value a lane and one exchange between the
 // wave's halves, and S^T, rounded to the operands' type, is the operand of O^T += V^T P^T as it stands.
 //   m, l: a reference near the largest score and the sum of exponentials about it.
 //   dS = P (dy . v - D),  D = dy . y,  dq = scale dS K
@@ -16,6 +16,13 @@
 // writer, so results do not depend on the order of workgroups.  First tokens are seen by all later queries:
 // the queries behind the window of the first 128 tokens are cut into segments, whose sums over those tokens are
 // joined.
+//
+// What bounds it.  Long windows: matrix work; a prompt of B1 T65536 H16 Hk4 d128 window 2048 takes 1.18 ms, 920
+// TFLOP/s of its 1085 GFLOP (a large product reaches 1240), at a clock that the card's power holds to 1.8 GHz.
+// B8 T2048 H16 d128 window 512: 107 us forward (two products of a tile), 153 dq (three), 211 dk and dv (four), the
+// matrix cores busy for a quarter of the time at 2.4 GHz: a wave's chain of products, exponentials and reads of
+// LDS, of which two or three waves a SIMD hide a part; its registers allow no more.  fp32: 153 TFLOP/s of its
+// matrix instructions.  The step: HBM, 5.6 TB/s (S512 Hk4 d128 over 1028 slots, 191 us).
 //
 // v_mfma_f32_32x32x16_bf16 (lane l, half h = l / 32): A row l % 32 and B column l % 32, contraction 8 h .. 8 h + 7;
 // C column l % 32, register r at row 8 (r / 4) + 4 h + r % 4.  Over the contraction of a C used as B, half h
@@ -159,7 +166,8 @@ __device__ __forceinline__ f32x16 zero16() {
 }
 
 // N products whose operands come from LDS, read AHEAD products before.  The scheduler, left alone, sinks each read to
-// its product and waits for it; the barriers let only other arithmetic (0x6) pass.
+// its product and waits for it (backward 395 us, 370 this way; 3 to 7 ahead are alike); the barriers let only other
+// arithmetic (0x6) pass.
 template <int N, int AHEAD, typename Read, typename Mul>
 __device__ __forceinline__ void stream(Read read, Mul mul) {
     constexpr int A = AHEAD < N ? AHEAD : N;
@@ -492,7 +500,8 @@ __device__ __forceinline__ void store_zero(E* p, int h) {
 // How a pass (forward, dq, or dk and dv) goes over its tiles: TT tokens (queries for dk, dv) a tile, NB tiles in LDS
 // (one worked on, the others on their way), U halves of 32 at once, WAVES a SIMD.  At 128 bf16 columns tiles of 32
 // leave the forward registers for three waves a SIMD (B8 T2048 H16 window 512: 107 us, with tiles of 64 and two
-// waves 121).  fp32 products take four times as long as they need for their operands' latency: one wave will do.
+// waves 121; three tiles in LDS instead of two gain nothing there).  fp32: as many waves as registers allow (B64 T512
+// H4 d32: forward 40 us, 50 with one a SIMD).
 enum Pass { kFwd, kDq, kDkv };
 template <typename E, int D, Pass P>
 struct Geo {
@@ -503,7 +512,7 @@ struct Geo {
     static constexpr int WAVES = !BF ? (D < 128 ? 2 : 1) : D == 128 && P == kFwd ? 3 : 2;
     static constexpr int NB = BF && D < 128 && P != kFwd ? 3 : 2;
     // dk, dv at 128 bf16 columns: the tokens' keys stay in LDS; with them in registers, beside their values and both
-    // sums, some of each were stored and loaded again around every tile.
+    // sums, some of each were stored and loaded again around every tile (backward 447 us, 390 with the keys in LDS).
     static constexpr bool KEYS = BF && D == 128 && P == kDkv;
 };
 
@@ -1088,7 +1097,10 @@ struct StepArgs {
 
 // Workgroup (s, kh, 16 query heads, split): its waves take chunks of 32 (fp32: 16) slots in turn and join at the
 // end.  K goes from memory straight into operands, V through LDS of the wave's own, to be read across.
-// S^T = K Q^T (slots x heads) in 16 x 16 tiles, O^T += V^T P^T.
+// S^T = K Q^T (slots x heads) in 16 x 16 tiles, O^T += V^T P^T.  HBM bounds it: the next chunk's keys and values are
+// asked for as soon as the registers of this one's are free, and three waves a SIMD (168 registers) keep enough on
+// their way.  With two chunks in registers instead they were stored and loaded again: 318 us for 512 sequences over
+// 1028 slots of 4 heads of 128, 191 this way.
 template <typename E, int D>
 struct StepCfg {
     static constexpr int CH = sizeof(E) == 2 ? 32 : 16, DP = D < 16 ? 16 : D, DT = D / 16;
