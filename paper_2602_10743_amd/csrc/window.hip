@@ -1066,21 +1066,22 @@ __global__ __launch_bounds__(256, (Geo<E, D, kDkv>::WAVES)) void win_dkv_kernel(
 template <typename E, int D>
 __global__ __launch_bounds__(256) void win_sum_kernel(WinArgs a, int n) {
     const int slots = 1 + 2 * a.nseg;
-    const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, total = (size_t)a.B * a.Hk * 2 * n * (D / 4);
-    if (x >= total) return;
-    const int col = (int)(x % (D / 4)) * 4, tok = (int)(x / (D / 4) % n), of = (int)(x / (D / 4) / n % 2);
-    const int bk = (int)(x / (D / 4) / n / 2), kh = bk % a.Hk, b = bk / a.Hk;
-    f32x4 s = zero4();
-    if (a.ksplit > 1)
+    const size_t total = (size_t)a.B * a.Hk * 2 * n * (D / 4);
+    for (size_t x = (size_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (size_t)gridDim.x * 256) {
+        const int col = (int)(x % (D / 4)) * 4, tok = (int)(x / (D / 4) % n), of = (int)(x / (D / 4) / n % 2);
+        const int bk = (int)(x / (D / 4) / n / 2), kh = bk % a.Hk, b = bk / a.Hk;
+        f32x4 s = zero4();
+        if (a.ksplit > 1)
 #pragma unroll 4
-        for (int i = 0; i < a.ksplit; ++i)
-            s += *reinterpret_cast<const f32x4*>(a.kpart + ((((size_t)bk * a.ksplit + i) * 2 + of) * a.Tk + tok) * D + col);
-    if (a.nseg > 0 && tok < a.sinks)
+            for (int i = 0; i < a.ksplit; ++i)
+                s += *reinterpret_cast<const f32x4*>(a.kpart + ((((size_t)bk * a.ksplit + i) * 2 + of) * a.Tk + tok) * D + col);
+        if (a.nseg > 0 && tok < a.sinks)
 #pragma unroll 4
-        for (int i = a.ksplit > 1 ? 1 : 0; i < slots; ++i)
-            s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
-    const float f[4] = {s[0], s[1], s[2], s[3]};
-    store4((E*)(of ? a.dv : a.dk) + (((size_t)b * a.Tk + tok) * a.Hk + kh) * D + col, f, nullptr);
+            for (int i = a.ksplit > 1 ? 1 : 0; i < slots; ++i)
+                s += *reinterpret_cast<const f32x4*>(a.part + ((((size_t)bk * slots + i) * 2 + of) * a.sinks + tok) * D + col);
+        const float f[4] = {s[0], s[1], s[2], s[3]};
+        store4((E*)(of ? a.dv : a.dk) + (((size_t)b * a.Tk + tok) * a.Hk + kh) * D + col, f, nullptr);
+    }
 }
 
 // ---------------------------------------------------------------- one token for S sequences
@@ -1419,7 +1420,8 @@ hipError_t bwd(WinArgs a, hipStream_t st) {
     if (a.nseg > 0 || a.ksplit > 1) {
         const int n = a.ksplit > 1 || a.sinks > a.Tk ? a.Tk : a.sinks;
         const size_t threads = (size_t)a.B * a.Hk * 2 * n * (D / 4);
-        hipLaunchKernelGGL((win_sum_kernel<E, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, n);
+        const size_t blocks = (threads + 255) / 256;   // a launch's threads are 32-bit
+        hipLaunchKernelGGL((win_sum_kernel<E, D>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, st, a, n);
     }
     return hipGetLastError();
 }
