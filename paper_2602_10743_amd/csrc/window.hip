@@ -17,7 +17,7 @@
 // the queries behind the window of the first 128 tokens are cut into segments, whose sums over those tokens are
 // joined.
 //
-// What bounds it.  Long windows: matrix work; a prompt of B1 T65536 H16 Hk4 d128 window 2048 takes 1.18 ms, 920
+// What bounds it.  Long windows: matrix work; a prompt of B1 T65536 H16 Hk4 d128 window 2048 takes 1.10 ms, 980
 // TFLOP/s of its 1085 GFLOP (a large product reaches 1240), at a clock that the card's power holds to 1.8 GHz.
 // B8 T2048 H16 d128 window 512: 107 us forward (two products of a tile), 153 dq (three), 211 dk and dv (four), the
 // matrix cores busy for a quarter of the time at 2.4 GHz: a wave's chain of products, exponentials and reads of
@@ -669,6 +669,17 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
     if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc - kAhead, l * kAheadExp} : float2{0.f, 0.f};
 }
 
+// Workgroup id's block of queries, head and sequence.  Heads that share keys go side by side, then blocks in order, where
+// the window makes most alike, since they read on in the tiles that the last ones left in L2 (B1 T65536 H16 Hk4 window
+// 2048: 1.06 ms; head after head 1.12, the blocks backwards 1.17), or the longest first where they are not alike (B2
+// T4096 window 4096: 179 us, in order 191).
+__device__ __forceinline__ void place_of(const WinArgs& a, int id, int& qb, int& head, int& b) {
+    const int nq = (a.T + kRows - 1) / kRows, G = a.H / a.Hk, at = id / G % nq, rest = id / G / nq;
+    qb = 2 * (int64_t)a.W > a.T ? nq - 1 - at : at;
+    head = rest % a.Hk * G + id % G;
+    b = rest / a.Hk;
+}
+
 template <typename E, int D>
 __global__ __launch_bounds__(256, (Geo<E, D, kFwd>::WAVES)) void win_fwd_kernel(WinArgs a) {
     __shared__ Shared<E, D, kFwd> sh;
@@ -676,7 +687,8 @@ __global__ __launch_bounds__(256, (Geo<E, D, kFwd>::WAVES)) void win_fwd_kernel(
     if (id >= a.blocks) return;
     const int split = id % a.nsplit;
     id /= a.nsplit;
-    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    int qb, head, b;
+    place_of(a, id, qb, head, b);
     if (sizeof(E) == 2 && (a.few || a.Tk - a.T + qb * kRows < kRows))
         win_fwd<E, D, sizeof(E) == 2>(a, sh, split, qb, head, b);
     else
@@ -888,7 +900,8 @@ __global__ __launch_bounds__(256, (Geo<E, D, kDq>::WAVES)) void win_dq_kernel(Wi
     __shared__ Shared<E, D, kDq> sh;
     const int id = block_of(a.blocks);
     if (id >= a.blocks) return;
-    const int nq = (a.T + kRows - 1) / kRows, qb = nq - 1 - id % nq, head = id / nq % a.H, b = id / nq / a.H;
+    int qb, head, b;
+    place_of(a, id, qb, head, b);
     if (sizeof(E) == 2 && (a.few || a.Tk - a.T + qb * kRows < kRows))
         win_dq<E, D, sizeof(E) == 2>(a, sh, qb, head, b);
     else
