@@ -51,9 +51,9 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgroup
 // The exponents' reference lies this far above the largest score (times c, rounded up) that moved it: weights are at
 // most 1, and a row is rescaled only when a score passes the reference, not whenever the maximum grows, which one of
-// a wave's 32 rows does in nearly every tile.  The backward takes it lower by as much (a whole number, exactly), with
-// the sum multiplied accordingly: small weights then end where exp2's range does below the largest, not 2^8 above.
-constexpr float kAhead = 8.f, kAheadExp = 256.f;
+// a wave's 32 rows does in nearly every tile.  The backward takes it lower by as much, with the sum multiplied
+// accordingly (context): small weights then end where exp2's range does below the largest, not 2^8 above.
+constexpr float kAhead = 8.f;
 constexpr int kFew = 256;    // visible tokens below which a row sees few
 constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which no weight is otherwise
 
@@ -373,6 +373,15 @@ __device__ __forceinline__ bool any_of(bool x, int* flag) {
     return *flag != 0;
 }
 
+// What the backward takes of a row with reference m and sum l: the reference less kAhead, and the sum about that.  m is a
+// whole number, but past 2^27 fp32 has no step of 8: the sum is multiplied by 2 to the distance that came out (0, 8 or
+// 16), exactly.  Rows without a score have zeros.
+__device__ __forceinline__ float2 context(float m, float l) {
+    if (l == 0.f) return float2{0.f, 0.f};
+    const float low = m - kAhead;
+    return float2{low, ldexpf(l, (int)(m - low))};
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // The value of the lane 32 away: of two copies the instruction swaps one's upper half with the other's lower one.
 __device__ __forceinline__ void both_halves(float x, float& lower, float& upper) {
@@ -666,7 +675,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
         store_row<E, D>(y, o, 1.f / l, h, qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr);
     else
         store_zero<E, D>(y, h);
-    if (a.stat && h == 0) a.stat[row] = live && l != 0.f ? float2{mc - kAhead, l * kAheadExp} : float2{0.f, 0.f};
+    if (a.stat && h == 0) a.stat[row] = context(mc, live ? l : 0.f);
 }
 
 // Workgroup id's block of queries, head and sequence.  Heads that share keys go side by side, then blocks in order, where
@@ -724,7 +733,7 @@ __global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsp
     const float x4[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
     const int qi = R > 0 ? (int)(row / H % T) : 0;
     store4(y + row * D + col, x4, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + col : nullptr);
-    if (stat && col == 0) stat[row] = l != 0.f ? float2{m - kAhead, l * kAheadExp} : float2{0.f, 0.f};
+    if (stat && col == 0) stat[row] = context(m, l);
 }
 
 // The same for few rows, a workgroup each: its lanes read the parts' m and l at once, its column groups the parts' O,
@@ -773,7 +782,7 @@ __global__ __launch_bounds__(2 * D) void win_join_kernel(size_t rows, int nsplit
     const float x[4] = {o[0] * r, o[1] * r, o[2] * r, o[3] * r};
     const int qi = R > 0 ? (int)(row / H % T) : 0;
     store4(y + row * D + 4 * c, x, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + 4 * c : nullptr);
-    if (stat && c == 0) stat[row] = l != 0.f ? float2{m - kAhead, l * kAheadExp} : float2{0.f, 0.f};
+    if (stat && c == 0) stat[row] = context(m, l);
 }
 
 // The ring caches after the last token of each sequence: slot < sinks holds that token, slot sinks + x the last

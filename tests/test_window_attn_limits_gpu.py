@@ -1,0 +1,36 @@
+"""Attention with a sliding window at the ends of its ranges: scores whose references have few digits left, rows without
+a score, weights of zero beside infinities, and what bf16 keeps of the rows of few tokens.  Tolerances as in
+test_window_attn_gpu.py."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from test_window_attn_gpu import DEV, TYPES, U, check, dev, expected, kla, make, run  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+FAR = [  # B, T, past, H, Hk, d, window, sinks: one workgroup a row, and keys dealt to several, joined in either way
+    (2, 40, 0, 2, 1, 64, 9, 2),
+    (1, 3, 1400, 2, 1, 64, 1500, 0),
+    (1, 600, 0, 4, 2, 128, 600, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", FAR, ids=lambda c: "-".join(map(str, c)))
+@pytest.mark.parametrize("unit,key", [(12, 1.0), (14, 0.375), (14, -0.375), (14, 1.0), (14, -1.0)])
+def test_scores_whose_reference_has_few_digits(kla, case, dtype, unit, key):
+    """All scores of a row are alike, key 2^(2 unit) and exact, so P is 1 / n as for scores of `key`, and the gradients
+    are those times 2^unit.  Exponents of up to 32 about a reference whose steps are up to 32 are off by 2^-20 ln 2,
+    11 u, less than the 2 (d + 4) u of scores that are sums."""
+    B, T, past, H, Hk, d, window, sinks = case
+    x = make(B, T, H, Hk, d, dtype, past, seed=12)
+    x["q"].zero_()[..., 0] = 1.0
+    x["k"].zero_()[..., 0] = key
+    ref = expected(x, window, sinks, 1.0, parts=min(window + sinks, past + T) < 256)
+    far = {**x, "q": x["q"] * 2.0 ** unit, "k": x["k"] * 2.0 ** unit}
+    got = run(kla, far, window, sinks, 1.0)
+    for n in ref:
+        f = 2.0 ** unit if n in ("dq", "dk") else 1.0
+        check(n, got[n], tuple(f * t for t in ref[n]))
