@@ -568,7 +568,8 @@ kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, c
  *
  * Scores, softmax and sums are fp32.  With bf16 inputs P and its gradient enter their products
  * rounded to bf16, in rows that see fewer than 256 tokens (or at a position under 128) in two
- * parts, 16 bits; the step rounds P.  With fp32 inputs everything stays fp32.  A row whose visible scores are all
+ * parts, 16 bits; the step rounds P.  With fp32 inputs everything stays fp32.  Scores have to stay below 2^30 in
+ * units of ln 2; a row whose largest is beyond is right or NaN.  A row whose visible scores are all
  * -inf has y = 0 and no gradient.  What is masked has no influence, finite or not.  The backward
  * takes y and saved of the forward and returns dq, dk, dv (dtype, all required).  scale > 0 and
  * finite, window >= 1, sinks in 0 .. 64, sinks + window <= 2^30, H d <= 2^22, Tk <= 2^28, and

@@ -373,6 +373,13 @@ __device__ __forceinline__ bool any_of(bool x, int* flag) {
     return *flag != 0;
 }
 
+// A row's sum l about the reference m.  The largest score lies within 9 of a reference below 2^24; past that by half of
+// fp32's steps more, 64 between 2^30 and 2^31.  A sum that says more is lost: NaN, where its row would else be zeros or
+// wrong.  (m = -inf: no score, or NaN.)
+__device__ __forceinline__ float sum_of(float l, float m) {
+    return m == -INFINITY || (l > 0x1p-64f && l < 0x1p64f) ? l : __uint_as_float(0x7fc00000u);
+}
+
 // What the backward takes of a row with reference m and sum l: the reference less kAhead, and the sum about that.  m is a
 // whole number, but past 2^27 fp32 has no step of 8: the sum is multiplied by 2 to the distance that came out (0, 8 or
 // 16), exactly.  Rows without a score have zeros.
@@ -660,7 +667,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
             for (int t = 0; t < DT; ++t) o[t] = zero16();
             walk(std::true_type{});
         }
-        l = halves_sum(l);
+        l = sum_of(halves_sum(l), mc);
     }
     if (qi >= a.T) return;
     if (a.nsplit > 1) {
@@ -1287,6 +1294,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 4 && D == 128 ? 2 : 3) void win_s
     // the waves' maxima and sums, and their O about the common maximum
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    l = sum_of(l, mc);
     if (g4 == 0) sst[wave][l16] = float2{mc, l};
     __syncthreads();
     float m = -INFINITY;

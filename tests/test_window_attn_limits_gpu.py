@@ -34,3 +34,31 @@ def test_scores_whose_reference_has_few_digits(kla, case, dtype, unit, key):
     for n in ref:
         f = 2.0 ** unit if n in ("dq", "dk") else 1.0
         check(n, got[n], tuple(f * t for t in ref[n]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_past_the_range_are_not_zeros(kla, dtype):
+    """Past 2^30 in units of scale log2(e) score no fp32 reference may lie near enough to a score for its exponential: a
+    row that sees one token is that token's, gradient too, or NaN; in the prompt, in pieces and in the step."""
+    T, d = 1000, 64
+    x = make(1, T, 1, 1, d, dtype, seed=14)
+    g = torch.Generator().manual_seed(15)
+    x["q"].zero_()[0, :, 0, 0] = torch.exp2(27 + 13 * torch.rand(T, generator=g)).to(TYPES[dtype])
+    x["k"].zero_()[0, :, 0, 0] = torch.tensor([1.0, -1.0]).repeat(T // 2).to(TYPES[dtype])
+    near = (x["q"][0, :, 0, 0].double() * math.log2(math.e) < 2.0 ** 30)
+    assert near.any() and not near.all()
+    zero = {**x, "q": torch.zeros_like(x["q"])}
+    ref = expected(zero, 1, 0, 1.0)
+    ref["step"] = expected(zero, 1, 0, 1.0, parts=False, grads=False)["y"]
+    got = run(kla, x, 1, 0, 1.0)
+    X = dev(x)
+    one = lambda n: X[n][0].contiguous()
+    cache = lambda: torch.zeros(T, 1, 1, d, dtype=TYPES[dtype], device=DEV)
+    got["step"] = kla.kla_window_attn_step(one("q"), one("k"), one("v"), cache(), cache(),
+                                           torch.zeros(T, dtype=torch.int32, device=DEV), scale=1.0)["y"][None]
+    for n in ("y", "dv", "step"):
+        value, tol = ref[n]
+        r = got[n].double().cpu()
+        lost = torch.isnan(r[0, :, 0]).all(-1)
+        assert not lost[near].any()
+        check(n, r[:, ~lost], (value[:, ~lost], tol[:, ~lost]))
