@@ -829,6 +829,7 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
     f32x16 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
+    bool scored = false;   // a row without a score has no gradient
     if (p1 >= p0) {
         const Tiles<TT> tiles(a, p0, p1);
         const Loader<E, D, TT> ld(stride, wave, lane);
@@ -852,7 +853,8 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
             Dq = halves_sum(Dq);
         }
         const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
-        const float li = st.y == 0.f ? 0.f : 1.f / st.y, Dl = Dq * li;
+        scored = st.y != 0.f;
+        const float li = scored ? 1.f / st.y : 0.f, Dl = Dq * li;
         if (h == 0 && qi < a.T64) {
             a.rows[at] = st.x;
             a.rows[nrow + at] = li;
@@ -896,7 +898,7 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
             }
         };
         walk(std::false_type{});
-        if (any_of(live && !finite(o), &sh.flag)) {
+        if (any_of(scored && !finite(o), &sh.flag)) {
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] = zero16();
             walk(std::true_type{});
@@ -905,7 +907,7 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
         a.rows[at] = a.rows[nrow + at] = a.rows[2 * nrow + at] = 0.f;
     }
     if (qi >= a.T) return;
-    if (live)
+    if (scored)
         store_row<E, D>(dq, o, a.scale, h);
     else
         store_zero<E, D>(dq, h);
@@ -1012,6 +1014,8 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             s[4 * j + e] = exp2_hw(fmaf(s[4 * j + e], a.c, -m[e])) * li[e];
+                            // rows without a score, whose q or dy may be infinite, take no part
+                            if constexpr (CAREFUL) s[4 * j + e] = li[e] == 0.f ? __uint_as_float(kMasked) : s[4 * j + e];
                             ds[4 * j + e] -= Dq[e];
                         }
                     }

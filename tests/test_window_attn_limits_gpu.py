@@ -62,3 +62,61 @@ def test_scores_past_the_range_are_not_zeros(kla, dtype):
         lost = torch.isnan(r[0, :, 0]).all(-1)
         assert not lost[near].any()
         check(n, r[:, ~lost], (value[:, ~lost], tol[:, ~lost]))
+
+
+def without_row(x, r):
+    """The inputs of which row r of the queries takes no part in a gradient."""
+    x = {n: t if t is None else t.clone() for n, t in x.items()}
+    x["q"][:, r] = 0.0
+    x["dy"][:, r] = 0.0
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,d,W,sinks", [(1, 64, 20, 2), (1, 128, 20, 2), (6, 128, 40, 0), (90, 32, 20, 2)])
+def test_an_infinite_query_without_a_score_has_no_gradient(kla, B, d, W, sinks, dtype):
+    """All scores of rows 70 and 250 are -inf by the query's infinity: zeros for the row, and nothing of it in dk and dv,
+    also where an upstream gradient of the row is not finite."""
+    T = 300
+    x = make(B, T, 2, 1, d, dtype, seed=16)
+    x["k"][..., 3] = x["k"][..., 3].abs() + 0.5
+    ref = expected(without_row(x, [70, 250]), W, sinks)
+    x["q"][:, [70, 250], :, 3] = -math.inf
+    for bad in (None, math.inf, math.nan):
+        if bad is not None:
+            x["dy"][:, [70, 250], :, 1] = bad
+        got = run(kla, x, W, sinks)
+        rows = torch.ones(T, dtype=torch.bool)
+        rows[[70, 250]] = False
+        for n in ("y", "dq"):
+            assert (got[n][:, [70, 250]] == 0).all(), n
+            check(n, got[n][:, rows.to(DEV)], tuple(t[:, rows] for t in ref[n]))
+        for n in ("dk", "dv"):
+            check(n, got[n], ref[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_infinite_keys_that_leave_a_row_without_a_score(kla, d, dtype):
+    """Row 70 sees keys of -inf alone: zeros, and finite dk and dv for all tokens.  In the reference those keys take no
+    weight because their scores are -38."""
+    T, W, r = 150, 5, 70
+    x = make(1, T, 2, 1, d, dtype, seed=17)
+    x["q"][..., 0] = 1.0
+    bad = slice(r - W + 1, r + 1)
+    y = {n: t if t is None else t.clone() for n, t in x.items()}
+    y["dy"][:, r] = 0.0
+    y["k"][:, bad, :, 0] = -38.0 * math.sqrt(d)
+    ref = expected(y, W, 0)
+    x["k"][:, bad, :, 0] = -math.inf
+    got = run(kla, x, W, 0)
+    assert (got["y"][:, r] == 0).all() and (got["dq"][:, r] == 0).all()
+    other, clear, finite = (torch.ones(T, dtype=torch.bool) for _ in range(3))
+    other[r] = False
+    clear[r - W + 1:r + W] = False    # rows that see none of those keys
+    finite[bad] = False
+    check("y", got["y"][:, other.to(DEV)], tuple(t[:, other] for t in ref["y"]))
+    check("dq", got["dq"][:, clear.to(DEV)], tuple(t[:, clear] for t in ref["dq"]))
+    for n in ("dk", "dv"):
+        check(n, got[n][:, finite.to(DEV)], tuple(t[:, finite] for t in ref[n]))
+        assert (got[n][:, bad] == 0).all(), n
