@@ -55,7 +55,10 @@ constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgro
 // accordingly (context): small weights then end where exp2's range does below the largest, not 2^8 above.
 constexpr float kAhead = 8.f;
 constexpr int kFew = 256;    // visible tokens below which a row sees few
-constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which no weight is otherwise
+constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which seen() keeps apart from others
+
+// A visible place's weight where masked ones are left out: dS is signed, and its zeros are +0.
+__device__ __forceinline__ float seen(float w) { return w == 0.f ? 0.f : w; }
 
 // Rows of D elements in LDS, in 16-byte pieces: piece c of row r lies at c ^ key(r), so that 16 rows read at one
 // piece, 4 rows of bf16 read across at four pieces, and rows of fp32 read across at eight, 4 rows apart, touch
@@ -872,7 +875,10 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
                 f32x16 dp;
                 rows_dot_two<D>(K, V, u0 + 32 * u, q, g, s[u], dp, l32, h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
+                for (int r = 0; r < 16; ++r) {
+                    s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -st.x)) * fmaf(dp[r], li, -Dl);
+                    if constexpr (CAREFUL) s[u][r] = seen(s[u][r]);
+                }
             }
             if (masked) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
 #pragma unroll
@@ -1037,7 +1043,7 @@ __device__ __forceinline__ void win_dkv(const WinArgs& a, Shared<E, D, kDkv>& sh
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         if constexpr (CAREFUL)
-                            ds[r] = __float_as_uint(s[r]) == kMasked ? s[r] : s[r] * ds[r];
+                            ds[r] = __float_as_uint(s[r]) == kMasked ? s[r] : seen(s[r] * ds[r]);
                         else
                             ds[r] *= s[r];
                     }

@@ -120,3 +120,23 @@ def test_infinite_keys_that_leave_a_row_without_a_score(kla, d, dtype):
     for n in ("dk", "dv"):
         check(n, got[n][:, finite.to(DEV)], tuple(t[:, finite] for t in ref[n]))
         assert (got[n][:, bad] == 0).all(), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_a_weight_of_zero_times_a_visible_infinity(kla, d, dtype):
+    """0 times an infinite key that a row sees is NaN, whichever sign the zero of dS has; rows that do not see it stay
+    finite."""
+    T, W, j = 150, 20, 70
+    x = make(1, T, 1, 1, d, dtype, seed=18)
+    x["q"][..., 0] = 1.0
+    x["k"][0, j, 0, 0] = -math.inf
+    for sign in (1.0, -1.0):
+        x["v"][0, j] = sign * x["v"][0, j].abs()
+        x["dy"].copy_(x["dy"].abs())
+        dq = run(kla, x, W, 0)["dq"][0, :, 0]
+        sees = torch.zeros(T, dtype=torch.bool, device=DEV)
+        sees[j + 1:j + W] = True   # row j itself sees other keys too
+        sees[j] = True
+        assert torch.isnan(dq[sees, 0]).all(), sign
+        assert torch.isfinite(dq[~sees]).all() and torch.isfinite(dq[:, 1:]).all()
