@@ -140,3 +140,75 @@ def test_a_weight_of_zero_times_a_visible_infinity(kla, d, dtype):
         sees[j] = True
         assert torch.isnan(dq[sees, 0]).all(), sign
         assert torch.isfinite(dq[~sees]).all() and torch.isfinite(dq[:, 1:]).all()
+
+
+EARLY = [  # B, T, past, H, Hk, d, window, sinks: the last two with keys dealt to two workgroups, joined in either way
+    (2, 300, 0, 2, 1, 64, 300, 2),
+    (3, 200, 70, 2, 1, 32, 256, 0),
+    (2, 150, 127, 1, 1, 128, 260, 0),
+    (2, 300, 100, 2, 2, 16, 270, 4),
+    (2, 600, 0, 2, 1, 64, 600, 0),
+    (2, 600, 40, 2, 1, 128, 600, 3),
+]
+
+
+def early_rows(x, window, sinks):
+    """expected() where positions under 128 count as rows of few tokens and the others do not: y and dq row by row, dk
+    and dv of either rows' dy alone, added up."""
+    T, past = x["q"].shape[1], x["k"].shape[1] - x["q"].shape[1]
+    early = past + torch.arange(T) < 128
+    part = [expected({**x, "dy": x["dy"] * m[None, :, None, None]}, window, sinks, parts=p) for p, m in
+            ((True, early), (False, ~early))]
+    rows = early[None, :, None, None]
+    ref = {n: tuple(torch.where(rows, a, b) for a, b in zip(part[0][n], part[1][n])) for n in ("y", "dq")}
+    ref.update({n: tuple(a + b for a, b in zip(part[0][n], part[1][n])) for n in ("dk", "dv")})
+    return ref, early
+
+
+@pytest.mark.parametrize("case", EARLY, ids=lambda c: "-".join(map(str, c)))
+@pytest.mark.parametrize("alike", [False, True], ids=["normal", "alike"])
+def test_first_positions_under_a_wide_window(kla, case, alike):
+    """Positions under 128 keep P and dS in two parts and y with 8 more bits, whatever the window.  alike: values that are
+    one bf16 step apart, so that y lies between two of them and dq is what the kept bits leave of D; without them dq
+    would miss its tolerance in most rows."""
+    B, T, past, H, Hk, d, window, sinks = case
+    x = make(B, T, H, Hk, d, "bf16", past, seed=19)
+    if alike:
+        g = torch.Generator().manual_seed(20)
+        x["v"] = (1 + 2.0 ** -7 * torch.randint(0, 2, x["v"].shape, generator=g)).bfloat16()
+        x["dy"] *= torch.nn.functional.one_hot(torch.randint(0, d, x["dy"].shape[:3], generator=g), d)   # one term of D
+    ref, early = early_rows(x, window, sinks)
+    if alike:   # what D would be off by with y rounded to bf16 alone, in dq
+        y = ref["y"][0]
+        off = (x["dy"].double() * (y.bfloat16().double() - y)).sum(-1, keepdim=True)
+        plain = expected(x, window, sinks, parts=True)["dq"]
+        mean = expected({**x, "v": x["k"]}, window, sinks, grads=False)["y"][0]
+        miss = (off * mean / math.sqrt(d)).abs() > 2 * plain[1]
+        assert miss[:, early].any(-1).double().mean() > 0.7
+    got = run(kla, x, window, sinks)
+    for n in ref:
+        check(n, got[n], ref[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_of_dealt_keys(kla, dtype):
+    """Parts of many rows, joined by a thread for every four columns, with the context that the backward takes."""
+    x = make(1, 1024, 4, 2, 128, dtype, lengths=[1000], seed=21)
+    ref = expected(x, 1024, 0, parts=False)
+    got = run(kla, x, 1024, 0)
+    for n in ref:
+        check(n, got[n], ref[n])
+        if n in ("y", "dq"):
+            assert (got[n][:, 1000:] == 0).all()
+
+
+@pytest.mark.parametrize("size", [3.0, 6.0, 20.0])
+def test_peaked_rows(kla, size):
+    """Scores of deviation 3 to 20: the largest weight is 0.35 to 0.9, and D is as large as dy . v in rows that see many
+    tokens and keep no further bits."""
+    x = make(1, 600, 2, 1, 128, "bf16", seed=22)
+    x["q"] = (x["q"].float() * size).bfloat16()
+    ref = expected(x, 512, 0, parts=False)
+    got = run(kla, x, 512, 0)
+    for n in ref:
+        check(n, got[n], ref[n])
