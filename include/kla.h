@@ -555,8 +555,7 @@ kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, c
  *   len  [B] int32 or NULL: sequence b has len[b] tokens (taken into 0 .. Tk).  Tokens past them
  *        are not read; y and the gradients of the rows past them are written as zeros.
  *   saved  kla_window_attn_saved_bytes(desc) or NULL: the forward's context for the backward (each
- *        row's largest score and sum of exponentials, and for bf16 rows that see few tokens what the
- *        rounding of y left)
+ *        row's reference of the exponentials and their sum, and for bf16 8 further bits of y)
  *   cache_k, cache_v [B, sinks + window, Hk, d] dtype or both NULL: the cache for the step, as it
  *        is after the last token; slots that hold no token are written as zeros
  *
@@ -567,10 +566,10 @@ kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, c
  * caches stay as they are and y is zero.
  *
  * Scores, softmax and sums are fp32.  With bf16 inputs P and its gradient enter their products
- * rounded to bf16, in rows that see fewer than 256 tokens (or at a position under 128) in two
- * parts, 16 bits; the step rounds P.  With fp32 inputs everything stays fp32.  Scores have to stay below 2^30 in
- * units of ln 2; a row whose largest is beyond is right or NaN.  A row whose visible scores are all
- * -inf has y = 0 and no gradient.  What is masked has no influence, finite or not.  The backward
+ * rounded to bf16, and y is divided by the sum of the rounded weights; positions under 128, and all rows
+ * where min(window + sinks, Tk) < 256, take them in two parts, 16 bits; the step rounds P.  With fp32
+ * inputs everything stays fp32.  |scale q . k| has to stay below 2^30 ln 2; a row whose largest score
+ * is beyond is right or NaN.  A row whose visible scores are all -inf has y = 0 and no gradient.  What is masked has no influence, finite or not.  The backward
  * takes y and saved of the forward and returns dq, dk, dv (dtype, all required).  scale > 0 and
  * finite, window >= 1, sinks in 0 .. 64, sinks + window <= 2^30, H d <= 2^22, Tk <= 2^28, and
  * fewer than 2^23 workgroups: B H (T / 128) and B Hk (Tk / 128 + T / 512).

@@ -29,10 +29,15 @@
 // therefore has rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 of 16, and A is read with the same.  fp32:
 // v_mfma_f32_32x32x2_f32, one contraction index a half.
 //
-// bf16: q, k, v, dy are exact operands; P and dS are rounded to bf16 (as much as the rounding of the outputs, and
-// with signs that average out), while scores, maxima, sums and accumulators stay in fp32.  In rows that see few
-// tokens (fewer than kFew) little averages out, and D, which is common to a row's dS, is as large as dy . v: there P and
-// dS enter in two parts, and y is saved with 8 more bits for D.  fp32 inputs keep fp32 operands throughout.
+// bf16: q, k, v, dy are exact operands; scores, references, sums and accumulators stay in fp32; P and dS are rounded to
+// bf16, which adds as much as the rounding of the outputs.  Where a few tokens take most of a row, D, which is common to a
+// row's dS, is as large as dy . v, and what y is off by is many times dS.  So y is divided by the sum of the weights as
+// rounded, which takes a heavy weight's rounding out again, and saved with 8 more bits for D.  Errors over those of exact
+// outputs rounded once (T1024 d128 window 512, rows from 256 on; scores of deviation 1, 6 and 20, whose largest weights
+// are 0.03, 0.6 and 0.9): y 1.4, 1.05, 1.02; dq and dk 1.4, 1.5, 1.55; dv 1.4, 1.3, 1.2; with the sum of the weights
+// themselves and y as stored dq would be off by 1.4, 3.1 and 5.3.  Calls whose rows all see few tokens (fewer than kFew), and
+// the first kRows positions, take P and dS in two parts: 1.0 (window 200, deviations 1 and 6).  fp32 inputs keep fp32
+// operands throughout.
 //
 // Values that are not finite: scores of masked places are left out by selection, but the products with a zero weight
 // are not, and an infinity or NaN there would reach rows that do not see it.  So a workgroup whose sums are not finite
@@ -54,7 +59,7 @@ constexpr int kRows = 128;   // queries, or tokens in the dk, dv pass, a workgro
 // a wave's 32 rows does in nearly every tile.  The backward takes it lower by as much, with the sum multiplied
 // accordingly (context): small weights then end where exp2's range does below the largest, not 2^8 above.
 constexpr float kAhead = 8.f;
-constexpr int kFew = 256;    // visible tokens below which a row sees few
+constexpr int kFew = 256;    // a call whose rows see fewer tokens than this sees few
 constexpr uint32_t kMasked = 0x80000000u;   // the weight of a masked place: -0, which seen() keeps apart from others
 
 // A visible place's weight where masked ones are left out: dS is signed, and its zeros are +0.
@@ -102,22 +107,18 @@ template <typename E, int D>
 using Acc = f32x16[Rows<E, D>::DP / 32];
 
 // What rounding to bf16 left of four values, in 1/254 of each one's last place: with it D = dy . y has 16 bits of
-// y.  D is common to a row's dS = P (dy . v - D); where a row sees few tokens it is as large as dy . v, and y's
-// rounding alone would be as much as that of dS.
+// y.  D is common to a row's dS = P (dy . v - D), and where a row sees few tokens, or a few of them take most of it, as
+// large as dy . v: y's rounding alone would be as much as that of dS, or many times as much.  Differences of bit
+// patterns, which go on past a power of two; an infinity and a zero leave 0.
 __device__ __forceinline__ uint32_t rest_of(const float (&x)[4], const uint2& y) {
     const uint32_t b[4] = {y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u};
-    uint32_t w = 0;
+    uint32_t t[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float per = __uint_as_float(0x7f000000u - (b[e] & 0x7f800000u));   // 1 / its power of two
-        const float q = fminf(fmaxf((x[e] - __uint_as_float(b[e])) * per * (254.f * 128.f), -127.f), 127.f);
-        w |= ((uint32_t)(int)rintf(q) & 0xffu) << (8 * e);
-    }
-    return w;
+    for (int e = 0; e < 4; ++e) t[e] = (uint32_t)(__mul24((int)(__float_as_uint(x[e]) - b[e]), 254) + 0x8000);   // byte 2
+    return __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0602u) | __builtin_amdgcn_perm(t[3], t[2], 0x06020c0cu);
 }
 __device__ __forceinline__ float rest_add(float y, uint32_t w, int e) {
-    const float unit = __uint_as_float(__float_as_uint(y) & 0x7f800000u);
-    return fmaf((float)(int8_t)(w >> (8 * e)), unit * (1.f / (254.f * 128.f)), y);
+    return __uint_as_float(__float_as_uint(y) + (uint32_t)__mul24((int)(int8_t)(w >> (8 * e)), 258));   // 2^16 / 254
 }
 
 // One row of a lane (A's or B's 32 rows): half h has every second piece.
@@ -276,6 +277,15 @@ struct Weights<float> {
     __device__ explicit Weights(const f32x16& w) : w(w) {}
 };
 
+// s + the sum of a lane's weights as rounded, two at once
+__device__ __forceinline__ float pairs_sum(const bf16x8& w, float s) {
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 pair_t;
+#pragma unroll
+    for (int r = 0; r < 8; r += 2)
+        s = __builtin_amdgcn_fdot2_f32_bf16(pair_t{w[r], w[r + 1]}, pair_t{(__bf16)1.f, (__bf16)1.f}, s, false);
+    return s;
+}
+
 // o[t] += (columns 32 t .. 32 t + 31 of rows row0 .. row0 + 31)^T w
 template <int D>
 __device__ __forceinline__ void cols_dot(Acc<uint16_t, D>& o, const unsigned char* x, int row0, const Weights<uint16_t>& w, int l32,
@@ -342,15 +352,18 @@ __device__ __forceinline__ f32x16 left_of(const f32x16& w, const Weights<uint16_
     return x;
 }
 
-// o += (rows row0 .. row0 + 31)^T w.  TWO: bf16 weights enter in two parts.
+// o += (rows row0 .. row0 + 31)^T w.  TWO: bf16 weights enter in two parts.  sum: takes the weights as rounded, where
+// they enter in one.
 template <bool CAREFUL, bool TWO, typename E, int D>
 __device__ __forceinline__ void add_cols(Acc<E, D>& o, const unsigned char* x, int row0, const f32x16& w, float* scratch, int l32,
-                                         int h) {
+                                         int h, float* sum = nullptr) {
     if constexpr (CAREFUL) {
 #pragma unroll
         for (int t = 0; t < Rows<E, D>::DP / 32; ++t) cols_apart<E, D>(o[t], x, row0, t, w, scratch, l32, h);
     } else {
         const Weights<E> b(w);
+        if constexpr (sizeof(E) == 2 && !TWO)
+            if (sum) *sum = pairs_sum(b.b[0], 0.f) + pairs_sum(b.b[1], *sum);
         cols_dot<D>(o, x, row0, b, l32, h);
         if constexpr (sizeof(E) == 2 && TWO) cols_dot<D>(o, x, row0, Weights<E>(left_of(w, b)), l32, h);
     }
@@ -415,14 +428,15 @@ struct WinArgs {
     void *o, *dq, *dk, *dv;   // o: y of the forward
     const int* len;
     float2* stat;             // [B, T, H]: the exponents' reference less kAhead and the sum of exponentials about it
-    int8_t* rest;             // [B, R, H, D]: what the rounding of y to bf16 left (rest_of)
+    int8_t* rest;             // bf16: [B, T, H, D], what the rounding of y left (rest_of)
     float* part;              // forward: partial O [nsplit][B T H][D]; dk, dv: the first tokens' sums
     float2* pstat;            // forward: [nsplit][B T H]
     float* rows;              // backward: [3][B H][T64] m, 1 / l, D
     float* kpart;             // dk, dv: [B Hk][ksplit][2][Tk][D], where a workgroup's queries are dealt to several
-    int B, T, Tk, H, Hk, W, sinks, blocks, nsplit, nseg, seg, ksplit, T64, R;
+    int B, T, Tk, H, Hk, W, sinks, blocks, nsplit, nseg, seg, ksplit, T64;
     float scale, c;           // c = scale log2(e)
     bool few;                 // rows see few tokens
+    bool sums;                // forward: the weights' own sums too, for the backward's P and for joining parts
 };
 
 // Workgroups go around the chip's 8 dies: a run of neighbours, which read the same keys, on one of them.
@@ -497,17 +511,33 @@ __device__ __forceinline__ void store4(float* p, const float (&x)[4], int8_t*) {
     *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
 }
 
-// A lane's column of a C over columns 32 t + 8 (r / 4) + 4 h + r % 4 of row p, 16 or 8 bytes at a time.
+// A lane's column of a C over columns 32 t + 8 (r / 4) + 4 h + r % 4 of row p, 16 bytes at a time.
 template <typename E, int D>
 __device__ __forceinline__ void store_row(E* p, const Acc<E, D>& o, float f, int h, int8_t* rest = nullptr) {
 #pragma unroll
     for (int t = 0; t < Rows<E, D>::DP / 32; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = 32 * t + 8 * j;
-            if (col >= D) continue;
-            const float x[4] = {o[t][4 * j] * f, o[t][4 * j + 1] * f, o[t][4 * j + 2] * f, o[t][4 * j + 3] * f};
-            store4(p + col + 4 * h, x, rest ? rest + col + 4 * h : nullptr);
+        for (int j = 0; j < 4; j += 2) {
+            if (32 * t + 8 * j >= D) continue;
+            float x[2][4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i / 4][i % 4] = o[t][4 * j + i] * f;
+            if constexpr (sizeof(E) == 4) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    *reinterpret_cast<float4*>(p + 32 * t + 8 * (j + i) + 4 * h) = float4{x[i][0], x[i][1], x[i][2], x[i][3]};
+            } else {   // the lower half takes both halves' columns of j, the upper one those of j + 1
+                const uint2 y[2] = {{cvt_pk_bf16(x[0][0], x[0][1]), cvt_pk_bf16(x[0][2], x[0][3])},
+                                    {cvt_pk_bf16(x[1][0], x[1][1]), cvt_pk_bf16(x[1][2], x[1][3])}};
+                const auto a = __builtin_amdgcn_permlane32_swap(y[0].x, y[1].x, false, false);
+                const auto b = __builtin_amdgcn_permlane32_swap(y[0].y, y[1].y, false, false);
+                const int col = 32 * t + 8 * (j + h);
+                *reinterpret_cast<uint4*>(p + col) = uint4{a[0], b[0], a[1], b[1]};
+                if (rest) {
+                    const auto r = __builtin_amdgcn_permlane32_swap(rest_of(x[0], y[0]), rest_of(x[1], y[1]), false, false);
+                    *reinterpret_cast<uint2*>(rest + col) = uint2{r[0], r[1]};
+                }
+            }
         }
 }
 template <typename E, int D>
@@ -576,6 +606,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
     using R = Rows<E, D>;
     using G = Geo<E, D, kFwd>;
     constexpr int DT = R::DP / 32, TT = G::TT, NB = G::NB, BYTES = R::bytes(TT);
+    constexpr bool ROUNDED = sizeof(E) == 2 && !TWO;   // y is divided by the sum of the weights as they entered
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32, h = lane / 32;
     const int kh = head / (a.H / a.Hk), past = a.Tk - a.T, end = end_of(a, b);
     const int q0 = qb * kRows, p0 = past + q0, p1 = min(past + min(q0 + kRows, a.T), end) - 1;
@@ -589,7 +620,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
     f32x16 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = zero16();
-    float mc = -INFINITY, l = 0.f;   // the exponents' reference, and the lane's share of the sum
+    float mc = -INFINITY, l = 0.f, lr = 0.f;   // the exponents' reference, the lane's shares of the sum and of that as rounded
     if (p1 >= p0) {
         const Tiles<TT> tiles(a, p0, p1);
         const int per = (tiles.n + a.nsplit - 1) / a.nsplit, i0 = split * per, i1 = min(i0 + per, tiles.n);
@@ -625,6 +656,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
                 const float now = top > mc ? ceilf(top) + kAhead : mc, f = now == -INFINITY ? 0.f : exp2_hw(mc - now);
                 mc = now;
                 l *= f;
+                lr *= f;
 #pragma unroll
                 for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -637,12 +669,21 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     s[u][r] = exp2_hw(fmaf(s[u][r], a.c, -base));
-                    sum[r % 4] += s[u][r];
+                    if (CAREFUL || !ROUNDED) sum[r % 4] += s[u][r];
                 }
+            if constexpr (!CAREFUL && ROUNDED) {
+                if (a.sums) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sum[r % 4] += s[u][r];
+                }
+            }
             if constexpr (CAREFUL) hide<U>(a, s, j0, pos, h, __uint_as_float(kMasked));
             l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, V, u0 + 32 * u, s[u], sh.scratch[wave], l32, h);
+            for (int u = 0; u < U; ++u) add_cols<CAREFUL, TWO, E, D>(o, V, u0 + 32 * u, s[u], sh.scratch[wave], l32, h, &lr);
+            if constexpr (CAREFUL || !ROUNDED) lr = l;
         };
         auto walk = [&](auto careful) {
             constexpr bool CAREFUL = decltype(careful)::value;
@@ -665,24 +706,26 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
         };
         walk(std::false_type{});
         if (any_of(live && !finite(o), &sh.flag)) {
-            mc = -INFINITY, l = 0.f;
+            mc = -INFINITY, l = lr = 0.f;
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] = zero16();
             walk(std::true_type{});
         }
         l = sum_of(halves_sum(l), mc);
+        lr = ROUNDED ? sum_of(halves_sum(lr), mc) : l;
+        if (ROUNDED && !a.sums) l = lr;
     }
     if (qi >= a.T) return;
     if (a.nsplit > 1) {
         const size_t at = (size_t)split * a.B * a.T * a.H + row;
         if (!live) l = 0.f, mc = -INFINITY;
-        if (live) store_row<float, D>(a.part + at * D, o, 1.f, h);
+        if (live) store_row<float, D>(a.part + at * D, o, ROUNDED ? l / lr : 1.f, h);
         if (h == 0) a.pstat[at] = float2{mc, l};
         return;
     }
     E* y = (E*)a.o + row * D;
     if (live && l != 0.f)
-        store_row<E, D>(y, o, 1.f / l, h, qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr);
+        store_row<E, D>(y, o, 1.f / lr, h, a.rest ? a.rest + row * D : nullptr);
     else
         store_zero<E, D>(y, h);
     if (a.stat && h == 0) a.stat[row] = context(mc, live ? l : 0.f);
@@ -719,8 +762,7 @@ __global__ __launch_bounds__(256, (Geo<E, D, kFwd>::WAVES)) void win_fwd_kernel(
 template <typename E, int D>
 __global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsplit, const float* __restrict__ part,
                                                             const float2* __restrict__ pstat, E* __restrict__ y,
-                                                            float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
-                                                            int R) {
+                                                            float2* __restrict__ stat, int8_t* __restrict__ rest) {
     const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, row = x / (D / 4);
     const int col = (int)(x % (D / 4)) * 4;
     if (row >= rows) return;
@@ -741,8 +783,7 @@ __global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsp
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
     const float x4[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
-    const int qi = R > 0 ? (int)(row / H % T) : 0;
-    store4(y + row * D + col, x4, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + col : nullptr);
+    store4(y + row * D + col, x4, rest ? rest + row * D + col : nullptr);
     if (stat && col == 0) stat[row] = context(m, l);
 }
 
@@ -752,8 +793,7 @@ __global__ __launch_bounds__(256) void win_join_rows_kernel(size_t rows, int nsp
 template <typename E, int D>
 __global__ __launch_bounds__(2 * D) void win_join_kernel(size_t rows, int nsplit, const float* __restrict__ part,
                                                          const float2* __restrict__ pstat, E* __restrict__ y,
-                                                         float2* __restrict__ stat, int8_t* __restrict__ rest, int T, int H,
-                                                         int R) {
+                                                         float2* __restrict__ stat, int8_t* __restrict__ rest) {
     constexpr int G = D / 4;   // column groups
     __shared__ float f[64];
     __shared__ f32x4 sum[8][G];
@@ -790,8 +830,7 @@ __global__ __launch_bounds__(2 * D) void win_join_kernel(size_t rows, int nsplit
     for (int s = 1; s < 8; ++s) o += sum[s][c];
     const float m = ml.x, l = ml.y, r = l == 0.f ? 0.f : 1.f / l;
     const float x[4] = {o[0] * r, o[1] * r, o[2] * r, o[3] * r};
-    const int qi = R > 0 ? (int)(row / H % T) : 0;
-    store4(y + row * D + 4 * c, x, qi < R ? rest + ((row / H / T * R + qi) * H + row % H) * D + 4 * c : nullptr);
+    store4(y + row * D + 4 * c, x, rest ? rest + row * D + 4 * c : nullptr);
     if (stat && c == 0) stat[row] = context(m, l);
 }
 
@@ -848,15 +887,15 @@ __device__ __forceinline__ void win_dq(const WinArgs& a, Shared<E, D, kDq>& sh, 
         Row<E, D> q, g;
         q.load((const E*)a.q + row * D, live, h);
         g.load((const E*)a.dy + row * D, live, h);
+        const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
+        scored = st.y != 0.f;
         float Dq;
         {
             Row<E, D> y;
             y.load((const E*)a.y + row * D, live, h);
-            Dq = g.dot(y, live && qi < a.R ? a.rest + (((size_t)b * a.R + qi) * a.H + head) * D : nullptr, h);
+            Dq = g.dot(y, scored ? a.rest + row * D : nullptr, h);   // other rows' y are zeros, with no rest
             Dq = halves_sum(Dq);
         }
-        const float2 st = live ? a.stat[row] : float2{0.f, 0.f};
-        scored = st.y != 0.f;
         const float li = scored ? 1.f / st.y : 0.f, Dl = Dq * li;
         if (h == 0 && qi < a.T64) {
             a.rows[at] = st.x;
@@ -1137,7 +1176,8 @@ struct StepArgs {
 
 // Workgroup (s, kh, 16 query heads, split): its waves take chunks of 32 (fp32: 16) slots in turn and join at the
 // end.  K goes from memory straight into operands, V through LDS of the wave's own, to be read across.
-// S^T = K Q^T (slots x heads) in 16 x 16 tiles, O^T += V^T P^T.  HBM bounds it: the next chunk's keys and values are
+// S^T = K Q^T (slots x heads) in 16 x 16 tiles, O^T += V^T P^T.  bf16 rounds P, and the sum takes what it rounds to;
+// in two parts registers were stored and loaded again (512 sequences 223 us, 191 this way).  HBM bounds it: the next chunk's keys and values are
 // asked for as soon as the registers of this one's are free, and three waves a SIMD (168 registers) keep enough on
 // their way.  With two chunks in registers instead they were stored and loaded again: 318 us for 512 sequences over
 // 1028 slots of 4 heads of 128, 191 this way.
@@ -1274,13 +1314,14 @@ __global__ __launch_bounds__(256, sizeof(E) == 4 && D == 128 ? 2 : 3) void win_s
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 sc[t][r] = exp2_hw(fmaf(sc[t][r], a.c, -base));
-                l += sc[t][r];
+                if constexpr (sizeof(E) == 4) l += sc[t][r];
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if constexpr (sizeof(E) == 2) {
             const bf16x8 w = __builtin_bit_cast(bf16x8, uint4{cvt_pk_bf16(sc[0][0], sc[0][1]), cvt_pk_bf16(sc[0][2], sc[0][3]),
                                                               cvt_pk_bf16(sc[1][0], sc[1][1]), cvt_pk_bf16(sc[1][2], sc[1][3])});
+            l = pairs_sum(w, l);
 #pragma unroll
             for (int t = 0; t < C::DT; ++t) {
                 const int r = 4 * g4 + (l16 >> 2), col = 16 * t + 4 * (l16 & 3);
@@ -1355,12 +1396,6 @@ bool sees_few(const WinShape& s) {
     return ((int64_t)s.window + s.sinks < s.Tk ? (int64_t)s.window + s.sinks : s.Tk) < kFew;
 }
 
-// Rows of a sequence, from the first on, whose y is saved with 8 more bits (bf16).
-int rest_rows(const WinShape& s) {
-    const int first = s.Tk - s.T < kRows ? kRows - (s.Tk - s.T) : 0;
-    return !s.bf16 ? 0 : sees_few(s) || first > s.T ? s.T : first;
-}
-
 WinArgs args_of(const WinShape& s, const void* q, const void* k, const void* v, const int* len) {
     WinArgs a{};
     a.q = q, a.k = k, a.v = v, a.len = len;
@@ -1375,19 +1410,17 @@ WinArgs args_of(const WinShape& s, const void* q, const void* k, const void* v, 
 // The saved context: stat, then the rest of y.
 void with_saved(const WinShape& s, WinArgs& a, void* saved) {
     a.stat = static_cast<float2*>(saved);
-    a.rest = static_cast<int8_t*>(saved) + align256((size_t)s.B * s.T * s.H * sizeof(float2));
-    a.R = rest_rows(s);
+    if (s.bf16) a.rest = static_cast<int8_t*>(saved) + align256((size_t)s.B * s.T * s.H * sizeof(float2));
 }
 
 template <typename E, int D>
-void join(size_t rows, int nsplit, const float* part, const float2* pstat, void* y, float2* stat, int8_t* rest, int T, int H, int R,
-          hipStream_t st) {
+void join(size_t rows, int nsplit, const float* part, const float2* pstat, void* y, float2* stat, int8_t* rest, hipStream_t st) {
     if (rows * (D / 4) >= 256 * 256)   // a thread for every four columns fills the chip
         hipLaunchKernelGGL((win_join_rows_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
-                           nsplit, part, pstat, (E*)y, stat, rest, T, H, R);
+                           nsplit, part, pstat, (E*)y, stat, rest);
     else
         hipLaunchKernelGGL((win_join_kernel<E, D>), dim3((unsigned)rows), dim3(2 * D), 0, st, rows, nsplit, part, pstat, (E*)y,
-                           stat, rest, T, H, R);
+                           stat, rest);
 }
 
 unsigned grid_of(int64_t blocks) { return (unsigned)((blocks + 7) / 8 * 8); }
@@ -1436,7 +1469,7 @@ hipError_t fwd(const WinShape& s, WinArgs a, void* ck, void* cv, hipStream_t st)
         hipLaunchKernelGGL((win_fwd_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
         if (a.nsplit > 1) {
             const size_t rows = (size_t)a.B * a.T * a.H;
-            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.o, a.stat, a.rest, a.T, a.H, a.R, st);
+            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.o, a.stat, a.rest, st);
         }
     }
     if (ck) {
@@ -1498,7 +1531,8 @@ int64_t window_blocks(const WinShape& s) {
 }
 
 size_t window_saved(const WinShape& s) {
-    return align256((size_t)s.B * s.T * s.H * sizeof(float2)) + (size_t)s.B * rest_rows(s) * s.H * s.d;
+    const size_t rows = (size_t)s.B * s.T * s.H;
+    return align256(rows * sizeof(float2)) + (s.bf16 ? rows * s.d : 0);
 }
 
 size_t window_workspace(const WinShape& s, bool backward) {
@@ -1524,6 +1558,7 @@ hipError_t launch_window_fwd(const WinShape& s, const void* q, const void* k, co
         a.part = static_cast<float*>(ws);
         a.pstat = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(a.nsplit * rows * s.d * sizeof(float)));
     }
+    a.sums = saved || a.nsplit > 1;
     a.blocks = s.B * s.H * ((s.T + kRows - 1) / kRows) * a.nsplit;
     return by_type(s.bf16, s.d, [&](auto e, auto d) { return fwd<decltype(e), decltype(d)::value>(s, a, ck, cv, st); });
 }
@@ -1563,7 +1598,7 @@ hipError_t launch_window_step(const StepShape& s, const void* q, const void* k, 
         constexpr int D = decltype(dd)::value;
         hipLaunchKernelGGL((win_step_kernel<E, D>), dim3(grid_of(a.blocks)), dim3(256), 0, st, a);
         if (a.nsplit > 1)
-            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.y, nullptr, nullptr, 1, a.H, 0, st);
+            join<E, D>(rows, a.nsplit, a.part, a.pstat, a.y, nullptr, nullptr, st);
         return hipGetLastError();
     });
 }

@@ -212,3 +212,70 @@ def test_peaked_rows(kla, size):
     got = run(kla, x, 512, 0)
     for n in ref:
         check(n, got[n], ref[n])
+
+
+def sharp(B, T, H, Hk, d, past=0, seed=0):
+    """bf16 inputs whose scores are exact whole numbers, products of one element each, in peaked rows: the largest of a
+    row takes most of it.  One term of dy a row."""
+    x = make(B, T, H, Hk, d, "bf16", past, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    one = lambda t: torch.nn.functional.one_hot(torch.randint(0, d, t.shape[:3], generator=g), d)
+    x["k"] = (2 * x["k"].float()).round().bfloat16()
+    x["q"] = (one(x["q"]) * torch.randint(1, 4, (*x["q"].shape[:3], 1), generator=g)).bfloat16()
+    x["dy"] *= one(x["dy"])
+    return x
+
+
+def normed(x, window, sinks, grads=True):
+    """expected() of one-part weights where y is divided by the sum of the weights as they entered, and keeps 8 more
+    bits: y is off by 2^-8 of P |v - y|, D by what y is and 2^-16."""
+    q, k, v, dy = (x[n].double() for n in ("q", "k", "v", "dy"))
+    B, T, H, d = q.shape
+    Tk, Hk = k.shape[1:3]
+    p, j = Tk - T + torch.arange(T)[:, None], torch.arange(Tk)[None]
+    see = (j <= p) & ((j > p - window) | (j < sinks))
+    heads = lambda t: t.permute(0, 2, 1, 3)
+    qv, dyv = heads(q), heads(dy)
+    kk, vv = (heads(t).repeat_interleave(H // Hk, 1) for t in (k, v))
+    s = (qv @ kk.transpose(-1, -2)).masked_fill(~see, -math.inf)
+    M = (qv.abs() @ kk.abs().transpose(-1, -2)).masked_fill(~see, 0.0).amax(-1, keepdim=True)
+    P = torch.softmax(s, -1)
+    eP = (2 * (d + 4) * M + 2 * Tk + 8) * U
+    y = P @ vv
+    # one column of v after another: sum_j P_j |v_j - y|
+    apart = torch.stack([(P * (vv[..., None, :, c] - y[..., c, None]).abs()).sum(-1) for c in range(d)], -1)
+    ty = (P * eP) @ vv.abs() + 2.0 ** -8 * apart
+    out = {"y": (heads(y), heads(ty + 2.0 ** -8 * y.abs()))}
+    if not grads:
+        return out
+    A = dyv.abs() @ vv.abs().transpose(-1, -2)
+    D = (dyv * y).sum(-1, keepdim=True)
+    eD = (dyv.abs() * (ty + 2.0 ** -16 * y.abs())).sum(-1, keepdim=True) + (d + 1) * U * (dyv * y).abs().sum(-1, keepdim=True)
+    dS = P * (dyv @ vv.transpose(-1, -2) - D)
+    tS = dS.abs() * (eP + 2.0 ** -8 + 4 * U) + P * ((d + 1) * U * A + eD)
+    dq, tq = dS @ kk, (tS + Tk * U * dS.abs()) @ kk.abs()
+    share = lambda t: heads(t.reshape(B, Hk, H // Hk, Tk, d).sum(2))
+    n = H // Hk * T * U
+    dk, tk = share(dS.transpose(-1, -2) @ qv), share((tS + n * dS.abs()).transpose(-1, -2) @ qv.abs())
+    out.update(dq=(heads(dq), heads(tq + 2.0 ** -8 * dq.abs())), dk=(dk, tk + 2.0 ** -8 * dk.abs()))
+    return out
+
+
+@pytest.mark.parametrize("B,T,past,H,Hk,d,window,sinks", [(2, 500, 0, 2, 1, 64, 300, 2), (1, 400, 130, 2, 2, 128, 256, 0),
+                                                          (2, 300, 200, 1, 1, 32, 270, 4), (1, 600, 40, 2, 1, 128, 640, 0)])
+def test_gradients_of_peaked_rows_that_see_many_tokens(kla, B, T, past, H, Hk, d, window, sinks):
+    """A heavy weight's rounding leaves y where its sum takes it too, and D keeps 16 bits of y: else D, as large as
+    dy . v, is off by 2^-8 of it, many times the row's dS."""
+    x = sharp(B, T, H, Hk, d, past, seed=23)
+    ref, got = normed(x, window, sinks), run(kla, x, window, sinks, 1.0)
+    for n in ref:
+        check(n, got[n], ref[n])
+
+
+@pytest.mark.parametrize("S,window,H,Hk,d", [(3, 700, 4, 2, 64), (2, 2000, 2, 2, 128), (200, 60, 16, 4, 32)])
+def test_step_of_peaked_rows(kla, S, window, H, Hk, d):
+    x = sharp(S, 1, H, Hk, d, window - 1, seed=24)
+    X = dev(x)
+    got = kla.kla_window_attn_step(X["q"][:, 0], X["k"][:, -1].contiguous(), X["v"][:, -1].contiguous(), X["k"].clone(),
+                                   X["v"].clone(), torch.full((S,), window - 1, dtype=torch.int32, device=DEV), scale=1.0)
+    check("y", got["y"][:, None], normed(x, window, 0, grads=False)["y"])
