@@ -572,7 +572,7 @@ kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, c
  * is beyond is right or NaN.  A row whose visible scores are all -inf has y = 0 and no gradient.  What is masked has no influence, finite or not.  The backward
  * takes y and saved of the forward and returns dq, dk, dv (dtype, all required).  scale > 0 and
  * finite, window >= 1, sinks in 0 .. 64, sinks + window <= 2^30, H d <= 2^22, Tk <= 2^28, and
- * fewer than 2^23 workgroups: B H (T / 128) and B Hk (Tk / 128 + T / 512).
+ * fewer than 2^23 workgroups: B H (T / 128) and B Hk (Tk / 128 + T / 256), each fraction rounded up.
  */
 typedef struct kla_window_desc {
     int32_t B, T, Tk;
