@@ -1415,7 +1415,9 @@ void with_saved(const WinShape& s, WinArgs& a, void* saved) {
 
 template <typename E, int D>
 void join(size_t rows, int nsplit, const float* part, const float2* pstat, void* y, float2* stat, int8_t* rest, hipStream_t st) {
-    if (rows * (D / 4) >= 256 * 256)   // a thread for every four columns fills the chip
+    // a thread for every four columns fills the chip (a prompt in four parts, d32, us by threads and by a workgroup a row:
+    // 16384 threads 18.6 and 18.8, 65536 22.2 and 23.5, 131072 29.5 and 33.5; one row of 32 parts 12.9 and 3.4, the join alone)
+    if (rows * (D / 4) >= 256 * 256)
         hipLaunchKernelGGL((win_join_rows_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, rows,
                            nsplit, part, pstat, (E*)y, stat, rest);
     else
@@ -1425,13 +1427,17 @@ void join(size_t rows, int nsplit, const float* part, const float2* pstat, void*
 
 unsigned grid_of(int64_t blocks) { return (unsigned)((blocks + 7) / 8 * 8); }
 
-// Keys are dealt to several workgroups where the queries are too few for two workgroups a CU, at least 256 to each
-// (the join is a launch more, 4 us).
+// Keys are dealt to several workgroups where those of the queries are fewer than CUs, at least 256 keys to each.  bf16: only
+// where a row's keys are many tiles, and the more the more queries, since the join reads each row's parts (us, all keys
+// visible, d64, one workgroup a row and dealt out: B4 T512 H8 11 and 15, after 1500 tokens 31 and 27; B2 T512 H8 11 and
+// 13, after 512 tokens 17.6 and 16.2; B1 T1024 H4 17.7 and 12.6; B8 T512 H8, 256 workgroups, 12 and 22, after 3500 tokens
+// 58 and 54).  An fp32 tile takes some times as long (B4 T512 H8 44 and 32; B8 T512 H8 45 and 49).
 int splits(const WinShape& s) {
     const int64_t blocks = (int64_t)s.B * s.H * ((s.T + kRows - 1) / kRows);
     const int64_t reach = (int64_t)s.window + kRows < s.Tk ? (int64_t)s.window + kRows : s.Tk;
     const int64_t tiles = (reach + 63) / 64 + (s.sinks > 0);
-    int64_t n = blocks > 0 ? 512 / blocks : 1;
+    if (blocks == 0 || blocks >= 256 || (s.bf16 && (tiles < 16 || 4 * tiles < blocks))) return 1;
+    int64_t n = 512 / blocks;
     if (n > tiles / 4) n = tiles / 4;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
@@ -1513,10 +1519,15 @@ hipError_t by_type(bool bf16, int d, F&& f) {
 int step_groups(const StepShape& s) { return (s.H / s.Hk + 15) / 16; }
 
 // Slots are dealt to several workgroups where sequences and heads are too few for four workgroups a CU, at least a
-// chunk to a wave.
+// chunk to a wave; not where 16 chunks do not pay the join's launch, nor at 192 to 256 workgroups, a CU's each, nor at more
+// of fewer than 128 chunks (us, one workgroup and by the rule above: bf16 d128, one sequence over 256 slots 6.6 and 8.2,
+// 1024 slots 14.4 and 8.3, 4096 44 and 9.5; 128 workgroups over 1024 slots 17 and 18, 4096 54 and 47; 256 over 1024 slots
+// 23 and 27, 4096 100 and 103; 512 over 1024 slots 44 and 47; 384 over 4096 165 and 153; fp32 d64, seven sequences of 3
+// heads over 128 slots 5.4 and 7.4, 256 slots 7.4 and 7.4, 512 slots 11.6 and 7.5).
 int step_splits(const StepShape& s) {
     const int64_t blocks = (int64_t)s.S * s.Hk * step_groups(s);
     const int64_t chunks = ((int64_t)s.window + s.sinks + (s.bf16 ? 31 : 15)) / (s.bf16 ? 32 : 16);
+    if (chunks < 16 || (blocks >= 192 && (blocks <= 256 || chunks < 128))) return 1;
     int64_t n = 1024 / blocks;
     if (n > chunks / 4) n = chunks / 4;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);

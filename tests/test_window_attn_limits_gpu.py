@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 FAR = [  # B, T, past, H, Hk, d, window, sinks: one workgroup a row, and keys dealt to several, joined in either way
     (2, 40, 0, 2, 1, 64, 9, 2),
     (1, 3, 1400, 2, 1, 64, 1500, 0),
-    (1, 600, 0, 4, 2, 128, 600, 0),
+    (1, 1024, 0, 4, 2, 128, 1024, 0),
 ]
 
 
@@ -142,13 +142,13 @@ def test_a_weight_of_zero_times_a_visible_infinity(kla, d, dtype):
         assert torch.isfinite(dq[~sees]).all() and torch.isfinite(dq[:, 1:]).all()
 
 
-EARLY = [  # B, T, past, H, Hk, d, window, sinks: the last two with keys dealt to two workgroups, joined in either way
+EARLY = [  # B, T, past, H, Hk, d, window, sinks: the last two with keys dealt to several workgroups, joined in either way
     (2, 300, 0, 2, 1, 64, 300, 2),
     (3, 200, 70, 2, 1, 32, 256, 0),
     (2, 150, 127, 1, 1, 128, 260, 0),
     (2, 300, 100, 2, 2, 16, 270, 4),
-    (2, 600, 0, 2, 1, 64, 600, 0),
-    (2, 600, 40, 2, 1, 128, 600, 3),
+    (2, 1024, 0, 1, 1, 64, 1024, 0),
+    (2, 1000, 40, 2, 1, 128, 1040, 3),
 ]
 
 
