@@ -17,12 +17,14 @@
 // the queries behind the window of the first 128 tokens are cut into segments, whose sums over those tokens are
 // joined.
 //
-// What bounds it.  Long windows: matrix work; a prompt of B1 T65536 H16 Hk4 d128 window 2048 takes 1.10 ms, 980
-// TFLOP/s of its 1085 GFLOP (a large product reaches 1240), at a clock that the card's power holds to 1.8 GHz.
-// B8 T2048 H16 d128 window 512: 107 us forward (two products of a tile), 153 dq (three), 211 dk and dv (four), the
-// matrix cores busy for a quarter of the time at 2.4 GHz: a wave's chain of products, exponentials and reads of
-// LDS, of which two or three waves a SIMD hide a part; its registers allow no more.  fp32: 153 TFLOP/s of its
-// matrix instructions.  The step: HBM, 5.6 TB/s (S512 Hk4 d128 over 1028 slots, 191 us).
+// What bounds it.  Long windows: matrix work; a prompt of B1 T65536 H16 Hk4 d128 window 2048 takes 1.10 ms, 985
+// TFLOP/s of its 1085 GFLOP (a large product reaches 1240), at a clock that the card's power holds to 1.9 GHz, the matrix
+// cores busy for half of the time; a wave's 32 rows read every product's other operand from LDS.  B8 T2048 H16 d128
+// window 512: 119 us forward (two products of a tile), 161 dq (three), 202 dk and dv (four), the matrix cores busy for a
+// quarter of the time at 2.4 GHz: reckoned from the prompt's time a tile, the forward's workgroups, of 22 tiles, spend more than
+// a third of their time outside the loop over them, on the first reads, the vote on sums that are not finite and the
+// stores, those of a round all at once.  fp32: its matrix instructions, 153 TFLOP/s, busy for 0.3 to 0.5 of the time and
+// CUs for 0.7 where workgroups are few.  The step: HBM, 5.6 TB/s (S512 Hk4 d128 over 1028 slots, 190 us).
 //
 // v_mfma_f32_32x32x16_bf16 (lane l, half h = l / 32): A row l % 32 and B column l % 32, contraction 8 h .. 8 h + 7;
 // C column l % 32, register r at row 8 (r / 4) + 4 h + r % 4.  Over the contraction of a C used as B, half h
@@ -548,9 +550,9 @@ __device__ __forceinline__ void store_zero(E* p, int h) {
 
 // How a pass (forward, dq, or dk and dv) goes over its tiles: TT tokens (queries for dk, dv) a tile, NB tiles in LDS
 // (one worked on, the others on their way), U halves of 32 at once, WAVES a SIMD.  At 128 bf16 columns tiles of 32
-// leave the forward registers for three waves a SIMD (B8 T2048 H16 window 512: 107 us, with tiles of 64 and two
-// waves 121; three tiles in LDS instead of two gain nothing there).  fp32: as many waves as registers allow (B64 T512
-// H4 d32: forward 40 us, 50 with one a SIMD).
+// leave the forward registers for three waves a SIMD (B8 T2048 H16 window 512: with tiles of 64 and two waves 13% more;
+// three tiles in LDS instead of two gain nothing there); of its 168 the walk without masked places stores five.  fp32: as
+// many waves as registers allow (B64 T512 H4 d32: forward 40 us, 50 with one a SIMD).
 enum Pass { kFwd, kDq, kDkv };
 template <typename E, int D, Pass P>
 struct Geo {
@@ -580,8 +582,6 @@ template <int NB, int L>
 __device__ __forceinline__ void wait_tile(int i, int n) {
     if (i + NB - 2 < n)
         wait_vm_le<(NB - 2) * L>();
-    else if (NB > 3 && i + 1 < n)
-        wait_vm_le<L>();
     else
         wait_vm_all();
     barrier_lds();
@@ -733,7 +733,7 @@ __device__ __forceinline__ void win_fwd(const WinArgs& a, Shared<E, D, kFwd>& sh
 
 // Workgroup id's block of queries, head and sequence.  Heads that share keys go side by side, then blocks in order, where
 // the window makes most alike, since they read on in the tiles that the last ones left in L2 (B1 T65536 H16 Hk4 window
-// 2048: 1.06 ms; head after head 1.12, the blocks backwards 1.17), or the longest first where they are not alike (B2
+// 2048: head after head takes 6% more, the blocks backwards 10%), or the longest first where they are not alike (B2
 // T4096 window 4096: 179 us, in order 191).
 __device__ __forceinline__ void place_of(const WinArgs& a, int id, int& qb, int& head, int& b) {
     const int nq = (a.T + kRows - 1) / kRows, G = a.H / a.Hk, at = id / G % nq, rest = id / G / nq;
@@ -1183,7 +1183,7 @@ struct StepArgs {
 // 1028 slots of 4 heads of 128, 191 this way.
 template <typename E, int D>
 struct StepCfg {
-    static constexpr int CH = sizeof(E) == 2 ? 32 : 16, DP = D < 16 ? 16 : D, DT = D / 16;
+    static constexpr int CH = sizeof(E) == 2 ? 32 : 16, DT = D / 16;
     static constexpr int NC = D * (int)sizeof(E) / 16;                       // pieces a row
     static constexpr int NK = sizeof(E) == 2 ? (D + 31) / 32 : D / 16;       // pieces of a lane's row of K
     static constexpr int NL = (CH * NC + 63) / 64;                           // loads of a chunk of V
