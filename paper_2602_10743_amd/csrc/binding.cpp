@@ -932,7 +932,11 @@ struct WindowAttn : torch::autograd::Function<WindowAttn> {
 Tensor window_attn(const Tensor& q, const Tensor& k, const Tensor& v, int64_t window, int64_t sinks, const Opt& len,
                    const c10::optional<double>& scale) {
     const kla_window_desc d = check_window(q, k, v, window, sinks, len, scale, true);
+    bool grad = false;   // or a tangent, which the node refuses
+    for (const Tensor* t : {&q, &k, &v})
+        grad = grad || (at::GradMode::is_enabled() && t->requires_grad()) || t->_fw_grad(0).defined();
     py::gil_scoped_release unlocked;
+    if (!grad) return win_forward(d, dense(q), dense(k), dense(v), len, c10::nullopt, false, false)[0];   // no context
     return WindowAttn::apply(q, k, v, len, d);
 }
 

@@ -279,3 +279,26 @@ def test_step_of_peaked_rows(kla, S, window, H, Hk, d):
     got = kla.kla_window_attn_step(X["q"][:, 0], X["k"][:, -1].contiguous(), X["v"][:, -1].contiguous(), X["k"].clone(),
                                    X["v"].clone(), torch.full((S,), window - 1, dtype=torch.int32, device=DEV), scale=1.0)
     check("y", got["y"][:, None], normed(x, window, 0, grads=False)["y"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_context_without_a_gradient(kla, dtype):
+    """Where nothing takes a gradient the differentiable form holds y and nothing more, with the same y."""
+    x = dev(make(2, 1100, 2, 1, 64, dtype, lengths=[1100, 901], seed=25))
+    args = (x["q"], x["k"], x["v"], 1100, 3, x["len"])
+    leaf = x["q"].clone().requires_grad_(True)
+    with_context = kla.kla_window_attn(leaf, *args[1:]).detach()
+    workspace = kla.kla_window_attn_forward(*args)["y"]
+    for given, off in ((args, False), ((leaf,) + args[1:], True)):
+        with torch.set_grad_enabled(not off):
+            peaks = []
+            for call in (lambda: kla.kla_window_attn_forward(*args)["y"], lambda: kla.kla_window_attn(*given)):
+                torch.cuda.synchronize()
+                torch.cuda.reset_peak_memory_stats()
+                before = torch.cuda.memory_allocated()
+                y = call()
+                peaks.append(torch.cuda.max_memory_allocated() - before)
+        assert not y.requires_grad and torch.equal(y, with_context) and torch.equal(y, workspace)
+        assert peaks[1] == peaks[0], peaks
+    with torch.autograd.forward_ad.dual_level(), pytest.raises((NotImplementedError, RuntimeError)):
+        kla.kla_window_attn(torch.autograd.forward_ad.make_dual(args[0], torch.ones_like(args[0])), *args[1:])
