@@ -288,17 +288,18 @@ def test_no_context_without_a_gradient(kla, dtype):
     args = (x["q"], x["k"], x["v"], 1100, 3, x["len"])
     leaf = x["q"].clone().requires_grad_(True)
     with_context = kla.kla_window_attn(leaf, *args[1:]).detach()
-    workspace = kla.kla_window_attn_forward(*args)["y"]
+    raw = kla.kla_window_attn_forward(*args)["y"]
     for given, off in ((args, False), ((leaf,) + args[1:], True)):
         with torch.set_grad_enabled(not off):
             peaks = []
             for call in (lambda: kla.kla_window_attn_forward(*args)["y"], lambda: kla.kla_window_attn(*given)):
                 torch.cuda.synchronize()
                 torch.cuda.reset_peak_memory_stats()
-                before = torch.cuda.memory_allocated()
+                asked = lambda n: torch.cuda.memory_stats()["requested_bytes.all." + n]
+                before = asked("current")
                 y = call()
-                peaks.append(torch.cuda.max_memory_allocated() - before)
-        assert not y.requires_grad and torch.equal(y, with_context) and torch.equal(y, workspace)
+                peaks.append(asked("peak") - before)
+        assert not y.requires_grad and torch.equal(y, with_context) and torch.equal(y, raw)
         assert peaks[1] == peaks[0], peaks
     with torch.autograd.forward_ad.dual_level(), pytest.raises((NotImplementedError, RuntimeError)):
         kla.kla_window_attn(torch.autograd.forward_ad.make_dual(args[0], torch.ones_like(args[0])), *args[1:])
