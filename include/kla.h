@@ -568,8 +568,8 @@ kla_status kla_qk_norm_rope_backward(const kla_rope_desc* desc, const void* q, c
  * Scores, softmax and sums are fp32.  With bf16 inputs P and its gradient enter their products
  * rounded to bf16, and y is divided by the sum of the rounded weights; positions under 128, and all rows
  * where min(window + sinks, Tk) < 256, take them in two parts, 16 bits; the step rounds P.  With fp32
- * inputs everything stays fp32.  |scale q . k| has to stay below 2^30 ln 2; a row whose largest score
- * is beyond is right or NaN.  A row whose visible scores are all -inf has y = 0 and no gradient.
+ * inputs everything stays fp32.  |scale q . k| has to stay below 2^30 ln 2; a row that sees a finite
+ * score beyond is right or NaN.  A row whose visible scores are all -inf has y = 0 and no gradient.
  * What is masked has no influence, finite or not.  The backward takes y and saved of the forward and
  * returns dq, dk, dv (dtype, all required).  scale > 0 and finite, window >= 1, sinks in 0 .. 64,
  * sinks + window <= 2^30, H d <= 2^22, Tk <= 2^28, in the step S >= 1 and S H <= 2^20, else B >= 1 and
